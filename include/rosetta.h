@@ -592,6 +592,114 @@ rosetta_status rosetta_seglut_precision(int function, const double *tau, uint32_
 rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log,
                                     uint64_t *out);
 
+/* ---- the clear side: 8-bit layers and the vocabulary loss ----------------
+ *
+ * What a hybrid program runs in the clear around the encrypted tables
+ * (Sec. 2.3: norms, projections, the head), and the loss whose
+ * exponential is the perplexity that Sec. 5 judges the tables by, with its
+ * gradient.
+ *
+ * CONVENTIONS:
+ *  - Matrices are row-major device arrays with contiguous rows; a `_stride`
+ *    is the distance of two rows in elements, at least the row's length.  No
+ *    alignment beyond the element's own is needed; rows that start on 16
+ *    bytes are read fastest.
+ *  - Types are rosetta_dtype.  Sums, norms, softmax statistics and scales are
+ *    held in 32 bits; 8-bit products are summed exactly.
+ *  - 8-bit rows: value = scale[row] * q, q in [-127, 127], scale = max |value|
+ *    / 127, rounded to nearest, ties to even.  A row of zeros has scale 0; a
+ *    row with a NaN or an infinity (or whose squares overflow 32 bits, in
+ *    the norm) has a scale that is not finite, or NaN, and unspecified q.
+ *  - Outputs must not overlap inputs or each other (ROSETTA_ERR_ALIAS) unless
+ *    stated.  rows == 0 is a successful no-op once sizes are valid, except
+ *    that gradients of weights are then zeros.
+ *  - Every sum is taken in an order that the sizes alone decide: equal inputs
+ *    give equal bits. */
+typedef enum { ROSETTA_F32 = 0, ROSETTA_BF16 = 1, ROSETTA_F16 = 2 } rosetta_dtype;
+
+/* Root-mean-square norm with the residual's addition, for `rows` rows of `dim`:
+ *   h = x + residual (residual NULL: h = x),
+ *   inv_rms = 1 / sqrt(mean h^2 + eps),  y = h * inv_rms * weight,
+ * and y in 8 bits (q, scale).  The norm reads the unrounded 32-bit sum.
+ * x, residual, h, y have type `dtype`, weight [dim] (NULL: ones) that type or
+ * ROSETTA_F32 (`weight_dtype`).  Each of h, y, (q, scale), inv_rms may be NULL
+ * and is then not written; q and scale go together.  h may be exactly x or
+ * residual (same address and stride).  eps >= 0. */
+rosetta_status rosetta_rms_norm(const void *x, size_t x_stride, const void *residual,
+                                size_t residual_stride, const void *weight, int weight_dtype,
+                                int dtype, size_t rows, size_t dim, float eps, void *h,
+                                size_t h_stride, void *y, size_t y_stride, int8_t *q,
+                                size_t q_stride, float *scale, float *inv_rms, void *stream);
+
+/* Gradient of the norm: given gy (of y) and gh (of h, from the residual
+ * stream; NULL: none), h and inv_rms as rosetta_rms_norm left them,
+ *   gx = gh + inv_rms gy w - h inv_rms^3 / dim * sum(gy w h),
+ *   gweight[c] = sum_rows gy h inv_rms   (32 bits; NULL: not wanted),
+ * gx being the gradient of x and of residual alike.  Through 8 bits the
+ * gradient passes straight (gy is then that of the values).  gx may be exactly
+ * gy or gh (same address and stride).  With gweight, `workspace` holds
+ * rosetta_rms_norm_backward_workspace_bytes bytes (else ROSETTA_ERR_SIZE). */
+rosetta_status rosetta_rms_norm_backward(const void *gy, size_t gy_stride, const void *gh,
+                                         size_t gh_stride, const void *h, size_t h_stride,
+                                         const void *weight, int weight_dtype,
+                                         const float *inv_rms, int dtype, size_t rows, size_t dim,
+                                         void *gx, size_t gx_stride, float *gweight,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+size_t rosetta_rms_norm_backward_workspace_bytes(size_t rows, size_t dim);
+
+/* Rows to 8 bits (weights, or what comes out of a table), and back to the
+ * values they stand for, rounded to `dtype`. */
+rosetta_status rosetta_quantize_rows(const void *x, size_t x_stride, int dtype, size_t rows,
+                                     size_t dim, int8_t *q, size_t q_stride, float *scale,
+                                     void *stream);
+rosetta_status rosetta_dequantize_rows(const int8_t *q, size_t q_stride, const float *scale,
+                                       int dtype, size_t rows, size_t dim, void *out,
+                                       size_t out_stride, void *stream);
+
+/* 8-bit matrix product with a scale per token and per channel:
+ *   out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] b[j][k] + bias[j]
+ * for i < m tokens, j < n channels; a [m][k], b [n][k] (a row per channel),
+ * bias [n] in 32 bits or NULL, out of type out_dtype.  The sum is exact (any
+ * 8-bit values); k <= 131071 (else ROSETTA_ERR_UNSUPPORTED); k = 0 gives the
+ * bias. */
+rosetta_status rosetta_q8_matmul(const int8_t *a, size_t a_stride, const float *a_scale,
+                                 const int8_t *b, size_t b_stride, const float *b_scale,
+                                 const float *bias, void *out, size_t out_stride, int out_dtype,
+                                 size_t m, size_t n, size_t k, void *stream);
+
+/* Softmax cross entropy over a vocabulary, straight from hidden states h
+ * [rows][dim] and head weights w [vocab][dim] (both of type `dtype`,
+ * ROSETTA_BF16 or ROSETTA_F16; ROSETTA_F32 is ROSETTA_ERR_UNSUPPORTED, its
+ * products would not run on the matrix cores).  With l[t][v] = <h_t, w_v>,
+ * never stored whole:
+ *   lse[t] = log sum_v exp l[t][v],   loss[t] = lse[t] - l[t][targets[t]];
+ * a row whose target is ignore_index has loss 0; any other target outside
+ * [0, vocab) gives loss NaN.  exp(mean loss over the rows that count) is the
+ * perplexity.  workspace: rosetta_cross_entropy_workspace_bytes bytes. */
+rosetta_status rosetta_cross_entropy(const void *h, size_t h_stride, const void *w,
+                                     size_t w_stride, int dtype, const int64_t *targets,
+                                     int64_t ignore_index, size_t rows, size_t dim, size_t vocab,
+                                     float *loss, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+size_t rosetta_cross_entropy_workspace_bytes(size_t rows, size_t dim, size_t vocab);
+
+/* Its gradients: with gloss [rows] the gradient of each row's loss,
+ *   gl[t][v] = gloss[t] (exp(l[t][v] - lse[t]) - [v = targets[t]]),
+ *   gh = gl w,   gw = gl^T h
+ * (of type `dtype`; either may be NULL).  Rows that are ignored, or whose
+ * target is outside [0, vocab), take no part.  The logits are made again, a
+ * piece of the vocabulary at a time; gl is held for one piece, in multiples of
+ * the largest |gloss|, rounded to `dtype`.  workspace: rosetta_cross_entropy_backward_workspace_bytes
+ * bytes. */
+rosetta_status rosetta_cross_entropy_backward(const void *h, size_t h_stride, const void *w,
+                                              size_t w_stride, int dtype, const int64_t *targets,
+                                              int64_t ignore_index, const float *lse,
+                                              const float *gloss, size_t rows, size_t dim,
+                                              size_t vocab, void *gh, size_t gh_stride, void *gw,
+                                              size_t gw_stride, void *workspace,
+                                              size_t workspace_bytes, void *stream);
+size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, size_t vocab);
+
 /* ---- test helpers: host memory, deterministic from the seed ------------ */
 
 /* Key generation for the PBS (Sec. 2.2.2 "TFHE Scheme": LWE encryption of

@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librosetta.so")
 SOURCES = ["kernels.hip", "exact_fft.hip", "keyswitch.hip", "lwe_ops.hip", "abi.cpp", "scratch.cpp", "noalloc.hip",
-           "host_helpers.cpp", "seglut.cpp", "lookup.cpp"]
+           "host_helpers.cpp", "seglut.cpp", "lookup.cpp", "clear_abi.cpp", "clear_norm.hip",
+           "q8_matmul.hip", "cross_entropy.hip"]
 ARCH = os.environ.get("ROSETTA_OFFLOAD_ARCH", "gfx950")
 
 

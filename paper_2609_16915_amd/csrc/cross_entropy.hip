@@ -1,0 +1,399 @@
+// Softmax cross entropy over a vocabulary from hidden states and head weights,
+// and its gradients.  The logits live in registers only.
+//
+// Forward: tiles of logits (X: rows of w, Y: rows of h), each reduced to a
+// maximum and a sum of exponentials per row and tile, joined afterwards.
+// Backward, a piece of the vocabulary at a time: the tiles again, turned into
+// gl = g (softmax - one-hot) and stored for the piece both ways round, then
+// gh += gl w and gw = gl^T h as products of rows.
+#include <cmath>
+
+#include "mma_tile.hpp"
+
+namespace rosetta {
+
+namespace {
+
+constexpr int BX = 128, BY = 128, WX = 2, WY = 2;
+constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
+
+size_t up(size_t a, size_t b) { return (a + b - 1) / b * b; }
+size_t tiles(size_t a, size_t b) { return (a + b - 1) / b; }
+
+struct Stat {
+  float top, sum;
+};
+
+// (a, b) as one: sums of exponentials above the larger maximum
+__device__ inline Stat join(Stat a, Stat b) {
+  const float top = fmaxf(a.top, b.top);
+  if (top == -INFINITY) return {top, a.sum + b.sum};
+  return {top, a.sum * __expf(a.top - top) + b.sum * __expf(b.top - top)};
+}
+
+__device__ inline bool counts(int64_t target, int64_t ignore, size_t vocab) {
+  return target != ignore && target >= 0 && target < (int64_t)vocab;
+}
+
+// part[tile of x][row], and the logit of each row's target
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(64 * WX *WY)
+k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) {
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  extern __shared__ char lds[];
+  const unsigned gx = (unsigned)((a.vocab + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
+  unsigned tx, ty;
+  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  const int64_t bytes = (int64_t)a.dim * sizeof(T);
+  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab, bytes};
+  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows, bytes};
+  v4f acc[Tl::TX][Tl::TY] = {};
+  Tl::template run<ALIGNED>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes, lds, acc);
+
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  Stat *joint = (Stat *)lds;  // [WX][BY]
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int y = Tl::y_at() + 16 * j;
+    const int64_t row = (int64_t)ty * BY + y;
+    const int64_t target = row < (int64_t)a.rows ? a.targets[row] : -1;
+    Stat s{-INFINITY, 0.f};
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (x0 + 4 * i + r >= (int64_t)a.vocab) acc[i][j][r] = -INFINITY;
+        s.top = fmaxf(s.top, acc[i][j][r]);
+      }
+    const float low = s.top == -INFINITY ? 0.f : s.top;
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (x0 + 4 * i + r == target && row < (int64_t)a.rows) at_target[row] = acc[i][j][r];
+        s.sum += __expf(acc[i][j][r] - low);
+      }
+#pragma unroll
+    for (int m = 16; m <= 32; m <<= 1)
+      s = join(s, Stat{__shfl_xor(s.top, m), __shfl_xor(s.sum, m)});
+    if (threadIdx.x % 64 < 16) joint[(threadIdx.x / 64 % WX) * BY + y] = s;
+  }
+  __syncthreads();
+  for (int y = threadIdx.x; y < BY; y += Tl::THREADS) {
+    const int64_t row = (int64_t)ty * BY + y;
+    if (row >= (int64_t)a.rows) break;
+    Stat s = joint[y];
+    for (int w = 1; w < WX; ++w) s = join(s, joint[w * BY + y]);
+    part[(size_t)tx * a.rows + row] = s;
+  }
+}
+
+// The tiles' parts of 16 rows joined, 16 threads to a row.
+__global__ void __launch_bounds__(256)
+k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
+            const float *__restrict__ at_target) {
+  __shared__ Stat lds[16][16];
+  const int r = threadIdx.x % 16, p = threadIdx.x / 16;
+  const size_t row = (size_t)blockIdx.x * 16 + r;
+  Stat s{-INFINITY, 0.f};
+  if (row < a.rows)
+    for (size_t t = p; t < nt; t += 16) s = join(s, part[t * a.rows + row]);
+  lds[p][r] = s;
+  __syncthreads();
+  if (p == 0 && row < a.rows) {
+    for (int q = 1; q < 16; ++q) s = join(s, lds[q][r]);
+    const float lse = s.top + logf(s.sum);
+    a.lse[row] = lse;
+    const int64_t target = a.targets[row];
+    a.loss[row] = target == a.ignore_index ? 0.f
+                  : counts(target, a.ignore_index, a.vocab) ? lse - at_target[row]
+                                                           : NAN;
+  }
+}
+
+// Factors of the rows of gl, coef[row], and what their products are multiplied
+// by in the end, coef[rows].  gl is held in 16 bits as multiples of max |gloss| /
+// GL_UP: the term -1 of a target is then exact in either type where all rows
+// weigh the same (rounding gloss itself put one error on all of them: gradients
+// off by 0.0026 of their norm, 0.0017 so), and f16 has room for probabilities
+// down to 2^-28.
+__global__ void __launch_bounds__(1024) k_loss_coef(LossArgs a, float *__restrict__ coef) {
+  __shared__ float lds[16];
+  float top = 0.f;
+  for (size_t t = threadIdx.x; t < a.rows; t += 1024)
+    if (counts(a.targets[t], a.ignore_index, a.vocab)) top = fmaxf(top, fabsf(a.gloss[t]));
+  for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = top;
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
+  const bool some = top > 0.f;
+  for (size_t t = threadIdx.x; t < a.rows; t += 1024) {
+    const float g = counts(a.targets[t], a.ignore_index, a.vocab) ? a.gloss[t] : 0.f;
+    coef[t] = some ? g / top * GL_UP : g;
+  }
+  if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
+}
+
+// gl of the vocabulary rows [v0, v0 + vp): as gl [rows][vp] and as gl_t
+// [vp][ld_t], zeros beyond the vocabulary and the rows.
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(64 * WX *WY)
+k_loss_grad_tile(LossArgs a, size_t v0, size_t vp, size_t ld_t, const float *__restrict__ coef,
+                 T *__restrict__ gl, T *__restrict__ gl_t) {
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  extern __shared__ char lds[];
+  const unsigned gx = (unsigned)(vp / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
+  unsigned tx, ty;
+  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  const int64_t bytes = (int64_t)a.dim * sizeof(T);
+  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab, bytes};
+  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows, bytes};
+  v4f acc[Tl::TX][Tl::TY] = {};
+  Tl::template run<ALIGNED>(X, Y, (int64_t)(v0 + (size_t)tx * BX), (int64_t)ty * BY, 0, bytes, lds,
+                            acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    const bool in = row < (int64_t)a.rows;
+    const float c = in ? coef[row] : 0.f, lse = in ? a.lse[row] : 0.f;
+    const int64_t target = in ? a.targets[row] : -1;
+    float f[4 * Tl::TX];
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t v = (int64_t)v0 + x0 + 4 * i + r;
+        const float p = __expf(acc[i][j][r] - lse) - (v == target ? 1.f : 0.f);
+        f[4 * i + r] = in && c != 0.f && v < (int64_t)a.vocab ? p * c : 0.f;
+      }
+    if (gl && in) store_run(gl + row * (int64_t)vp + x0, 4 * Tl::TX, f);
+    if (gl_t && row < (int64_t)ld_t) {
+#pragma unroll
+      for (int i = 0; i < 4 * Tl::TX; ++i) gl_t[(x0 + i) * (int64_t)ld_t + row] = (T)f[i];
+    }
+  }
+}
+
+// out [cols][ld] = in [rows][cols] the other way round, zeros in columns
+// [rows, ld).
+template <class T>
+__global__ void __launch_bounds__(256)
+k_transpose(const T *__restrict__ in, size_t in_stride, size_t rows, size_t cols,
+            T *__restrict__ out, size_t ld) {
+  __shared__ T lds[64][66];
+  const size_t r0 = (size_t)blockIdx.x * 64, c0 = (size_t)blockIdx.y * 64;
+  const int l = threadIdx.x % 64;
+  for (int i = threadIdx.x / 64; i < 64; i += 4)
+    lds[i][l] = r0 + i < rows && c0 + l < cols ? in[(r0 + i) * in_stride + c0 + l] : (T)0.f;
+  __syncthreads();
+  for (int i = threadIdx.x / 64; i < 64; i += 4)
+    if (c0 + i < cols && r0 + l < ld) out[(c0 + i) * ld + r0 + l] = lds[l][i];
+}
+
+// part[split][row][d] (+)= gl [rows][vp] times w_t [dim][vp]: split s takes an
+// equal run of the piece's vocabulary.
+template <class T>
+__global__ void __launch_bounds__(64 * WX *WY)
+k_loss_gh_tile(size_t rows, size_t dim, size_t vp, const T *__restrict__ gl,
+               const T *__restrict__ w_t, float *__restrict__ part, size_t run, int add) {
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  extern __shared__ char lds[];
+  const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
+  const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
+  unsigned tx, ty;
+  band_tile(b % (gx * gy), gx, gy, tx, ty);
+  const int64_t bytes = (int64_t)vp * sizeof(T);
+  const Operand X{(const char *)w_t, bytes, (int64_t)dim, bytes};
+  const Operand Y{(const char *)gl, bytes, (int64_t)rows, bytes};
+  const int64_t k0 = (int64_t)(split * run * sizeof(T));
+  int64_t k1 = k0 + (int64_t)(run * sizeof(T));
+  k1 = k1 < bytes ? k1 : bytes;
+  v4f acc[Tl::TX][Tl::TY] = {};
+  Tl::template run<true>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, k0, k1, lds, acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    if (row >= (int64_t)rows || x0 >= (int64_t)dim) continue;
+    float *out = part + ((size_t)split * rows + row) * dim + x0;
+    float f[4 * Tl::TX];
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        f[4 * i + r] = acc[i][j][r];
+        if (add && x0 + 4 * i + r < (int64_t)dim) f[4 * i + r] += out[4 * i + r];
+      }
+    store_run(out, (int64_t)dim - x0, f);
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t dim,
+               const float *__restrict__ coef, T *__restrict__ out, size_t out_stride) {
+  const size_t c = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (c >= dim) return;
+  for (size_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    float s = 0.f;
+    for (int q = 0; q < splits; ++q) s += part[((size_t)q * rows + row) * dim + c];
+    out[row * out_stride + c] = (T)(s * coef[rows]);
+  }
+}
+
+// gw rows [v0, ..) = gl_t [vp][ld_t] times h_t [dim][ld_t]
+template <class T>
+__global__ void __launch_bounds__(64 * WX *WY)
+k_loss_gw_tile(LossArgs a, size_t v0, size_t vp, size_t ld_t, const float *__restrict__ coef,
+               const T *__restrict__ gl_t, const T *__restrict__ h_t) {
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  extern __shared__ char lds[];
+  const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)(vp / BY);
+  unsigned tx, ty;
+  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  const int64_t bytes = (int64_t)ld_t * sizeof(T);
+  const Operand X{(const char *)h_t, bytes, (int64_t)a.dim, bytes};
+  const Operand Y{(const char *)gl_t, bytes, (int64_t)vp, bytes};
+  v4f acc[Tl::TX][Tl::TY] = {};
+  Tl::template run<true>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes, lds, acc);
+  const float back = coef[a.rows];
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t v = (int64_t)v0 + (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    if (v >= (int64_t)a.vocab || x0 >= (int64_t)a.dim) continue;
+    float f[4 * Tl::TX];
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[4 * i + r] = acc[i][j][r] * back;
+    store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, (int64_t)a.dim - x0, f);
+  }
+}
+
+// Pieces of the vocabulary and what the workspace holds.
+struct Plan {
+  size_t vp, pieces, ld_t, splits, run;
+  size_t coef, gl, gl_t, w_t, h_t, part, bytes;
+};
+
+Plan plan(size_t rows, size_t dim, size_t vocab) {
+  constexpr size_t BUDGET = (size_t)512 << 20;
+  Plan p{};
+  p.ld_t = up(rows, 64);
+  const size_t column = 2 * (rows + p.ld_t + dim);
+  size_t vp = BUDGET / column / BX * BX;
+  vp = vp < BX ? BX : vp;
+  p.pieces = tiles(up(vocab, BX), vp);
+  p.vp = up(tiles(vocab, p.pieces), BX);
+  p.pieces = tiles(vocab, p.vp);
+  // enough blocks for gh: its tiles are few, its sums long
+  const size_t t = tiles(dim, BX) * tiles(rows, BY);
+  size_t s = 512 / t;
+  const size_t most = p.vp / 512;
+  s = s > most ? most : s;
+  p.splits = s < 1 ? 1 : s;
+  p.run = up(tiles(p.vp, p.splits), 64);
+  p.splits = tiles(p.vp, p.run);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes, 256);
+    return here;
+  };
+  p.coef = take((rows + 1) * 4);
+  p.gl = take(rows * p.vp * 2);
+  p.gl_t = take(p.vp * p.ld_t * 2);
+  p.w_t = take(dim * p.vp * 2);
+  p.h_t = take(dim * p.ld_t * 2);
+  p.part = take(p.splits * rows * dim * 4);
+  p.bytes = at;
+  return p;
+}
+
+template <class T>
+hipError_t forward(const LossArgs &a, hipStream_t st) {
+  const size_t gx = tiles(a.vocab, BX), gy = tiles(a.rows, BY);
+  Stat *part = (Stat *)a.workspace;
+  float *at_target = (float *)(part + gx * a.rows);
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * 2), (int64_t)a.vocab,
+                  (int64_t)(a.dim * 2)};
+  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * 2), (int64_t)a.rows,
+                  (int64_t)(a.dim * 2)};
+  const bool al = rows_aligned(X) && rows_aligned(Y);
+  auto k = al ? k_loss_tile<T, true> : k_loss_tile<T, false>;
+  hipLaunchKernelGGL(k, dim3((unsigned)(gx * gy)), dim3(Tl::THREADS), Tl::LDS, st, a, part,
+                     at_target);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_loss_join, dim3((unsigned)tiles(a.rows, 16)), dim3(256), 0, st, a, part, gx,
+                     at_target);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t backward(const LossArgs &a, hipStream_t st) {
+  const Plan p = plan(a.rows, a.dim, a.vocab);
+  using Tl = Tile<T, BX, BY, WX, WY>;
+  char *ws = (char *)a.workspace;
+  float *coef = (float *)(ws + p.coef), *part = (float *)(ws + p.part);
+  T *gl = a.gh ? (T *)(ws + p.gl) : nullptr, *gl_t = a.gw ? (T *)(ws + p.gl_t) : nullptr;
+  T *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
+  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * 2), (int64_t)a.vocab,
+                  (int64_t)(a.dim * 2)};
+  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * 2), (int64_t)a.rows,
+                  (int64_t)(a.dim * 2)};
+  const bool al = rows_aligned(X) && rows_aligned(Y);
+  hipLaunchKernelGGL(k_loss_coef, dim3(1), dim3(1024), 0, st, a, coef);
+  if (a.gw)
+    hipLaunchKernelGGL(k_transpose<T>,
+                       dim3((unsigned)tiles(p.ld_t, 64), (unsigned)tiles(a.dim, 64)), dim3(256), 0,
+                       st, (const T *)a.h, a.h_stride, a.rows, a.dim, h_t, p.ld_t);
+  hipError_t e = hipGetLastError();
+  for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
+    const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
+    auto k = al ? k_loss_grad_tile<T, true> : k_loss_grad_tile<T, false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(p.vp / BX * tiles(a.rows, BY))), dim3(Tl::THREADS),
+                       Tl::LDS, st, a, v0, p.vp, p.ld_t, coef, gl, gl_t);
+    if (a.gh) {
+      hipLaunchKernelGGL(k_transpose<T>,
+                         dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), dim3(256), 0,
+                         st, (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
+      hipLaunchKernelGGL(k_loss_gh_tile<T>,
+                         dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))),
+                         dim3(Tl::THREADS), Tl::LDS, st, a.rows, a.dim, p.vp, gl, w_t, part, p.run,
+                         i > 0);
+    }
+    if (a.gw)
+      hipLaunchKernelGGL(k_loss_gw_tile<T>, dim3((unsigned)(tiles(a.dim, BX) * (p.vp / BY))),
+                         dim3(Tl::THREADS), Tl::LDS, st, a, v0, p.vp, p.ld_t, coef, gl_t, h_t);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && a.gh) {
+    hipLaunchKernelGGL(k_loss_gh_join<T>, dim3((unsigned)tiles(a.dim, 256), (unsigned)(a.rows < 32768 ? a.rows : 32768)),
+                       dim3(256), 0, st, part, (int)p.splits, a.rows, a.dim, coef, (T *)a.gh,
+                       a.gh_stride);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+size_t cross_entropy_workspace(size_t rows, size_t dim, size_t vocab) {
+  return tiles(vocab, BX) * rows * sizeof(Stat) + rows * 4;
+}
+size_t cross_entropy_backward_workspace(size_t rows, size_t dim, size_t vocab) {
+  return plan(rows, dim, vocab).bytes;
+}
+
+hipError_t launch_cross_entropy(const LossArgs &a, hipStream_t st) {
+  return a.dtype == ROSETTA_BF16 ? forward<bf16>(a, st) : forward<f16>(a, st);
+}
+hipError_t launch_cross_entropy_backward(const LossArgs &a, hipStream_t st) {
+  return a.dtype == ROSETTA_BF16 ? backward<bf16>(a, st) : backward<f16>(a, st);
+}
+
+}  // namespace rosetta

@@ -10,7 +10,9 @@ raised.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -142,6 +144,28 @@ SIGNATURES.update({
     "rosetta_lookup_workspace_offset": (C.c_size_t, [_pp, _lpp, C.c_size_t, C.c_uint32]),
     "rosetta_lookup_eval": (_ST, [_u64p, _u64p, _u64p, _u64p, _u64p, _u64p, _u64p, _u64p,
                                   C.c_size_t, _pp, _lpp, _u64p, C.c_size_t, C.c_void_p]),
+})
+
+_sz, _i32, _i64, _f32 = C.c_size_t, C.c_int, C.c_int64, C.c_float
+SIGNATURES.update({
+    "rosetta_rms_norm": (_ST, [_u64p, _sz, _u64p, _sz, _u64p, _i32, _i32, _sz, _sz, _f32, _u64p,
+                               _sz, _u64p, _sz, _u64p, _sz, _u64p, _u64p, C.c_void_p]),
+    "rosetta_rms_norm_backward": (_ST, [_u64p, _sz, _u64p, _sz, _u64p, _sz, _u64p, _i32, _u64p,
+                                        _i32, _sz, _sz, _u64p, _sz, _u64p, _u64p, _sz,
+                                        C.c_void_p]),
+    "rosetta_rms_norm_backward_workspace_bytes": (_sz, [_sz, _sz]),
+    "rosetta_quantize_rows": (_ST, [_u64p, _sz, _i32, _sz, _sz, _u64p, _sz, _u64p, C.c_void_p]),
+    "rosetta_dequantize_rows": (_ST, [_u64p, _sz, _u64p, _i32, _sz, _sz, _u64p, _sz,
+                                      C.c_void_p]),
+    "rosetta_q8_matmul": (_ST, [_u64p, _sz, _u64p, _u64p, _sz, _u64p, _u64p, _u64p, _sz, _i32,
+                                _sz, _sz, _sz, C.c_void_p]),
+    "rosetta_cross_entropy": (_ST, [_u64p, _sz, _u64p, _sz, _i32, _u64p, _i64, _sz, _sz, _sz,
+                                    _u64p, _u64p, _u64p, _sz, C.c_void_p]),
+    "rosetta_cross_entropy_workspace_bytes": (_sz, [_sz, _sz, _sz]),
+    "rosetta_cross_entropy_backward": (_ST, [_u64p, _sz, _u64p, _sz, _i32, _u64p, _i64, _u64p,
+                                             _u64p, _sz, _sz, _sz, _u64p, _sz, _u64p, _sz, _u64p,
+                                             _sz, C.c_void_p]),
+    "rosetta_cross_entropy_backward_workspace_bytes": (_sz, [_sz, _sz, _sz]),
 })
 
 FUNCTIONS = {"inv": 0, "inv_sqrt": 1, "silu": 2, "gelu": 3, "exp": 4}
@@ -593,6 +617,276 @@ def sample_extract(glwe_in, N: int, out=None, stream=None):
     _check(lib().rosetta_sample_extract(_dev(glwe_in, "glwe_in"), _dev(out, "big_out"), batch, N,
                                         _stream(stream)))
     return out
+
+
+# --------------------------------------------------------------------------
+# the clear side: 8-bit layers and the vocabulary loss (device)
+# --------------------------------------------------------------------------
+
+def _types():
+    torch = _torch()
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _type(dtype, name: str) -> int:
+    code = _types().get(dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, not {dtype}")
+    return code
+
+
+def _mat(t, name: str, dtype=None, shape=None):
+    """(address, row stride, rows, columns) of a device matrix with contiguous
+    rows; a vector is one row.  TypeError for the wrong kind of tensor,
+    ValueError for the wrong size, before any library call."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() > 2 or t.dim() < 1:
+        raise ValueError(f"{name} must be a matrix or one row, not {tuple(t.shape)}")
+    rows, cols = t.shape if t.dim() == 2 else (1, t.shape[0])
+    if shape is not None and (rows, cols) != tuple(shape):
+        raise ValueError(f"{name} is {rows} x {cols}, the call needs {shape[0]} x {shape[1]}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a torch tensor on a ROCm device")
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    stride = t.stride(0) if t.dim() == 2 and rows > 1 else cols
+    return t.data_ptr(), stride, rows, cols
+
+
+def _vec(t, name: str, dtype, count: int) -> int:
+    """Address of a contiguous device vector of `count` elements."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError(f"{name} must be a torch tensor of {dtype}")
+    _expect(t, name, count)
+    if not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous on a ROCm device")
+    return t.data_ptr()
+
+
+def _made(out, name: str, shape, dtype, like):
+    """`out` checked, or a new tensor of that shape and type."""
+    if out is None:
+        return _torch().empty(shape, dtype=dtype, device=like.device)
+    _mat(out, name, dtype, shape)
+    return out
+
+
+def _scratch(workspace, need: int, like):
+    """`workspace` checked, or a new one: (address, bytes, tensor)."""
+    if workspace is None:
+        workspace = _torch().empty(need, dtype=_torch().uint8, device=like.device)
+    have = workspace.numel() * workspace.element_size()
+    if have < need:
+        raise ValueError(f"workspace holds {have} bytes, the call needs {need}")
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be contiguous on a ROCm device")
+    return workspace.data_ptr(), have, workspace
+
+
+def _on_its_stream(call):
+    """With a stream given, what `call` allocates (outputs, workspaces) belongs to
+    that stream, so that no memory is reused while its work still runs."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with _torch().cuda.stream(stream):
+            return call(*args, stream=stream, **kw)
+    return on_stream
+
+
+class NormQ8(NamedTuple):
+    """What rms_norm_q8 returns: the 8-bit rows and their scales, h = x +
+    residual (None without a residual), 1 / rms, and y where it was asked for."""
+    q: object
+    scale: object
+    h: object
+    inv_rms: object
+    y: object
+
+
+def _norm(x, weight, eps, residual, h, y, q, scale, inv_rms, stream):
+    torch = _torch()
+    xp, xs, rows, dim = _mat(x, "x")
+    dt = _type(x.dtype, "x")
+    rp = rs = 0
+    if residual is not None:
+        rp, rs, _, _ = _mat(residual, "residual", x.dtype, (rows, dim))
+    wp, wt = None, dt
+    if weight is not None:
+        if weight.dtype not in (x.dtype, torch.float32):
+            raise TypeError(f"weight must be {x.dtype} or float32, not {weight.dtype}")
+        wp, wt = _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
+    hp, hs = _mat(h, "h", x.dtype, (rows, dim))[:2] if h is not None else (None, dim)
+    yp, ys = _mat(y, "y", x.dtype, (rows, dim))[:2] if y is not None else (None, dim)
+    qp, qs = _mat(q, "q", torch.int8, (rows, dim))[:2] if q is not None else (None, dim)
+    sp = _vec(scale, "scale", torch.float32, rows) if scale is not None else None
+    ip = _vec(inv_rms, "inv_rms", torch.float32, rows) if inv_rms is not None else None
+    _check(lib().rosetta_rms_norm(xp, xs, rp or None, rs or dim, wp, wt, dt, rows, dim, eps, hp,
+                                  hs, yp, ys, qp, qs, sp, ip, _stream(stream)))
+
+
+@_on_its_stream
+def rms_norm_q8(x, weight, eps: float, residual=None, h=None, want_y: bool = False, q=None,
+                stream=None) -> NormQ8:
+    """RMS norm of x + residual ([rows][dim], float32, bfloat16 or float16) to
+    8 bits with a scale per row.  weight [dim] (None: ones) has x's type or
+    float32.  h may be x or residual, which it then replaces."""
+    torch = _torch()
+    _, _, rows, dim = _mat(x, "x")
+    if h is None and residual is not None:
+        h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+    q = _made(q, "q", (rows, dim), torch.int8, x)
+    ends = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    scale, inv_rms = ends.unbind(0)
+    y = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if want_y else None
+    _norm(x, weight, eps, residual, h, y, q, scale, inv_rms, stream)
+    return NormQ8(q, scale, h, inv_rms, y)
+
+
+@_on_its_stream
+def rms_norm(x, weight, eps: float, residual=None, h=None, y=None, stream=None):
+    """The same without the 8 bits: (y, h, inv_rms)."""
+    torch = _torch()
+    _, _, rows, dim = _mat(x, "x")
+    if h is None and residual is not None:
+        h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+    y = _made(y, "y", (rows, dim), x.dtype, x)
+    inv_rms = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _norm(x, weight, eps, residual, h, y, None, None, inv_rms, stream)
+    return y, h, inv_rms
+
+
+@_on_its_stream
+def rms_norm_backward(gy, h, weight, inv_rms, gh=None, gx=None, want_gweight: bool = True,
+                      workspace=None, stream=None):
+    """(gx, gweight) from gy, the gradient of y (or, passed straight through the
+    rounding, of the 8-bit values), and gh, that of h.  h is rms_norm's h, or its
+    x where there was no residual.  gx may be gy or gh; gweight is float32."""
+    torch = _torch()
+    yp, ys, rows, dim = _mat(gy, "gy")
+    dt = _type(gy.dtype, "gy")
+    hp, hs = _mat(h, "h", gy.dtype, (rows, dim))[:2]
+    gp, gs = _mat(gh, "gh", gy.dtype, (rows, dim))[:2] if gh is not None else (None, dim)
+    wp, wt = None, dt
+    if weight is not None:
+        if weight.dtype not in (gy.dtype, torch.float32):
+            raise TypeError(f"weight must be {gy.dtype} or float32, not {weight.dtype}")
+        wp, wt = _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
+    ip = _vec(inv_rms, "inv_rms", torch.float32, rows)
+    gx = _made(gx, "gx", (rows, dim), gy.dtype, gy)
+    gweight, wsp, wsb = None, None, 0
+    if want_gweight:
+        gweight = torch.empty(dim, dtype=torch.float32, device=gy.device)
+        wsp, wsb, workspace = _scratch(
+            workspace, lib().rosetta_rms_norm_backward_workspace_bytes(rows, dim), gy)
+    xp, xs = _mat(gx, "gx")[:2]
+    _check(lib().rosetta_rms_norm_backward(yp, ys, gp, gs, hp, hs, wp, wt, ip, dt, rows, dim, xp,
+                                           xs, gweight.data_ptr() if want_gweight else None, wsp,
+                                           wsb, _stream(stream)))
+    return gx, gweight
+
+
+@_on_its_stream
+def quantize_rows(x, q=None, scale=None, stream=None):
+    """Rows to 8 bits: (q, scale)."""
+    torch = _torch()
+    xp, xs, rows, dim = _mat(x, "x")
+    dt = _type(x.dtype, "x")
+    q = _made(q, "q", (rows, dim), torch.int8, x)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    qp, qs = _mat(q, "q")[:2]
+    _check(lib().rosetta_quantize_rows(xp, xs, dt, rows, dim, qp, qs,
+                                       _vec(scale, "scale", torch.float32, rows), _stream(stream)))
+    return q, scale
+
+
+@_on_its_stream
+def dequantize_rows(q, scale, dtype, out=None, stream=None):
+    """The values that 8-bit rows stand for."""
+    torch = _torch()
+    qp, qs, rows, dim = _mat(q, "q", torch.int8)
+    dt = _type(dtype, "dtype")
+    sp = _vec(scale, "scale", torch.float32, rows)
+    out = _made(out, "out", (rows, dim), dtype, q)
+    op, os_ = _mat(out, "out")[:2]
+    _check(lib().rosetta_dequantize_rows(qp, qs, sp, dt, rows, dim, op, os_, _stream(stream)))
+    return out
+
+
+@_on_its_stream
+def q8_matmul(a, a_scale, b, b_scale, bias=None, out_dtype=None, out=None, stream=None):
+    """a [m][k] times b [n][k] (a row per channel), both int8, with a scale per
+    row of each: [m][n] of out_dtype (default bfloat16)."""
+    torch = _torch()
+    out_dtype = (out.dtype if out is not None else torch.bfloat16) if out_dtype is None \
+        else out_dtype
+    ap, as_, m, k = _mat(a, "a", torch.int8)
+    bp, bs, n, kb = _mat(b, "b", torch.int8)
+    if kb != k:
+        raise ValueError(f"b is {n} x {kb}, the call needs rows of {k}")
+    sa = _vec(a_scale, "a_scale", torch.float32, m)
+    sb = _vec(b_scale, "b_scale", torch.float32, n)
+    bi = _vec(bias, "bias", torch.float32, n) if bias is not None else None
+    dt = _type(out_dtype, "out_dtype")
+    out = _made(out, "out", (m, n), out_dtype, a)
+    op, os_ = _mat(out, "out")[:2]
+    _check(lib().rosetta_q8_matmul(ap, as_, sa, bp, bs, sb, bi, op, os_, dt, m, n, k,
+                                   _stream(stream)))
+    return out
+
+
+@_on_its_stream
+def cross_entropy(h, w, targets, ignore_index: int = -100, workspace=None, stream=None):
+    """(loss, lse) per row, float32, of hidden states h [rows][dim] under head
+    weights w [vocab][dim] (bfloat16 or float16); targets int64."""
+    torch = _torch()
+    hp, hs, rows, dim = _mat(h, "h")
+    dt = _type(h.dtype, "h")
+    wp, ws, vocab, dw = _mat(w, "w", h.dtype)
+    if dw != dim:
+        raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
+    tp = _vec(targets, "targets", torch.int64, rows)
+    ends = torch.empty((2, rows), dtype=torch.float32, device=h.device)
+    loss, lse = ends.unbind(0)
+    sp, sb, workspace = _scratch(
+        workspace, lib().rosetta_cross_entropy_workspace_bytes(rows, dim, vocab), h)
+    _check(lib().rosetta_cross_entropy(hp, hs, wp, ws, dt, tp, ignore_index, rows, dim, vocab,
+                                       loss.data_ptr(), lse.data_ptr(), sp, sb, _stream(stream)))
+    return loss, lse
+
+
+@_on_its_stream
+def cross_entropy_backward(h, w, targets, lse, gloss, ignore_index: int = -100,
+                           want_gh: bool = True, want_gw: bool = True, gh=None, gw=None,
+                           workspace=None, stream=None):
+    """(gh, gw) from gloss [rows], the gradient of each row's loss, and lse as
+    cross_entropy returned it."""
+    torch = _torch()
+    hp, hs, rows, dim = _mat(h, "h")
+    dt = _type(h.dtype, "h")
+    wp, ws, vocab, dw = _mat(w, "w", h.dtype)
+    if dw != dim:
+        raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
+    tp = _vec(targets, "targets", torch.int64, rows)
+    ep = _vec(lse, "lse", torch.float32, rows)
+    gp = _vec(gloss, "gloss", torch.float32, rows)
+    gh = _made(gh, "gh", (rows, dim), h.dtype, h) if want_gh else None
+    gw = _made(gw, "gw", (vocab, dim), w.dtype, w) if want_gw else None
+    ghp, ghs = _mat(gh, "gh")[:2] if want_gh else (None, dim)
+    gwp, gws = _mat(gw, "gw")[:2] if want_gw else (None, dim)
+    sp, sb, workspace = _scratch(
+        workspace, lib().rosetta_cross_entropy_backward_workspace_bytes(rows, dim, vocab), h)
+    _check(lib().rosetta_cross_entropy_backward(hp, hs, wp, ws, dt, tp, ignore_index, ep, gp, rows,
+                                                dim, vocab, ghp, ghs, gwp, gws, sp, sb,
+                                                _stream(stream)))
+    return gh, gw
 
 
 # --------------------------------------------------------------------------
