@@ -9,9 +9,17 @@
 #include <cstddef>
 #include <cstdint>
 
-#include "rosetta.h"
+#include "internal.hpp"
 
 namespace rosetta {
+
+// Allow a kernel more than the default 64 KiB of dynamic LDS.
+template <typename K>
+inline hipError_t allow_lds(K kernel, size_t bytes) {
+  if (bytes <= 65536) return hipSuccess;
+  return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)bytes);
+}
 
 using bf16 = __bf16;
 using f16 = _Float16;

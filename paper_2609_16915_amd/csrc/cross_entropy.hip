@@ -14,7 +14,16 @@ namespace rosetta {
 
 namespace {
 
-constexpr int BX = 128, BY = 128, WX = 2, WY = 2;
+// Tiles of many rows, and of few rows or short ones.
+template <int BX_, int BY_, int WX_, int WY_>
+struct Shape {
+  static constexpr int BX = BX_, BY = BY_, WX = WX_, WY = WY_, THREADS = 64 * WX * WY;
+};
+using Large = Shape<256, 256, 4, 2>;
+using Small = Shape<128, 128, 2, 2>;
+template <class T, class S>
+using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY>;
+
 constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
 
 size_t up(size_t a, size_t b) { return (a + b - 1) / b * b; }
@@ -36,10 +45,11 @@ __device__ inline bool counts(int64_t target, int64_t ignore, size_t vocab) {
 }
 
 // part[tile of x][row], and the logit of each row's target
-template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(64 * WX *WY)
+template <class T, class S, bool ALIGNED>
+__global__ void __launch_bounds__(S::THREADS)
 k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) {
-  using Tl = Tile<T, BX, BY, WX, WY>;
+  using Tl = TileOf<T, S>;
+  constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.vocab + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
@@ -51,7 +61,7 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
   Tl::template run<ALIGNED>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes, lds, acc);
 
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
-  Stat *joint = (Stat *)lds;  // [WX][BY]
+  Stat *joint = (Stat *)lds;  // [S::WX][BY]
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int y = Tl::y_at() + 16 * j;
@@ -76,32 +86,72 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
 #pragma unroll
     for (int m = 16; m <= 32; m <<= 1)
       s = join(s, Stat{__shfl_xor(s.top, m), __shfl_xor(s.sum, m)});
-    if (threadIdx.x % 64 < 16) joint[(threadIdx.x / 64 % WX) * BY + y] = s;
+    if (threadIdx.x % 64 < 16) joint[(threadIdx.x / 64 % S::WX) * BY + y] = s;
   }
   __syncthreads();
   for (int y = threadIdx.x; y < BY; y += Tl::THREADS) {
     const int64_t row = (int64_t)ty * BY + y;
     if (row >= (int64_t)a.rows) break;
     Stat s = joint[y];
-    for (int w = 1; w < WX; ++w) s = join(s, joint[w * BY + y]);
+    for (int w = 1; w < S::WX; ++w) s = join(s, joint[w * BY + y]);
     part[(size_t)tx * a.rows + row] = s;
   }
 }
 
-// The tiles' parts of 16 rows joined, 16 threads to a row.
-__global__ void __launch_bounds__(256)
+// The same for at most 16 NY rows.
+template <class T, int NX, int NY>
+__global__ void __launch_bounds__(1024)
+k_loss_thin(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) {
+  using Th = Thin<T, NX, NY>;
+  extern __shared__ char lds[];
+  const int64_t bytes = (int64_t)a.dim * sizeof(T);
+  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab, bytes};
+  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows, bytes};
+  const size_t tx = xcd_block(blockIdx.x, gridDim.x);
+  const int64_t x0 = (int64_t)tx * 16 * NX;
+  v4f l = Th::run(X, Y, x0, lds);
+  const int t = threadIdx.x;
+  const int64_t x = x0 + 16 * (t / 64 % NX) + 4 * (t % 64 / 16), row = 16 * (t / 64 / NX) + t % 16;
+  Stat s{-INFINITY, 0.f};
+  if (t < Th::SUMS && row < (int64_t)a.rows) {
+    const int64_t target = a.targets[row];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (x + r >= (int64_t)a.vocab) l[r] = -INFINITY;
+      if (x + r == target) at_target[row] = l[r];
+      s.top = fmaxf(s.top, l[r]);
+    }
+    const float low = s.top == -INFINITY ? 0.f : s.top;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s.sum += __expf(l[r] - low);
+  }
+#pragma unroll
+  for (int m = 16; m <= 32; m <<= 1) s = join(s, Stat{__shfl_xor(s.top, m), __shfl_xor(s.sum, m)});
+  Stat *joint = (Stat *)lds;  // [NX][16 NY]
+  __syncthreads();            // (the waves' sums have been read)
+  if (t < Th::SUMS && t % 64 < 16) joint[t / 64 % NX * 16 * NY + row] = s;
+  __syncthreads();
+  if (t < 16 * NY && t < (int64_t)a.rows) {
+    s = joint[t];
+    for (int i = 1; i < NX; ++i) s = join(s, joint[i * 16 * NY + t]);
+    part[tx * a.rows + t] = s;
+  }
+}
+
+// The tiles' parts of 16 rows joined, 64 threads to a row.
+__global__ void __launch_bounds__(1024)
 k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
             const float *__restrict__ at_target) {
-  __shared__ Stat lds[16][16];
+  __shared__ Stat lds[64][16];
   const int r = threadIdx.x % 16, p = threadIdx.x / 16;
   const size_t row = (size_t)blockIdx.x * 16 + r;
   Stat s{-INFINITY, 0.f};
   if (row < a.rows)
-    for (size_t t = p; t < nt; t += 16) s = join(s, part[t * a.rows + row]);
+    for (size_t t = p; t < nt; t += 64) s = join(s, part[t * a.rows + row]);
   lds[p][r] = s;
   __syncthreads();
   if (p == 0 && row < a.rows) {
-    for (int q = 1; q < 16; ++q) s = join(s, lds[q][r]);
+    for (int q = 1; q < 64; ++q) s = join(s, lds[q][r]);
     const float lse = s.top + logf(s.sum);
     a.lse[row] = lse;
     const int64_t target = a.targets[row];
@@ -134,15 +184,17 @@ __global__ void __launch_bounds__(1024) k_loss_coef(LossArgs a, float *__restric
   if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
 }
 
-// gl of the vocabulary rows [v0, v0 + vp): as gl [rows][vp] and as gl_t
-// [vp][ld_t], zeros beyond the vocabulary and the rows.
-template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(64 * WX *WY)
-k_loss_grad_tile(LossArgs a, size_t v0, size_t vp, size_t ld_t, const float *__restrict__ coef,
+// gl of the vocabulary rows [v0, v0 + here), `here` rounded up to whole tiles: as
+// gl [rows][vp] and as gl_t [vp][ld_t], zeros beyond the vocabulary and the rows.
+template <class T, class S, bool ALIGNED>
+__global__ void __launch_bounds__(S::THREADS)
+k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
+                 const float *__restrict__ coef,
                  T *__restrict__ gl, T *__restrict__ gl_t) {
-  using Tl = Tile<T, BX, BY, WX, WY>;
+  using Tl = TileOf<T, S>;
+  constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
-  const unsigned gx = (unsigned)(vp / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
+  const unsigned gx = (unsigned)((here + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
   const int64_t bytes = (int64_t)a.dim * sizeof(T);
@@ -191,21 +243,23 @@ k_transpose(const T *__restrict__ in, size_t in_stride, size_t rows, size_t cols
     if (c0 + i < cols && r0 + l < ld) out[(c0 + i) * ld + r0 + l] = lds[l][i];
 }
 
-// part[split][row][d] (+)= gl [rows][vp] times w_t [dim][vp]: split s takes an
-// equal run of the piece's vocabulary.
-template <class T>
-__global__ void __launch_bounds__(64 * WX *WY)
-k_loss_gh_tile(size_t rows, size_t dim, size_t vp, const T *__restrict__ gl,
+// part[split][row][d] (+)= gl [rows][vp] times w_t [dim][vp] over the piece's
+// first `here`: split s takes an equal run of them, perhaps none of the last.
+template <class T, class S>
+__global__ void __launch_bounds__(S::THREADS)
+k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restrict__ gl,
                const T *__restrict__ w_t, float *__restrict__ part, size_t run, int add) {
-  using Tl = Tile<T, BX, BY, WX, WY>;
+  using Tl = TileOf<T, S>;
+  constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
   const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
   unsigned tx, ty;
   band_tile(b % (gx * gy), gx, gy, tx, ty);
-  const int64_t bytes = (int64_t)vp * sizeof(T);
-  const Operand X{(const char *)w_t, bytes, (int64_t)dim, bytes};
-  const Operand Y{(const char *)gl, bytes, (int64_t)rows, bytes};
+  // (whole 16 bytes: both have zeros there)
+  const int64_t ld = (int64_t)vp * sizeof(T), bytes = (int64_t)((here + 7) / 8 * 8) * sizeof(T);
+  const Operand X{(const char *)w_t, ld, (int64_t)dim, bytes};
+  const Operand Y{(const char *)gl, ld, (int64_t)rows, bytes};
   const int64_t k0 = (int64_t)(split * run * sizeof(T));
   int64_t k1 = k0 + (int64_t)(run * sizeof(T));
   k1 = k1 < bytes ? k1 : bytes;
@@ -242,19 +296,20 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
   }
 }
 
-// gw rows [v0, ..) = gl_t [vp][ld_t] times h_t [dim][ld_t]
-template <class T>
-__global__ void __launch_bounds__(64 * WX *WY)
-k_loss_gw_tile(LossArgs a, size_t v0, size_t vp, size_t ld_t, const float *__restrict__ coef,
+// gw rows [v0, v0 + here) = gl_t [here][ld_t] times h_t [dim][ld_t]
+template <class T, class S>
+__global__ void __launch_bounds__(S::THREADS)
+k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__restrict__ coef,
                const T *__restrict__ gl_t, const T *__restrict__ h_t) {
-  using Tl = Tile<T, BX, BY, WX, WY>;
+  using Tl = TileOf<T, S>;
+  constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
-  const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)(vp / BY);
+  const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)((here + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
   const int64_t bytes = (int64_t)ld_t * sizeof(T);
   const Operand X{(const char *)h_t, bytes, (int64_t)a.dim, bytes};
-  const Operand Y{(const char *)gl_t, bytes, (int64_t)vp, bytes};
+  const Operand Y{(const char *)gl_t, bytes, (int64_t)here, bytes};
   v4f acc[Tl::TX][Tl::TY] = {};
   Tl::template run<true>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes, lds, acc);
   const float back = coef[a.rows];
@@ -272,13 +327,24 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t vp, size_t ld_t, const float *__res
   }
 }
 
+// Rows of the vocabulary in a block of the forward pass; 0: Thin's, for as few
+// rows of h as it takes (bound by w's bytes either way; 33 rows: see thin_rows).
+constexpr size_t THIN_ROWS = 32;
+constexpr size_t thin_x(size_t rows) { return rows <= 16 ? 64 : 32; }
+bool large(size_t rows, size_t dim) { return rows > 128 && dim > 128; }
+size_t forward_x(size_t rows, size_t dim) {
+  return rows <= THIN_ROWS ? thin_x(rows) : large(rows, dim) ? Large::BX : Small::BX;
+}
+
 // Pieces of the vocabulary and what the workspace holds.
 struct Plan {
   size_t vp, pieces, ld_t, splits, run;
   size_t coef, gl, gl_t, w_t, h_t, part, bytes;
 };
 
+template <class S>
 Plan plan(size_t rows, size_t dim, size_t vocab) {
+  constexpr size_t BX = S::BX, BY = S::BY;
   constexpr size_t BUDGET = (size_t)512 << 20;
   Plan p{};
   p.ld_t = up(rows, 64);
@@ -290,7 +356,7 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   p.pieces = tiles(vocab, p.vp);
   // enough blocks for gh: its tiles are few, its sums long
   const size_t t = tiles(dim, BX) * tiles(rows, BY);
-  size_t s = 512 / t;
+  size_t s = (BX == 256 ? 256 : 512) / t;
   const size_t most = p.vp / 512;
   s = s > most ? most : s;
   p.splits = s < 1 ? 1 : s;
@@ -312,88 +378,97 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   return p;
 }
 
-template <class T>
-hipError_t forward(const LossArgs &a, hipStream_t st) {
-  const size_t gx = tiles(a.vocab, BX), gy = tiles(a.rows, BY);
-  Stat *part = (Stat *)a.workspace;
-  float *at_target = (float *)(part + gx * a.rows);
-  using Tl = Tile<T, BX, BY, WX, WY>;
+bool aligned(const LossArgs &a) {
   const Operand X{(const char *)a.w, (int64_t)(a.w_stride * 2), (int64_t)a.vocab,
                   (int64_t)(a.dim * 2)};
   const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * 2), (int64_t)a.rows,
                   (int64_t)(a.dim * 2)};
-  const bool al = rows_aligned(X) && rows_aligned(Y);
-  auto k = al ? k_loss_tile<T, true> : k_loss_tile<T, false>;
-  hipLaunchKernelGGL(k, dim3((unsigned)(gx * gy)), dim3(Tl::THREADS), Tl::LDS, st, a, part,
-                     at_target);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_loss_join, dim3((unsigned)tiles(a.rows, 16)), dim3(256), 0, st, a, part, gx,
-                     at_target);
-  return hipGetLastError();
+  return rows_aligned(X) && rows_aligned(Y);
 }
 
+// Launch of `kernel` with its LDS allowed, `e` the status so far.
+#define LAUNCH(KERNEL, BLOCKS, THREADS, LDS, ...)                                               \
+  do {                                                                                          \
+    if (e == hipSuccess) e = allow_lds(KERNEL, LDS);                                             \
+    if (e == hipSuccess) {                                                                      \
+      hipLaunchKernelGGL(KERNEL, BLOCKS, dim3(THREADS), LDS, st, __VA_ARGS__);                   \
+      e = hipGetLastError();                                                                    \
+    }                                                                                           \
+  } while (0)
+
 template <class T>
+hipError_t forward(const LossArgs &a, hipStream_t st) {
+  const size_t nx = tiles(a.vocab, forward_x(a.rows, a.dim));
+  Stat *part = (Stat *)a.workspace;
+  float *at_target = (float *)(part + nx * a.rows);
+  hipError_t e = hipSuccess;
+  auto tile = [&](auto shape) {
+    using S = decltype(shape);
+    auto k = aligned(a) ? k_loss_tile<T, S, true> : k_loss_tile<T, S, false>;
+    LAUNCH(k, dim3((unsigned)(nx * tiles(a.rows, S::BY))), S::THREADS, (TileOf<T, S>::LDS), a, part,
+           at_target);
+  };
+  if (a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1>::LDS), a, part, at_target);
+  else if (a.rows <= 32) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2>::LDS), a, part, at_target);
+  else if (large(a.rows, a.dim)) tile(Large{});
+  else tile(Small{});
+  LAUNCH(k_loss_join, dim3((unsigned)tiles(a.rows, 16)), 1024, 0, a, part, nx, at_target);
+  return e;
+}
+
+template <class T, class S>
 hipError_t backward(const LossArgs &a, hipStream_t st) {
-  const Plan p = plan(a.rows, a.dim, a.vocab);
-  using Tl = Tile<T, BX, BY, WX, WY>;
+  constexpr size_t BX = S::BX, BY = S::BY;
+  using Tl = TileOf<T, S>;
+  const Plan p = plan<S>(a.rows, a.dim, a.vocab);
   char *ws = (char *)a.workspace;
   float *coef = (float *)(ws + p.coef), *part = (float *)(ws + p.part);
   T *gl = a.gh ? (T *)(ws + p.gl) : nullptr, *gl_t = a.gw ? (T *)(ws + p.gl_t) : nullptr;
   T *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
-  const Operand X{(const char *)a.w, (int64_t)(a.w_stride * 2), (int64_t)a.vocab,
-                  (int64_t)(a.dim * 2)};
-  const Operand Y{(const char *)a.h, (int64_t)(a.h_stride * 2), (int64_t)a.rows,
-                  (int64_t)(a.dim * 2)};
-  const bool al = rows_aligned(X) && rows_aligned(Y);
-  hipLaunchKernelGGL(k_loss_coef, dim3(1), dim3(1024), 0, st, a, coef);
+  hipError_t e = hipSuccess;
+  LAUNCH(k_loss_coef, dim3(1), 1024, 0, a, coef);
   if (a.gw)
-    hipLaunchKernelGGL(k_transpose<T>,
-                       dim3((unsigned)tiles(p.ld_t, 64), (unsigned)tiles(a.dim, 64)), dim3(256), 0,
-                       st, (const T *)a.h, a.h_stride, a.rows, a.dim, h_t, p.ld_t);
-  hipError_t e = hipGetLastError();
+    LAUNCH(k_transpose<T>, dim3((unsigned)tiles(p.ld_t, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
+           (const T *)a.h, a.h_stride, a.rows, a.dim, h_t, p.ld_t);
   for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
-    auto k = al ? k_loss_grad_tile<T, true> : k_loss_grad_tile<T, false>;
-    hipLaunchKernelGGL(k, dim3((unsigned)(p.vp / BX * tiles(a.rows, BY))), dim3(Tl::THREADS),
-                       Tl::LDS, st, a, v0, p.vp, p.ld_t, coef, gl, gl_t);
+    auto k = aligned(a) ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
+    LAUNCH(k, dim3((unsigned)(tiles(here, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a, v0, here,
+           p.vp, p.ld_t, coef, gl, gl_t);
     if (a.gh) {
-      hipLaunchKernelGGL(k_transpose<T>,
-                         dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), dim3(256), 0,
-                         st, (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
-      hipLaunchKernelGGL(k_loss_gh_tile<T>,
-                         dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))),
-                         dim3(Tl::THREADS), Tl::LDS, st, a.rows, a.dim, p.vp, gl, w_t, part, p.run,
-                         i > 0);
+      LAUNCH(k_transpose<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
+             (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
+      LAUNCH((k_loss_gh_tile<T, S>),
+             dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS,
+             a.rows, a.dim, here, p.vp, gl, w_t, part, p.run, i > 0);
     }
     if (a.gw)
-      hipLaunchKernelGGL(k_loss_gw_tile<T>, dim3((unsigned)(tiles(a.dim, BX) * (p.vp / BY))),
-                         dim3(Tl::THREADS), Tl::LDS, st, a, v0, p.vp, p.ld_t, coef, gl_t, h_t);
-    e = hipGetLastError();
+      LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)(tiles(a.dim, BX) * tiles(here, BY))), S::THREADS,
+             Tl::LDS, a, v0, here, p.ld_t, coef, gl_t, h_t);
   }
-  if (e == hipSuccess && a.gh) {
-    hipLaunchKernelGGL(k_loss_gh_join<T>, dim3((unsigned)tiles(a.dim, 256), (unsigned)(a.rows < 32768 ? a.rows : 32768)),
-                       dim3(256), 0, st, part, (int)p.splits, a.rows, a.dim, coef, (T *)a.gh,
-                       a.gh_stride);
-    e = hipGetLastError();
-  }
+  if (a.gh)
+    LAUNCH(k_loss_gh_join<T>,
+           dim3((unsigned)tiles(a.dim, 256), (unsigned)(a.rows < 32768 ? a.rows : 32768)), 256, 0,
+           part, (int)p.splits, a.rows, a.dim, coef, (T *)a.gh, a.gh_stride);
   return e;
 }
 
 }  // namespace
 
 size_t cross_entropy_workspace(size_t rows, size_t dim, size_t vocab) {
-  return tiles(vocab, BX) * rows * sizeof(Stat) + rows * 4;
+  return tiles(vocab, forward_x(rows, dim)) * rows * sizeof(Stat) + rows * 4;
 }
 size_t cross_entropy_backward_workspace(size_t rows, size_t dim, size_t vocab) {
-  return plan(rows, dim, vocab).bytes;
+  return (large(rows, dim) ? plan<Large>(rows, dim, vocab) : plan<Small>(rows, dim, vocab)).bytes;
 }
 
 hipError_t launch_cross_entropy(const LossArgs &a, hipStream_t st) {
   return a.dtype == ROSETTA_BF16 ? forward<bf16>(a, st) : forward<f16>(a, st);
 }
 hipError_t launch_cross_entropy_backward(const LossArgs &a, hipStream_t st) {
-  return a.dtype == ROSETTA_BF16 ? backward<bf16>(a, st) : backward<f16>(a, st);
+  if (large(a.rows, a.dim))
+    return a.dtype == ROSETTA_BF16 ? backward<bf16, Large>(a, st) : backward<f16, Large>(a, st);
+  return a.dtype == ROSETTA_BF16 ? backward<bf16, Small>(a, st) : backward<f16, Small>(a, st);
 }
 
 }  // namespace rosetta

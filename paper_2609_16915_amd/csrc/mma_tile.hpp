@@ -63,9 +63,32 @@ struct Operand {
   int64_t bytes;
 };
 
-// Whether rows can be brought in by 16 bytes at a time straight to LDS.
+// Whether rows can be brought in by 16 bytes at a time straight to LDS (a
+// tile's rows within 32-bit offsets of its first).
 inline bool rows_aligned(const Operand &o) {
-  return (uintptr_t)o.p % FRAG == 0 && o.ld % FRAG == 0 && o.bytes % FRAG == 0;
+  return (uintptr_t)o.p % FRAG == 0 && o.ld % FRAG == 0 && o.bytes % FRAG == 0 &&
+         o.ld <= (int64_t)1 << 22 && o.bytes <= (int64_t)1 << 30;
+}
+
+// Memory at `base`, for buffer loads (raw, 32-bit offsets).
+__device__ inline v4i buffer_at(const char *base) {
+  const uint64_t b = (uint64_t)base;
+  return v4i{__builtin_amdgcn_readfirstlane((int)b),
+             __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), -1, 0x00027000};
+}
+
+// 16 bytes per lane from buf + at + k to LDS address `lds` + 16 lane.  Nothing
+// waits for it but barrier_loaded().
+__device__ inline void load_to_lds(v4i buf, int at, int k, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+                   __builtin_amdgcn_readfirstlane(lds)),
+               "v"(at), "s"(buf), "s"(k)
+               : "memory", "m0");
+}
+
+// This wave's LDS loads have landed and its LDS reads are done; then all of them.
+__device__ inline void barrier_loaded() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // Block b of `blocks`, numbered so that each of the eight XCDs (blocks are
@@ -112,10 +135,10 @@ template <class T, int BX, int BY, int WX, int WY>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
-  static constexpr int STAGE = (BX + BY) * STEP;
+  static constexpr int STAGE = (BX + BY) * STEP;  // a power of two
   static constexpr int LDS = 2 * STAGE;
   static constexpr int LOADS = (BX + BY) / 8 / WAVES;  // of 8 rows, per wave and stage
-  static_assert((BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
+  static_assert((STAGE & (STAGE - 1)) == 0 && (BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
   using Acc = typename Mma<T>::Acc;
 
   __device__ static int key_x(int row) {
@@ -125,59 +148,147 @@ struct Tile {
   __device__ static int key_y(int row) { return (row >> 1) & 7; }
 
   // acc += X rows [x0, x0 + BX) times Y rows [y0, y0 + BY) over bytes
-  // [k0, k1) of the rows (k0 a multiple of 16).
+  // [k0, k1) of the rows (k0 a multiple of 16; ALIGNED: k1 too).  x0 < X.rows and
+  // y0 < Y.rows: a tile has a row at least, or its loads would leave the matrix.
   template <bool ALIGNED>
   __device__ static void run(const Operand &X, const Operand &Y, int64_t x0, int64_t y0,
                              int64_t k0, int64_t k1, char *lds, Acc (&acc)[TX][TY]) {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    if (k0 >= k1) return;
+    const int lane = threadIdx.x % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wx = wave % WX, wy = wave / WX;
-    // this lane's source of each load: row 8 q + lane / 8, chunk (lane % 8) ^ key
-    const char *src[LOADS];
-    int chunk[LOADS];
+    constexpr int LX = BX / 8 / WAVES;  // loads of X, the rest are of Y
+    // this lane's source of load i: row 8 q + lane / 8 of X or Y, chunk (lane % 8)
+    // ^ key; rows past the last are the last again
+    int row[LOADS], chunk[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int row = (i * WAVES + wave) * 8 + lane / 8;
-      const bool isx = i < BX / 8 / WAVES;
-      const int r = isx ? row : row - BX;
-      const Operand &o = isx ? X : Y;
-      int64_t at = (isx ? x0 : y0) + r;
-      at = at < o.rows ? at : o.rows - 1;
-      chunk[i] = ((lane % 8) ^ (isx ? key_x(r) : key_y(r))) * FRAG;
-      src[i] = o.p + at * o.ld;
+      const int r = (i * WAVES + wave) * 8 + lane / 8 - (i < LX ? 0 : BX);
+      const int64_t left = (i < LX ? X.rows - x0 : Y.rows - y0) - 1;
+      row[i] = r < left ? r : (int)left;
+      chunk[i] = ((lane % 8) ^ (i < LX ? key_x(r) : key_y(r))) * FRAG;
     }
-    auto load = [&](int64_t k, char *stage) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const v4i v = load_frag(src[i], k + chunk[i], k1);
-        *(v4i *)(stage + (i * WAVES + wave) * 1024 + lane * FRAG) = v;
-      }
-    };
     // this lane's place in fragment 0 of its wave's X and Y
     const int m = lane % 16, g = lane / 16;
     const int key = (m >> 1) & 7;
     const int atx = (wx * (BX / WX) + (m / 4) * 4 * TX + m % 4) * STEP;
     const int aty = (BX + wy * (BY / WY) + m) * STEP;
-    auto compute = [&](const char *stage) {
+    // Half s of a stage to registers; of a step's last bytes only `left` count.
+    auto read = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], int left, auto tail) {
+      const int c = ((s * 4 + g) ^ key) * FRAG;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int c = ((s * 4 + g) ^ key) * FRAG;
-        v4i x[TX], y[TY];
+      for (int i = 0; i < TX; ++i) x[i] = *(const v4i *)(stage + atx + i * 4 * STEP + c);
 #pragma unroll
-        for (int i = 0; i < TX; ++i) x[i] = *(const v4i *)(stage + atx + i * 4 * STEP + c);
+      for (int j = 0; j < TY; ++j) y[j] = *(const v4i *)(stage + aty + j * 16 * STEP + c);
+      if (tail.value && (s * 4 + g) * FRAG >= left) {
 #pragma unroll
-        for (int j = 0; j < TY; ++j) y[j] = *(const v4i *)(stage + aty + j * 16 * STEP + c);
+        for (int i = 0; i < TX; ++i) x[i] = v4i{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < TY; ++j)
-#pragma unroll
-          for (int i = 0; i < TX; ++i) acc[i][j] = Mma<T>::mac(x[i], y[j], acc[i][j]);
+        for (int j = 0; j < TY; ++j) y[j] = v4i{0, 0, 0, 0};
       }
     };
-    int b = 0;
-    if (k0 < k1) load(k0, lds);
-    for (int64_t k = k0; k < k1; k += STEP, b ^= 1) {
-      __syncthreads();
-      if (k + STEP < k1) load(k + STEP, lds + (b ^ 1) * STAGE);
-      compute(lds + b * STAGE);
+    auto multiply = [&](const v4i(&x)[TX], const v4i(&y)[TY]) {
+#pragma unroll
+      for (int j = 0; j < TY; ++j)
+#pragma unroll
+        for (int i = 0; i < TX; ++i) acc[i][j] = Mma<T>::mac(x[i], y[j], acc[i][j]);
+    };
+    // Half s of a stage to (x, y) while (px, py) are multiplied, a few reads and
+    // loads at a time between products.
+    auto half = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], const v4i(&px)[TX],
+                    const v4i(&py)[TY], auto load) {
+      const int c = ((s * 4 + g) ^ key) * FRAG;
+      constexpr int READS = TX + TY;
+#pragma unroll
+      for (int j = 0; j < TY; ++j) {
+#pragma unroll
+        for (int i = j * LOADS / TY; i < (j + 1) * LOADS / TY; ++i) load(i);
+#pragma unroll
+        for (int i = j * READS / TY; i < (j + 1) * READS / TY; ++i) {
+          if (i < TX) x[i] = *(const v4i *)(stage + atx + i * 4 * STEP + c);
+          else y[i - TX] = *(const v4i *)(stage + aty + (i - TX) * 16 * STEP + c);
+        }
+#pragma unroll
+        for (int i = 0; i < TX; ++i) acc[i][j] = Mma<T>::mac(px[i], py[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    v4i x0f[TX], y0f[TY], x1f[TX], y1f[TY];
+    constexpr std::false_type whole{};
+    if constexpr (ALIGNED) {
+      const v4i bx = buffer_at(X.p + x0 * X.ld), by = buffer_at(Y.p + y0 * Y.ld);
+      int at[LOADS];
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) at[i] = row[i] * (int)(i < LX ? X.ld : Y.ld) + chunk[i];
+      const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+      auto load = [&](int k, int stage) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          load_to_lds(i < LX ? bx : by, at[i], k, base + stage + (i * WAVES + wave) * 1024);
+      };
+      // the last step may be part of one: chunks beyond it read its first again,
+      // and read() takes them as zeros
+      const int end = (int)k1, left = (int)((k1 - k0 - 1) % STEP) + 1;
+      auto load_last = [&](int k, int stage) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          load_to_lds(i < LX ? bx : by, at[i] - (chunk[i] < left ? 0 : chunk[i]), k,
+                      base + stage + (i * WAVES + wave) * 1024);
+      };
+      auto load_any = [&](int k, int stage) {
+        if (k + STEP <= end) load(k, stage);
+        else if (k < end) load_last(k, stage);
+      };
+      int k = (int)k0, b = 0;
+      load_any(k, 0);
+      barrier_loaded();
+      load_any(k + STEP, STAGE);
+      // Both halves of a step in registers, one ahead: the second half's reads go
+      // with the first's products, then, the next step's loads having landed, the
+      // next first half's with the second's.
+      if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
+      for (; k + 3 * STEP <= end; k += STEP, b ^= STAGE) {
+        half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
+        barrier_loaded();
+        half(lds + (b ^ STAGE), 0, x0f, y0f, x1f, y1f, [&](int i) {
+          load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP, base + b + (i * WAVES + wave) * 1024);
+        });
+      }
+      // at most two more whole steps and a part of one
+      for (; k + STEP <= end; k += STEP, b ^= STAGE) {
+        read(lds + b, 1, x1f, y1f, STEP, whole);
+        multiply(x0f, y0f);
+        barrier_loaded();
+        load_any(k + 2 * STEP, b);
+        if (k + 2 * STEP <= end) read(lds + (b ^ STAGE), 0, x0f, y0f, STEP, whole);
+        multiply(x1f, y1f);
+      }
+      if (k < end) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          read(lds + b, s, x0f, y0f, left, std::true_type{});
+          multiply(x0f, y0f);
+        }
+      }
+    } else {
+      auto load = [&](int64_t k, char *stage) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const char *src = i < LX ? X.p + (x0 + row[i]) * X.ld : Y.p + (y0 + row[i]) * Y.ld;
+          *(v4i *)(stage + (i * WAVES + wave) * 1024 + lane * FRAG) =
+              load_frag(src, k + chunk[i], k1);
+        }
+      };
+      int b = 0;
+      load(k0, lds);
+      for (int64_t k = k0; k < k1; k += STEP, b ^= STAGE) {
+        __syncthreads();
+        if (k + STEP < k1) load(k + STEP, lds + (b ^ STAGE));
+        read(lds + b, 0, x0f, y0f, STEP, whole);
+        multiply(x0f, y0f);
+        read(lds + b, 1, x0f, y0f, STEP, whole);
+        multiply(x0f, y0f);
+      }
     }
     __syncthreads();
   }
@@ -189,6 +300,98 @@ struct Tile {
   }
   __device__ static int y_at() {
     return (threadIdx.x / 64) / WX * (BY / WY) + threadIdx.x % 16;
+  }
+};
+
+// A few rows of Y (16 NY at most): a workgroup takes 16 NX rows of X, its 16 waves
+// the steps of the rows in turn, straight from memory to registers (the rows of
+// X are read once, those of Y come from the L2), two steps ahead of the products.
+// The waves' sums are then added up, in order, in LDS.
+template <class T, int NX, int NY>
+struct Thin {
+  static constexpr int WAVES = 16, THREADS = 64 * WAVES;
+  static constexpr int LDS = WAVES * NX * NY * 1024;
+  static constexpr int SUMS = NX * NY * 64;  // threads that hold sums in the end
+  static_assert(SUMS <= THREADS && LDS <= 64 * 1024, "");
+  using Acc = typename Mma<T>::Acc;
+
+  // The sums of thread t < SUMS: x = x0 + 16 (t / 64 % NX) + 4 (t % 64 / 16) + 0..3,
+  // y = 16 (t / 64 / NX) + t % 16.
+  __device__ static Acc run(const Operand &X, const Operand &Y, int64_t x0, char *lds) {
+    const int lane = threadIdx.x % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int m = lane % 16, g = lane / 16;
+    const char *xs[NX], *ys[NY];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int64_t r = x0 + 16 * i + m;
+      xs[i] = X.p + (r < X.rows ? r : X.rows - 1) * X.ld + g * FRAG;
+    }
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      const int64_t r = 16 * j + m;
+      ys[j] = Y.p + (r < Y.rows ? r : Y.rows - 1) * Y.ld + g * FRAG;
+    }
+    struct Step {
+      v4i x[NX][2], y[NY][2];
+    };
+    const int bytes = (int)X.bytes;
+    auto load = [&](Step &f, int k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < NX; ++i) __builtin_memcpy(&f.x[i][h], xs[i] + k + h * 64, FRAG);
+#pragma unroll
+        for (int j = 0; j < NY; ++j) __builtin_memcpy(&f.y[j][h], ys[j] + k + h * 64, FRAG);
+      }
+    };
+    Acc acc[NX][NY] = {};
+    auto multiply = [&](const Step &f) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+#pragma unroll
+          for (int j = 0; j < NY; ++j) acc[i][j] = Mma<T>::mac(f.x[i][h], f.y[j][h], acc[i][j]);
+    };
+    constexpr int TURN = WAVES * STEP;
+    const int whole = bytes / STEP * STEP;
+    Step a, b;
+    int k = wave * STEP;
+    if (k < whole) load(a, k);
+    if (k + TURN < whole) load(b, k + TURN);
+    for (; k + TURN < whole; k += 2 * TURN) {
+      multiply(a);
+      if (k + 2 * TURN < whole) load(a, k + 2 * TURN);
+      multiply(b);
+      if (k + 3 * TURN < whole) load(b, k + 3 * TURN);
+    }
+    if (k < whole) multiply(a);
+    // what is left of a step, by the wave whose turn it is
+    if (whole < bytes && whole / STEP % WAVES == wave) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+          a.x[i][h] = load_frag(xs[i] - g * FRAG, whole + h * 64 + g * FRAG, bytes);
+#pragma unroll
+        for (int j = 0; j < NY; ++j)
+          a.y[j][h] = load_frag(ys[j] - g * FRAG, whole + h * 64 + g * FRAG, bytes);
+      }
+      multiply(a);
+    }
+    Acc *sums = (Acc *)lds;
+#pragma unroll
+    for (int j = 0; j < NY; ++j)
+#pragma unroll
+      for (int i = 0; i < NX; ++i) sums[(wave * NX * NY + j * NX + i) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    Acc s = {};
+    if ((int)threadIdx.x < SUMS) {
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) s += sums[w * SUMS + threadIdx.x];
+    }
+    return s;
   }
 };
 

@@ -51,7 +51,7 @@ def placed(t, pad=0, offset=0):
 
 
 def within(got, want, bound):
-    d = (got.detach().cpu().to(D) - want).abs()
+    d = (got.detach().to(want.device, D) - want).abs()
     worst = float((d - bound).max()) if d.numel() else 0.0
     assert not torch.isnan(d).any() and worst <= 0, \
         f"off by {worst:.3g} more than the bound (largest difference {float(d.max()):.3g})"
@@ -289,26 +289,28 @@ def loss64(h, w, t, ignore):
     return logits, lse, loss, valid, at
 
 
-def check_loss(h, w, t, g, ignore, dtype, pad=0, offset=0):
+def check_loss(h, w, t, g, ignore, dtype, pad=0, offset=0, dev="cpu"):
+    """`dev`: where the 64-bit products are taken."""
     rows, dim = h.shape
-    vocab = w.shape[0]
-    logits, lse, loss, valid, at = loss64(h, w, t, ignore)
     hd, wd, td, gd = placed(h, pad, offset), placed(w, pad, offset), t.cuda(), g.cuda()
+    h, w, t, g = (x.to(dev) for x in (h, w, t, g))
+    logits, lse, loss, valid, at = loss64(h, w, t, ignore)
     got, got_lse = R.cross_entropy(hd, wd, td, ignore)
     # a logit's error, and with it a log-sum's; exp and log add units of E
     delta = 4 * E * math.sqrt(dim) * h.to(D).norm(dim=1) * w.to(D).norm(dim=1).max() \
         + 64 * E * (1 + lse.abs() + logits.abs().amax(1))
     within(got_lse, lse, delta)
-    assert torch.equal(torch.isnan(got).cpu(), torch.isnan(loss))
+    got = got.to(dev)
+    assert torch.equal(torch.isnan(got), torch.isnan(loss))
     fine = ~torch.isnan(loss)
-    within(got[fine.cuda()], loss[fine], 2 * delta[fine])
-    assert not got.cpu()[t == ignore].any()
+    within(got[fine], loss[fine], 2 * delta[fine])
+    assert not got[t == ignore].any()
 
     gh, gw = R.cross_entropy_backward(hd, wd, td, got_lse, gd, ignore)
     p = torch.exp(logits - lse[:, None])
     gl = p.clone()
-    gl[torch.arange(rows), at] -= 1
-    c = torch.where(valid, g.to(D), torch.zeros(rows, dtype=D))[:, None]
+    gl[torch.arange(rows, device=dev), at] -= 1
+    c = torch.where(valid, g.to(D), torch.zeros(rows, dtype=D, device=dev))[:, None]
     gl, p = gl * c, p * c.abs()
     u = U[dtype]
     # gl is rounded once; p is off by its logit's error; f16 holds it in steps of
@@ -352,6 +354,18 @@ def test_cross_entropy_large_logits_and_uneven_factors(dtype):
     g[5] = 0
     g[6] = -2
     check_loss(h, w, targets(63, rows, vocab, 7, 3), g, 3, dtype)
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF16, 64), (F16, 192)])
+def test_cross_entropy_gradients_in_pieces(dtype, dim):
+    """Enough rows that gl is held for a part of the vocabulary at a time, the last
+    part shorter than the others by more than a tile."""
+    rows, vocab = 16384, 8300
+    one = R.lib().rosetta_cross_entropy_backward_workspace_bytes(rows, dim, vocab)
+    assert one < 2 * 2 * rows * vocab  # (not all of gl, twice)
+    g = torch.full((rows,), 1.0 / rows)
+    check_loss(normal(64, rows, dim, dtype), normal(65, vocab, dim, dtype, 1.0 / math.sqrt(dim)),
+               targets(66, rows, vocab, 1000), g, -100, dtype, dev="cuda")
 
 
 def test_cross_entropy_targets_out_of_range():
