@@ -603,7 +603,7 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
  *  - Matrices are row-major device arrays with contiguous rows; a `_stride`
  *    is the distance of two rows in elements, at least the row's length.  No
  *    alignment beyond the element's own is needed; rows that start on 16
- *    bytes are read fastest.
+ *    bytes are read fastest.  Workspaces start on 16 bytes.
  *  - Types are rosetta_dtype.  Sums, norms, softmax statistics and scales are
  *    held in 32 bits; 8-bit products are summed exactly.
  *  - 8-bit rows: value = scale[row] * q, q in [-127, 127], scale = max |value|
@@ -661,11 +661,16 @@ rosetta_status rosetta_dequantize_rows(const int8_t *q, size_t q_stride, const f
  * for i < m tokens, j < n channels; a [m][k], b [n][k] (a row per channel),
  * bias [n] in 32 bits or NULL, out of type out_dtype.  The sum is exact (any
  * 8-bit values); k <= 131071 (else ROSETTA_ERR_UNSUPPORTED); k = 0 gives the
- * bias. */
+ * bias.  Where there are few outputs for the length of their sums, those are
+ * split over the chip and joined in `workspace`:
+ * rosetta_q8_matmul_workspace_bytes bytes (0 for most sizes); without one
+ * (NULL) they are not split, with the same results. */
 rosetta_status rosetta_q8_matmul(const int8_t *a, size_t a_stride, const float *a_scale,
                                  const int8_t *b, size_t b_stride, const float *b_scale,
                                  const float *bias, void *out, size_t out_stride, int out_dtype,
-                                 size_t m, size_t n, size_t k, void *stream);
+                                 size_t m, size_t n, size_t k, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+size_t rosetta_q8_matmul_workspace_bytes(size_t m, size_t n, size_t k);
 
 /* Softmax cross entropy over a vocabulary, straight from hidden states h
  * [rows][dim] and head weights w [vocab][dim] (both of type `dtype`,

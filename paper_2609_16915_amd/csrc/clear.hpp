@@ -72,7 +72,9 @@ struct Q8Args {
   size_t out_stride;
   int out_dtype;
   size_t m, n, k;
+  int *workspace;  // q8_matmul_workspace bytes, or null
 };
+size_t q8_matmul_workspace(size_t m, size_t n, size_t k);
 hipError_t launch_q8_matmul(const Q8Args &a, hipStream_t st);
 
 struct LossArgs {

@@ -250,10 +250,15 @@ rosetta_status rosetta_dequantize_rows(const int8_t *q, size_t q_stride, const f
                                      (hipStream_t)stream), "rosetta_dequantize_rows");
 }
 
+size_t rosetta_q8_matmul_workspace_bytes(size_t m, size_t n, size_t k) {
+  return m && n ? q8_matmul_workspace(m, n, k) : 0;
+}
+
 rosetta_status rosetta_q8_matmul(const int8_t *a, size_t a_stride, const float *a_scale,
                                  const int8_t *b, size_t b_stride, const float *b_scale,
                                  const float *bias, void *out, size_t out_stride, int out_dtype,
-                                 size_t m, size_t n, size_t k, void *stream) {
+                                 size_t m, size_t n, size_t k, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
   if (!is_type(out_dtype)) return fail(ROSETTA_ERR_PARAMS, "type %d", out_dtype);
   if (n < 1) return fail(ROSETTA_ERR_PARAMS, "rows of no elements");
   if (k > MAX_K)
@@ -274,9 +279,14 @@ rosetta_status rosetta_q8_matmul(const int8_t *a, size_t a_stride, const float *
   NEED(a_scale);
   NEED(b_scale);
   NEED(out);
-  TRY(check_arrays({aa, ab, as, bs, bi, ao}));
+  const size_t need = workspace ? rosetta_q8_matmul_workspace_bytes(m, n, k) : 0;
+  if (workspace && workspace_bytes < need)
+    return fail(ROSETTA_ERR_SIZE, "workspace holds %zu bytes, the call needs %zu", workspace_bytes,
+                need);
+  const Array ws{"workspace", need ? workspace : nullptr, 1, need / 16, need / 16, 16, true};
+  TRY(check_arrays({aa, ab, as, bs, bi, ao, ws}));
   const Q8Args q{a, b, a_stride, b_stride, a_scale, b_scale, bias, out, out_stride, out_dtype,
-                 m, n, k};
+                 m, n, k, need ? (int *)workspace : nullptr};
   return done(launch_q8_matmul(q, (hipStream_t)stream), "rosetta_q8_matmul");
 }
 
@@ -306,7 +316,7 @@ rosetta_status rosetta_cross_entropy(const void *h, size_t h_stride, const void 
   const Array ah{"h", h, rows, dim, h_stride, 2, false}, aw{"w", w, vocab, dim, w_stride, 2, false};
   const Array at{"targets", targets, 1, rows, rows, 8, false};
   const Array al{"loss", loss, 1, rows, rows, 4, true}, ae{"lse", lse, 1, rows, rows, 4, true};
-  const Array ws{"workspace", workspace, 1, need / 4, need / 4, 4, true};
+  const Array ws{"workspace", workspace, 1, need / 16, need / 16, 16, true};
   TRY(check_strides({ah, aw}));
   if (rows == 0) return done(hipSuccess, "");
   NEED(h);
@@ -354,7 +364,7 @@ rosetta_status rosetta_cross_entropy_backward(const void *h, size_t h_stride, co
   const Array ae{"lse", lse, 1, rows, rows, 4, false}, ag{"gloss", gloss, 1, rows, rows, 4, false};
   const Array agh{"gh", gh, rows, dim, gh_stride, 2, true};
   const Array agw{"gw", gw, vocab, dim, gw_stride, 2, true};
-  const Array ws{"workspace", workspace, 1, need / 4, need / 4, 4, true};
+  const Array ws{"workspace", workspace, 1, need / 16, need / 16, 16, true};
   TRY(check_strides({ah, aw, agh, agw}));
   if (rows == 0)
     return done(gw ? zero_rows(gw, dim * 2, gw_stride * 2, vocab, (hipStream_t)stream) : hipSuccess,

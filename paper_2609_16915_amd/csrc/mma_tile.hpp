@@ -135,10 +135,10 @@ template <class T, int BX, int BY, int WX, int WY>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
-  static constexpr int STAGE = (BX + BY) * STEP;  // a power of two
-  static constexpr int LDS = 2 * STAGE;
+  static constexpr int STAGE = (BX + BY) * STEP;
+  static constexpr int LDS = 2 * STAGE;  // what the stages take
   static constexpr int LOADS = (BX + BY) / 8 / WAVES;  // of 8 rows, per wave and stage
-  static_assert((STAGE & (STAGE - 1)) == 0 && (BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
+  static_assert((BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
   using Acc = typename Mma<T>::Acc;
 
   __device__ static int key_x(int row) {
@@ -147,32 +147,32 @@ struct Tile {
   }
   __device__ static int key_y(int row) { return (row >> 1) & 7; }
 
-  // acc += X rows [x0, x0 + BX) times Y rows [y0, y0 + BY) over bytes
-  // [k0, k1) of the rows (k0 a multiple of 16; ALIGNED: k1 too).  x0 < X.rows and
-  // y0 < Y.rows: a tile has a row at least, or its loads would leave the matrix.
-  template <bool ALIGNED>
-  __device__ static void run(const Operand &X, const Operand &Y, int64_t x0, int64_t y0,
-                             int64_t k0, int64_t k1, char *lds, Acc (&acc)[TX][TY]) {
-    if (k0 >= k1) return;
+  // A tile: rows [x0, x0 + BX) of X and [y0, y0 + BY) of Y over bytes [k0, k1)
+  // of the rows (k0 a multiple of 16; ALIGNED: k1 too).  x0 < X.rows and y0 <
+  // Y.rows: a tile has a row at least, or its loads would leave the matrix.
+  struct Place {
+    Operand X, Y;
+    int64_t x0, y0, k0, k1;
+  };
+
+  // The tiles first, first + stride, .. below count, one after the other:
+  // where(t) says where tile t is, done(t, acc) takes its sums.  The loads of a
+  // tile's first steps run while the sums of the one before are written; done()
+  // must leave the stages (the first LDS bytes) alone.
+  template <bool ALIGNED, class Where, class Done>
+  __device__ static void each(unsigned first, unsigned stride, unsigned count, char *lds,
+                              Where where, Done done) {
+    if (first >= count) return;
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wx = wave % WX, wy = wave / WX;
     constexpr int LX = BX / 8 / WAVES;  // loads of X, the rest are of Y
-    // this lane's source of load i: row 8 q + lane / 8 of X or Y, chunk (lane % 8)
-    // ^ key; rows past the last are the last again
-    int row[LOADS], chunk[LOADS];
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = (i * WAVES + wave) * 8 + lane / 8 - (i < LX ? 0 : BX);
-      const int64_t left = (i < LX ? X.rows - x0 : Y.rows - y0) - 1;
-      row[i] = r < left ? r : (int)left;
-      chunk[i] = ((lane % 8) ^ (i < LX ? key_x(r) : key_y(r))) * FRAG;
-    }
     // this lane's place in fragment 0 of its wave's X and Y
     const int m = lane % 16, g = lane / 16;
     const int key = (m >> 1) & 7;
     const int atx = (wx * (BX / WX) + (m / 4) * 4 * TX + m % 4) * STEP;
     const int aty = (BX + wy * (BY / WY) + m) * STEP;
+    Acc acc[TX][TY];
     // Half s of a stage to registers; of a step's last bytes only `left` count.
     auto read = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], int left, auto tail) {
       const int c = ((s * 4 + g) ^ key) * FRAG;
@@ -215,12 +215,23 @@ struct Tile {
     };
     v4i x0f[TX], y0f[TY], x1f[TX], y1f[TY];
     constexpr std::false_type whole{};
+    // Row of the tile and byte of the step of this lane's load i: row 8 q + lane / 8
+    // of X or Y, chunk (lane % 8) ^ key.
+    auto row_of = [&](int i) { return (i * WAVES + wave) * 8 + lane / 8 - (i < LX ? 0 : BX); };
+    auto chunk_of = [&](int i) {
+      const int r = row_of(i);
+      return ((lane % 8) ^ (i < LX ? key_x(r) : key_y(r))) * FRAG;
+    };
+    // rows past the last are the last again
+    auto row_in = [&](const Place &p, int i) {
+      const int64_t left = (i < LX ? p.X.rows - p.x0 : p.Y.rows - p.y0) - 1;
+      const int r = row_of(i);
+      return r < left ? r : (int)left;
+    };
     if constexpr (ALIGNED) {
-      const v4i bx = buffer_at(X.p + x0 * X.ld), by = buffer_at(Y.p + y0 * Y.ld);
-      int at[LOADS];
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) at[i] = row[i] * (int)(i < LX ? X.ld : Y.ld) + chunk[i];
       const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+      v4i bx, by;
+      int at[LOADS], k, end, left;
       auto load = [&](int k, int stage) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
@@ -228,69 +239,101 @@ struct Tile {
       };
       // the last step may be part of one: chunks beyond it read its first again,
       // and read() takes them as zeros
-      const int end = (int)k1, left = (int)((k1 - k0 - 1) % STEP) + 1;
-      auto load_last = [&](int k, int stage) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          load_to_lds(i < LX ? bx : by, at[i] - (chunk[i] < left ? 0 : chunk[i]), k,
-                      base + stage + (i * WAVES + wave) * 1024);
-      };
       auto load_any = [&](int k, int stage) {
         if (k + STEP <= end) load(k, stage);
-        else if (k < end) load_last(k, stage);
-      };
-      int k = (int)k0, b = 0;
-      load_any(k, 0);
-      barrier_loaded();
-      load_any(k + STEP, STAGE);
-      // Both halves of a step in registers, one ahead: the second half's reads go
-      // with the first's products, then, the next step's loads having landed, the
-      // next first half's with the second's.
-      if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
-      for (; k + 3 * STEP <= end; k += STEP, b ^= STAGE) {
-        half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
-        barrier_loaded();
-        half(lds + (b ^ STAGE), 0, x0f, y0f, x1f, y1f, [&](int i) {
-          load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP, base + b + (i * WAVES + wave) * 1024);
-        });
-      }
-      // at most two more whole steps and a part of one
-      for (; k + STEP <= end; k += STEP, b ^= STAGE) {
-        read(lds + b, 1, x1f, y1f, STEP, whole);
-        multiply(x0f, y0f);
-        barrier_loaded();
-        load_any(k + 2 * STEP, b);
-        if (k + 2 * STEP <= end) read(lds + (b ^ STAGE), 0, x0f, y0f, STEP, whole);
-        multiply(x1f, y1f);
-      }
-      if (k < end) {
+        else if (k < end) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          read(lds + b, s, x0f, y0f, left, std::true_type{});
-          multiply(x0f, y0f);
+          for (int i = 0; i < LOADS; ++i)
+            load_to_lds(i < LX ? bx : by, at[i] - (chunk_of(i) < left ? 0 : chunk_of(i)), k,
+                        base + stage + (i * WAVES + wave) * 1024);
         }
+      };
+      auto begin = [&](const Place &p) {
+        bx = buffer_at(p.X.p + p.x0 * p.X.ld);
+        by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          at[i] = row_in(p, i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
+        k = (int)p.k0;
+        end = (int)p.k1;
+        left = (end - k - 1) % STEP + 1;
+        load_any(k, 0);
+        load_any(k + STEP, STAGE);
+      };
+      begin(where(first));
+      for (unsigned t = first; t < count; t += stride) {
+#pragma unroll
+        for (int i = 0; i < TX; ++i)
+#pragma unroll
+          for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        int b = 0;
+        barrier_loaded();
+        // Both halves of a step in registers, one ahead: the second half's reads go
+        // with the first's products, then, the next step's loads having landed, the
+        // next first half's with the second's.
+        if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
+        for (; k + 3 * STEP <= end; k += STEP, b = STAGE - b) {
+          half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
+          barrier_loaded();
+          half(lds + (STAGE - b), 0, x0f, y0f, x1f, y1f, [&](int i) {
+            load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP,
+                        base + b + (i * WAVES + wave) * 1024);
+          });
+        }
+        // at most two more whole steps and a part of one
+        for (; k + STEP <= end; k += STEP, b = STAGE - b) {
+          read(lds + b, 1, x1f, y1f, STEP, whole);
+          multiply(x0f, y0f);
+          barrier_loaded();
+          load_any(k + 2 * STEP, b);
+          if (k + 2 * STEP <= end) read(lds + (STAGE - b), 0, x0f, y0f, STEP, whole);
+          multiply(x1f, y1f);
+        }
+        if (k < end) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            read(lds + b, s, x0f, y0f, left, std::true_type{});
+            multiply(x0f, y0f);
+          }
+        }
+        barrier_loaded();  // (nothing is read from the stages any more)
+        if (t + stride < count) begin(where(t + stride));
+        done(t, acc);
       }
     } else {
-      auto load = [&](int64_t k, char *stage) {
+      for (unsigned t = first; t < count; t += stride) {
+        const Place p = where(t);
+        v4i ahead[LOADS];
+        auto fetch = [&](int64_t k) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          const char *src = i < LX ? X.p + (x0 + row[i]) * X.ld : Y.p + (y0 + row[i]) * Y.ld;
-          *(v4i *)(stage + (i * WAVES + wave) * 1024 + lane * FRAG) =
-              load_frag(src, k + chunk[i], k1);
+          for (int i = 0; i < LOADS; ++i) {
+            const char *src = i < LX ? p.X.p + (p.x0 + row_in(p, i)) * p.X.ld
+                                     : p.Y.p + (p.y0 + row_in(p, i)) * p.Y.ld;
+            if (k + STEP <= p.k1) __builtin_memcpy(&ahead[i], src + k + chunk_of(i), FRAG);
+            else ahead[i] = load_frag(src, k + chunk_of(i), p.k1);
+          }
+        };
+#pragma unroll
+        for (int i = 0; i < TX; ++i)
+#pragma unroll
+          for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        int b = 0;
+        if (p.k0 < p.k1) fetch(p.k0);
+        for (int64_t k = p.k0; k < p.k1; k += STEP, b = STAGE - b) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i)
+            *(v4i *)(lds + b + (i * WAVES + wave) * 1024 + lane * FRAG) = ahead[i];
+          __syncthreads();
+          if (k + STEP < p.k1) fetch(k + STEP);
+          read(lds + b, 0, x0f, y0f, STEP, whole);
+          multiply(x0f, y0f);
+          read(lds + b, 1, x0f, y0f, STEP, whole);
+          multiply(x0f, y0f);
         }
-      };
-      int b = 0;
-      load(k0, lds);
-      for (int64_t k = k0; k < k1; k += STEP, b ^= STAGE) {
         __syncthreads();
-        if (k + STEP < k1) load(k + STEP, lds + (b ^ STAGE));
-        read(lds + b, 0, x0f, y0f, STEP, whole);
-        multiply(x0f, y0f);
-        read(lds + b, 1, x0f, y0f, STEP, whole);
-        multiply(x0f, y0f);
+        done(t, acc);
       }
     }
-    __syncthreads();
   }
 
   // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r and
@@ -303,21 +346,29 @@ struct Tile {
   }
 };
 
-// A few rows of Y (16 NY at most): a workgroup takes 16 NX rows of X, its 16 waves
+// A few rows of Y (16 NY at most): a workgroup takes 16 NX rows of X, its waves
 // the steps of the rows in turn, straight from memory to registers (the rows of
 // X are read once, those of Y come from the L2), two steps ahead of the products.
 // The waves' sums are then added up, in order, in LDS.
-template <class T, int NX, int NY>
+template <class T, int NX, int NY, int WAVES_>
 struct Thin {
-  static constexpr int WAVES = 16, THREADS = 64 * WAVES;
+  static constexpr int WAVES = WAVES_, THREADS = 64 * WAVES;
   static constexpr int LDS = WAVES * NX * NY * 1024;
-  static constexpr int SUMS = NX * NY * 64;  // threads that hold sums in the end
-  static_assert(SUMS <= THREADS && LDS <= 64 * 1024, "");
+  static constexpr int SUMS = NX * NY * 64;  // quadruples of sums
   using Acc = typename Mma<T>::Acc;
 
-  // The sums of thread t < SUMS: x = x0 + 16 (t / 64 % NX) + 4 (t % 64 / 16) + 0..3,
-  // y = 16 (t / 64 / NX) + t % 16.
-  __device__ static Acc run(const Operand &X, const Operand &Y, int64_t x0, char *lds) {
+  // Quadruple t of the sums, once run() is done: x = x0 + 16 (t / 64 % NX) + 4 (t %
+  // 64 / 16) + 0..3, y = 16 (t / 64 / NX) + t % 16.
+  __device__ static Acc sum(int t, const char *lds) {
+    Acc s = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) s += ((const Acc *)lds)[w * SUMS + t];
+    return s;
+  }
+
+  // Over bytes [k0, k1) of the rows, k0 a multiple of STEP.
+  __device__ static void run(const Operand &X, const Operand &Y, int64_t x0, int k0, int k1,
+                             char *lds) {
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int m = lane % 16, g = lane / 16;
@@ -335,7 +386,6 @@ struct Thin {
     struct Step {
       v4i x[NX][2], y[NY][2];
     };
-    const int bytes = (int)X.bytes;
     auto load = [&](Step &f, int k) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -345,7 +395,11 @@ struct Thin {
         for (int j = 0; j < NY; ++j) __builtin_memcpy(&f.y[j][h], ys[j] + k + h * 64, FRAG);
       }
     };
-    Acc acc[NX][NY] = {};
+    Acc acc[NX][NY];
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+#pragma unroll
+      for (int j = 0; j < NY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     auto multiply = [&](const Step &f) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -355,9 +409,9 @@ struct Thin {
           for (int j = 0; j < NY; ++j) acc[i][j] = Mma<T>::mac(f.x[i][h], f.y[j][h], acc[i][j]);
     };
     constexpr int TURN = WAVES * STEP;
-    const int whole = bytes / STEP * STEP;
+    const int whole = k0 + (k1 - k0) / STEP * STEP;
     Step a, b;
-    int k = wave * STEP;
+    int k = k0 + wave * STEP;
     if (k < whole) load(a, k);
     if (k + TURN < whole) load(b, k + TURN);
     for (; k + TURN < whole; k += 2 * TURN) {
@@ -368,15 +422,15 @@ struct Thin {
     }
     if (k < whole) multiply(a);
     // what is left of a step, by the wave whose turn it is
-    if (whole < bytes && whole / STEP % WAVES == wave) {
+    if (whole < k1 && (whole - k0) / STEP % WAVES == wave) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int i = 0; i < NX; ++i)
-          a.x[i][h] = load_frag(xs[i] - g * FRAG, whole + h * 64 + g * FRAG, bytes);
+          a.x[i][h] = load_frag(xs[i] - g * FRAG, whole + h * 64 + g * FRAG, k1);
 #pragma unroll
         for (int j = 0; j < NY; ++j)
-          a.y[j][h] = load_frag(ys[j] - g * FRAG, whole + h * 64 + g * FRAG, bytes);
+          a.y[j][h] = load_frag(ys[j] - g * FRAG, whole + h * 64 + g * FRAG, k1);
       }
       multiply(a);
     }
@@ -386,12 +440,6 @@ struct Thin {
 #pragma unroll
       for (int i = 0; i < NX; ++i) sums[(wave * NX * NY + j * NX + i) * 64 + lane] = acc[i][j];
     __syncthreads();
-    Acc s = {};
-    if ((int)threadIdx.x < SUMS) {
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += sums[w * SUMS + threadIdx.x];
-    }
-    return s;
   }
 };
 

@@ -1,61 +1,20 @@
 // 8-bit matrix product with a scale per token and per channel.
 //
-// X are the channels (b, contiguous in the output's rows), Y the tokens (a).
+// X are the channels (b, contiguous in the output's rows), Y the tokens (a).  The
+// sums are exact in 32-bit integers, so they may be split at will: where there
+// are few outputs for the length of their sums, blocks take parts of the sums,
+// which k_q8_join adds up.
+#include <algorithm>
+
 #include "mma_tile.hpp"
 
 namespace rosetta {
 
 namespace {
 
-template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
-__global__ void __launch_bounds__(64 * WX *WY) k_q8_tile(Q8Args a) {
-  using Tl = Tile<int8_t, BX, BY, WX, WY>;
-  extern __shared__ char lds[];
-  const unsigned gx = (unsigned)((a.n + BX - 1) / BX), gy = (unsigned)((a.m + BY - 1) / BY);
-  unsigned tx, ty;
-  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
-  const Operand X{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k};
-  const Operand Y{(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k};
-  v4i acc[Tl::TX][Tl::TY] = {};
-  Tl::template run<ALIGNED>(X, Y, (int64_t)tx * BX, (int64_t)ty * BY, 0, (int64_t)a.k, lds, acc);
-
-  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
-  float bs[Tl::TX][4], bias[Tl::TX][4];
-#pragma unroll
-  for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t x = x0 + 4 * i + r;
-      bs[i][r] = x < (int64_t)a.n ? a.b_scale[x] : 0.f;
-      bias[i][r] = a.bias && x < (int64_t)a.n ? a.bias[x] : 0.f;
-    }
-#pragma unroll
-  for (int j = 0; j < Tl::TY; ++j) {
-    const int64_t y = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-    if (y >= (int64_t)a.m) continue;
-    const float as = a.a_scale[y];
-    O *out = (O *)a.out + y * (int64_t)a.out_stride;
-    float f[4 * Tl::TX];
-#pragma unroll
-    for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        f[4 * i + r] = (float)acc[i][j][r] * as * bs[i][r] + bias[i][r];
-    if (x0 < (int64_t)a.n) store_run(out + x0, (int64_t)a.n - x0, f);
-  }
-}
-
-template <class O, int NX, int NY>
-__global__ void __launch_bounds__(1024) k_q8_thin(Q8Args a) {
-  using Th = Thin<int8_t, NX, NY>;
-  extern __shared__ char lds[];
-  const Operand X{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k};
-  const Operand Y{(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k};
-  const int64_t x0 = (int64_t)xcd_block(blockIdx.x, gridDim.x) * 16 * NX;
-  const v4i s = Th::run(X, Y, x0, lds);
-  const int t = threadIdx.x;
-  const int64_t x = x0 + 16 * (t / 64 % NX) + 4 * (t % 64 / 16), y = 16 * (t / 64 / NX) + t % 16;
-  if (t >= Th::SUMS || y >= (int64_t)a.m || x >= (int64_t)a.n) return;
+// Four neighbouring outputs from their sums.
+template <class O>
+__device__ inline void put4(const Q8Args &a, int64_t y, int64_t x, v4i s) {
   const float as = a.a_scale[y];
   float f[4];
 #pragma unroll
@@ -66,55 +25,217 @@ __global__ void __launch_bounds__(1024) k_q8_thin(Q8Args a) {
   store_run((O *)a.out + y * (int64_t)a.out_stride + x, (int64_t)a.n - x, f);
 }
 
+// Part `split` of the sums, rows of n rounded up to 4.
+__device__ inline int *part_at(const Q8Args &a, int64_t ld, unsigned split, int64_t y, int64_t x) {
+  return a.workspace + ((int64_t)split * (int64_t)a.m + y) * ld + x;
+}
+
+// `run`: bytes of the rows per split, all of them in one.
 template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
-hipError_t tile(const Q8Args &a, hipStream_t st) {
+__global__ void __launch_bounds__(64 * WX *WY) k_q8_tile(Q8Args a, int splits, int run) {
+  using Tl = Tile<int8_t, BX, BY, WX, WY>;
+  extern __shared__ char lds[];
+  const unsigned gx = (unsigned)((a.n + BX - 1) / BX), gy = (unsigned)((a.m + BY - 1) / BY);
+  const unsigned count = gx * gy * splits;
+  auto where = [&](unsigned t) {
+    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
+    unsigned tx, ty;
+    band_tile(b % (gx * gy), gx, gy, tx, ty);
+    const int64_t k0 = (int64_t)split * run, k1 = k0 + run < (int64_t)a.k ? k0 + run : (int64_t)a.k;
+    return typename Tl::Place{{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k},
+                              {(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k},
+                              (int64_t)tx * BX, (int64_t)ty * BY, k0, k1};
+  };
+  auto done = [&](unsigned t, v4i(&acc)[Tl::TX][Tl::TY]) {
+    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
+    unsigned tx, ty;
+    band_tile(b % (gx * gy), gx, gy, tx, ty);
+    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+    if (splits > 1) {
+      const int64_t ld = ((int64_t)a.n + 3) / 4 * 4;
+#pragma unroll
+      for (int j = 0; j < Tl::TY; ++j) {
+        const int64_t y = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+        if (y >= (int64_t)a.m) continue;
+#pragma unroll
+        for (int i = 0; i < Tl::TX; ++i)
+          if (x0 + 4 * i < ld) *(v4i *)part_at(a, ld, split, y, x0 + 4 * i) = acc[i][j];
+      }
+      return;
+    }
+    float bs[Tl::TX][4], bias[Tl::TX][4];
+#pragma unroll
+    for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t x = x0 + 4 * i + r;
+        bs[i][r] = x < (int64_t)a.n ? a.b_scale[x] : 0.f;
+        bias[i][r] = a.bias && x < (int64_t)a.n ? a.bias[x] : 0.f;
+      }
+#pragma unroll
+    for (int j = 0; j < Tl::TY; ++j) {
+      const int64_t y = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+      if (y >= (int64_t)a.m) continue;
+      const float as = a.a_scale[y];
+      O *out = (O *)a.out + y * (int64_t)a.out_stride;
+      float f[4 * Tl::TX];
+#pragma unroll
+      for (int i = 0; i < Tl::TX; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          f[4 * i + r] = (float)acc[i][j][r] * as * bs[i][r] + bias[i][r];
+      if (x0 < (int64_t)a.n) store_run(out + x0, (int64_t)a.n - x0, f);
+    }
+  };
+  Tl::template each<ALIGNED>(blockIdx.x, gridDim.x, count, lds, where, done);
+}
+
+template <class O, int NX, int NY, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_q8_thin(Q8Args a, int splits, int run) {
+  using Th = Thin<int8_t, NX, NY, WAVES>;
+  extern __shared__ char lds[];
+  const Operand X{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k};
+  const Operand Y{(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k};
+  const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b % splits;
+  const int64_t x0 = (int64_t)(b / splits) * 16 * NX, ld = ((int64_t)a.n + 3) / 4 * 4;
+  const int k0 = (int)split * run, k1 = k0 + run < (int)a.k ? k0 + run : (int)a.k;
+  Th::run(X, Y, x0, k0, k1, lds);
+  for (int t = threadIdx.x; t < Th::SUMS; t += Th::THREADS) {
+    const int64_t x = x0 + 16 * (t / 64 % NX) + 4 * (t % 64 / 16), y = 16 * (t / 64 / NX) + t % 16;
+    if (y >= (int64_t)a.m || x >= (int64_t)a.n) continue;
+    const v4i s = Th::sum(t, lds);
+    if (splits > 1) *(v4i *)part_at(a, ld, split, y, x) = s;
+    else put4<O>(a, y, x, s);
+  }
+}
+
+template <class O>
+__global__ void __launch_bounds__(256) k_q8_join(Q8Args a, int splits) {
+  const int64_t ld = ((int64_t)a.n + 3) / 4 * 4, of = ld / 4 * (int64_t)a.m;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= of) return;
+  const int64_t y = i / (ld / 4), x = i % (ld / 4) * 4;
+  v4i s = *(const v4i *)part_at(a, ld, 0, y, x);
+  for (int q = 1; q < splits; ++q) s += *(const v4i *)part_at(a, ld, q, y, x);
+  put4<O>(a, y, x, s);
+}
+
+// How a product is cut up.
+enum class Cut { THIN, SMALL, LARGE };
+struct Plan {
+  Cut cut;
+  int nx, ny;  // THIN
+  int splits, run;
+};
+
+size_t tiles(size_t a, size_t b) { return (a + b - 1) / b; }
+
+Plan plan(size_t m, size_t n, size_t k) {
+  const size_t cus = std::max(1, device_cus());
+  Plan p{Cut::THIN, 1, 1, 1, 0};
+  size_t most = 1;
+  if (m <= 16) {
+    // Few tokens: bound by the channels' bytes, so every CU needs channels to
+    // read, and the more a block has the less often the tokens are read.
+    p.nx = tiles(n, 64) >= cus ? 4 : tiles(n, 32) >= cus ? 2 : 1;
+  } else if (m <= 32) {
+    p.ny = 2;
+    p.nx = tiles(n, 32) >= cus ? 2 : 1;
+  } else if (m <= 64) {
+    p.ny = m <= 48 ? 3 : 4;
+    p.nx = 4;
+    most = tiles(2 * cus, tiles(n, 64));
+  } else {
+    // Large tiles do a product at half the cost of small ones but come one to a
+    // CU, small ones two: the smaller of the two times, in steps of a large one.
+    const size_t steps = tiles(k, STEP);
+    const size_t nl = tiles(n, 256) * tiles(m, 256), ns = tiles(n, 128) * tiles(m, 128);
+    const double large = (double)tiles(nl, cus) * (steps + 3);
+    const double small = (ns <= cus ? 0.42 : 0.63 * ((double)ns / (2 * cus) + 0.5)) * (steps + 3);
+    p.cut = large <= small ? Cut::LARGE : Cut::SMALL;
+    if (p.cut == Cut::SMALL && ns <= cus) most = 2 * cus / ns;
+  }
+  // a part of a sum is 8 steps at least, or the joining costs more than it gives
+  const size_t parts = std::max((size_t)1, std::min(most, k / (8 * STEP)));
+  p.run = (int)(tiles(tiles(k, parts), STEP) * STEP);
+  p.splits = k ? (int)tiles(k, (size_t)p.run) : 1;
+  return p;
+}
+
+template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
+hipError_t tile(const Q8Args &a, const Plan &p, bool one_each, hipStream_t st) {
   using Tl = Tile<int8_t, BX, BY, WX, WY>;
   auto k = k_q8_tile<O, ALIGNED, BX, BY, WX, WY>;
   const hipError_t e = allow_lds(k, Tl::LDS);
   if (e != hipSuccess) return e;
-  const size_t blocks = (a.n + BX - 1) / BX * ((a.m + BY - 1) / BY);
-  hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(Tl::THREADS), Tl::LDS, st, a);
+  const size_t count = tiles(a.n, BX) * tiles(a.m, BY) * p.splits, cus = (size_t)device_cus();
+  hipLaunchKernelGGL(k, dim3((unsigned)(one_each || !cus ? count : std::min(count, cus))),
+                     dim3(Tl::THREADS), Tl::LDS, st, a, p.splits, p.run);
   return hipGetLastError();
 }
 
-template <class O, int NX, int NY>
-hipError_t thin(const Q8Args &a, hipStream_t st) {
-  using Th = Thin<int8_t, NX, NY>;
-  hipLaunchKernelGGL((k_q8_thin<O, NX, NY>), dim3((unsigned)((a.n + 16 * NX - 1) / (16 * NX))),
-                     dim3(Th::THREADS), Th::LDS, st, a);
+template <class O, int NX, int NY, int WAVES>
+hipError_t thin(const Q8Args &a, const Plan &p, hipStream_t st) {
+  using Th = Thin<int8_t, NX, NY, WAVES>;
+  auto k = k_q8_thin<O, NX, NY, WAVES>;
+  const hipError_t e = allow_lds(k, Th::LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k, dim3((unsigned)(tiles(a.n, 16 * NX) * p.splits)), dim3(Th::THREADS),
+                     Th::LDS, st, a, p.splits, p.run);
   return hipGetLastError();
-}
-
-template <class O, bool ALIGNED>
-hipError_t by_size(const Q8Args &a, hipStream_t st) {
-  const size_t cus = (size_t)device_cus();
-  auto blocks = [&](size_t x, size_t y) { return (a.n + x - 1) / x * ((a.m + y - 1) / y); };
-  // Few tokens: bound by the channels' bytes, so every CU needs channels to read,
-  // and the more each block has the less often the tokens are read.
-  if (a.m <= 16)
-    return blocks(64, 16) >= cus   ? thin<O, 4, 1>(a, st)
-           : blocks(32, 16) >= cus ? thin<O, 2, 1>(a, st)
-                                   : thin<O, 1, 1>(a, st);
-  if (a.m <= 32) return blocks(32, 32) >= cus ? thin<O, 2, 2>(a, st) : thin<O, 1, 2>(a, st);
-  if (a.m <= 64) return thin<O, 1, 4>(a, st);
-  if (blocks(256, 256) >= cus) return tile<O, ALIGNED, 256, 256, 4, 2>(a, st);
-  return tile<O, ALIGNED, 128, 128, 2, 2>(a, st);
 }
 
 template <class O>
-hipError_t by_alignment(const Q8Args &a, hipStream_t st) {
+hipError_t launch(const Q8Args &a, hipStream_t st) {
+  Plan p = plan(a.m, a.n, a.k);
+  if (!a.workspace) {
+    p.splits = 1;
+    p.run = (int)a.k;
+  }
   const Operand X{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k};
   const Operand Y{(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k};
-  return rows_aligned(X) && rows_aligned(Y) ? by_size<O, true>(a, st) : by_size<O, false>(a, st);
+  const bool al = rows_aligned(X) && rows_aligned(Y);
+  hipError_t e = hipSuccess;
+  switch (p.cut) {
+    case Cut::THIN:
+      switch (p.ny * 8 + p.nx) {
+        case 9: e = thin<O, 1, 1, 16>(a, p, st); break;
+        case 10: e = thin<O, 2, 1, 16>(a, p, st); break;
+        case 12: e = thin<O, 4, 1, 16>(a, p, st); break;
+        case 17: e = thin<O, 1, 2, 16>(a, p, st); break;
+        case 18: e = thin<O, 2, 2, 16>(a, p, st); break;
+        case 28: e = thin<O, 4, 3, 8>(a, p, st); break;
+        default: e = thin<O, 4, 4, 8>(a, p, st); break;
+      }
+      break;
+    case Cut::SMALL:
+      e = al ? tile<O, true, 128, 128, 4, 2>(a, p, true, st)
+             : tile<O, false, 128, 128, 4, 2>(a, p, true, st);
+      break;
+    case Cut::LARGE:
+      e = al ? tile<O, true, 256, 256, 4, 2>(a, p, false, st)
+             : tile<O, false, 256, 256, 4, 2>(a, p, false, st);
+      break;
+  }
+  if (e != hipSuccess || p.splits == 1) return e;
+  const size_t quads = tiles(a.n, 4) * a.m;
+  hipLaunchKernelGGL(k_q8_join<O>, dim3((unsigned)tiles(quads, 256)), dim3(256), 0, st, a,
+                     p.splits);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+size_t q8_matmul_workspace(size_t m, size_t n, size_t k) {
+  const Plan p = plan(m, n, k);
+  return p.splits == 1 ? 0 : (size_t)p.splits * m * tiles(n, 4) * 4 * sizeof(int);
+}
+
 hipError_t launch_q8_matmul(const Q8Args &a, hipStream_t st) {
   switch (a.out_dtype) {
-    case ROSETTA_F32: return by_alignment<float>(a, st);
-    case ROSETTA_BF16: return by_alignment<bf16>(a, st);
-    default: return by_alignment<f16>(a, st);
+    case ROSETTA_F32: return launch<float>(a, st);
+    case ROSETTA_BF16: return launch<bf16>(a, st);
+    default: return launch<f16>(a, st);
   }
 }
 

@@ -158,7 +158,8 @@ SIGNATURES.update({
     "rosetta_dequantize_rows": (_ST, [_u64p, _sz, _u64p, _i32, _sz, _sz, _u64p, _sz,
                                       C.c_void_p]),
     "rosetta_q8_matmul": (_ST, [_u64p, _sz, _u64p, _u64p, _sz, _u64p, _u64p, _u64p, _sz, _i32,
-                                _sz, _sz, _sz, C.c_void_p]),
+                                _sz, _sz, _sz, _u64p, _sz, C.c_void_p]),
+    "rosetta_q8_matmul_workspace_bytes": (_sz, [_sz, _sz, _sz]),
     "rosetta_cross_entropy": (_ST, [_u64p, _sz, _u64p, _sz, _i32, _u64p, _i64, _sz, _sz, _sz,
                                     _u64p, _u64p, _u64p, _sz, C.c_void_p]),
     "rosetta_cross_entropy_workspace_bytes": (_sz, [_sz, _sz, _sz]),
@@ -623,6 +624,7 @@ def sample_extract(glwe_in, N: int, out=None, stream=None):
 # the clear side: 8-bit layers and the vocabulary loss (device)
 # --------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=None)
 def _types():
     torch = _torch()
     return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -669,11 +671,29 @@ def _vec(t, name: str, dtype, count: int) -> int:
 
 
 def _made(out, name: str, shape, dtype, like):
-    """`out` checked, or a new tensor of that shape and type."""
+    """`out` checked, or a new tensor of that shape and type: (tensor, address,
+    row stride)."""
     if out is None:
-        return _torch().empty(shape, dtype=dtype, device=like.device)
-    _mat(out, name, dtype, shape)
-    return out
+        out = _torch().empty(shape, dtype=dtype, device=like.device)
+        return out, out.data_ptr(), shape[1]
+    return out, *_mat(out, name, dtype, shape)[:2]
+
+
+def _weight(weight, dtype, code: int, dim: int):
+    """(address, type) of a norm's weight, of x's type or float32; None is ones."""
+    if weight is None:
+        return None, code
+    if weight.dtype != dtype and weight.dtype != _torch().float32:
+        raise TypeError(f"weight must be {dtype} or float32, not {weight.dtype}")
+    return _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
+
+
+def _stream_of(t, stream) -> int:
+    """The stream given, or the current one of the tensor's device (read as a plain
+    number: a Stream object takes 2.6 us to make, as long as the launch)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _torch()._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _scratch(workspace, need: int, like):
@@ -710,25 +730,26 @@ class NormQ8(NamedTuple):
     y: object
 
 
-def _norm(x, weight, eps, residual, h, y, q, scale, inv_rms, stream):
+def _norm(x, weight, eps, residual, h, y, want_y, q, want_q, stream):
     torch = _torch()
     xp, xs, rows, dim = _mat(x, "x")
-    dt = _type(x.dtype, "x")
-    rp = rs = 0
-    if residual is not None:
-        rp, rs, _, _ = _mat(residual, "residual", x.dtype, (rows, dim))
-    wp, wt = None, dt
-    if weight is not None:
-        if weight.dtype not in (x.dtype, torch.float32):
-            raise TypeError(f"weight must be {x.dtype} or float32, not {weight.dtype}")
-        wp, wt = _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
-    hp, hs = _mat(h, "h", x.dtype, (rows, dim))[:2] if h is not None else (None, dim)
-    yp, ys = _mat(y, "y", x.dtype, (rows, dim))[:2] if y is not None else (None, dim)
-    qp, qs = _mat(q, "q", torch.int8, (rows, dim))[:2] if q is not None else (None, dim)
-    sp = _vec(scale, "scale", torch.float32, rows) if scale is not None else None
-    ip = _vec(inv_rms, "inv_rms", torch.float32, rows) if inv_rms is not None else None
-    _check(lib().rosetta_rms_norm(xp, xs, rp or None, rs or dim, wp, wt, dt, rows, dim, eps, hp,
-                                  hs, yp, ys, qp, qs, sp, ip, _stream(stream)))
+    dtype = x.dtype
+    code = _type(dtype, "x")
+    rp, rs = (None, dim) if residual is None else _mat(residual, "residual", dtype, (rows, dim))[:2]
+    wp, wt = _weight(weight, dtype, code, dim)
+    hp, hs, yp, ys, qp, qs, scale, sp = None, dim, None, dim, None, dim, None, None
+    if h is not None or residual is not None:
+        h, hp, hs = _made(h, "h", (rows, dim), dtype, x)
+    if want_y:
+        y, yp, ys = _made(y, "y", (rows, dim), dtype, x)
+    if want_q:
+        q, qp, qs = _made(q, "q", (rows, dim), torch.int8, x)
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        sp = scale.data_ptr()
+    inv_rms = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(lib().rosetta_rms_norm(xp, xs, rp, rs, wp, wt, code, rows, dim, eps, hp, hs, yp, ys, qp,
+                                  qs, sp, inv_rms.data_ptr(), _stream_of(x, stream)))
+    return q, scale, h, inv_rms, y
 
 
 @_on_its_stream
@@ -737,28 +758,13 @@ def rms_norm_q8(x, weight, eps: float, residual=None, h=None, want_y: bool = Fal
     """RMS norm of x + residual ([rows][dim], float32, bfloat16 or float16) to
     8 bits with a scale per row.  weight [dim] (None: ones) has x's type or
     float32.  h may be x or residual, which it then replaces."""
-    torch = _torch()
-    _, _, rows, dim = _mat(x, "x")
-    if h is None and residual is not None:
-        h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-    q = _made(q, "q", (rows, dim), torch.int8, x)
-    ends = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    scale, inv_rms = ends.unbind(0)
-    y = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if want_y else None
-    _norm(x, weight, eps, residual, h, y, q, scale, inv_rms, stream)
-    return NormQ8(q, scale, h, inv_rms, y)
+    return NormQ8(*_norm(x, weight, eps, residual, h, None, want_y, q, True, stream))
 
 
 @_on_its_stream
 def rms_norm(x, weight, eps: float, residual=None, h=None, y=None, stream=None):
     """The same without the 8 bits: (y, h, inv_rms)."""
-    torch = _torch()
-    _, _, rows, dim = _mat(x, "x")
-    if h is None and residual is not None:
-        h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-    y = _made(y, "y", (rows, dim), x.dtype, x)
-    inv_rms = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _norm(x, weight, eps, residual, h, y, None, None, inv_rms, stream)
+    _, _, h, inv_rms, y = _norm(x, weight, eps, residual, h, y, True, None, False, stream)
     return y, h, inv_rms
 
 
@@ -770,25 +776,21 @@ def rms_norm_backward(gy, h, weight, inv_rms, gh=None, gx=None, want_gweight: bo
     x where there was no residual.  gx may be gy or gh; gweight is float32."""
     torch = _torch()
     yp, ys, rows, dim = _mat(gy, "gy")
-    dt = _type(gy.dtype, "gy")
-    hp, hs = _mat(h, "h", gy.dtype, (rows, dim))[:2]
-    gp, gs = _mat(gh, "gh", gy.dtype, (rows, dim))[:2] if gh is not None else (None, dim)
-    wp, wt = None, dt
-    if weight is not None:
-        if weight.dtype not in (gy.dtype, torch.float32):
-            raise TypeError(f"weight must be {gy.dtype} or float32, not {weight.dtype}")
-        wp, wt = _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
+    dtype = gy.dtype
+    code = _type(dtype, "gy")
+    hp, hs = _mat(h, "h", dtype, (rows, dim))[:2]
+    gp, gs = (None, dim) if gh is None else _mat(gh, "gh", dtype, (rows, dim))[:2]
+    wp, wt = _weight(weight, dtype, code, dim)
     ip = _vec(inv_rms, "inv_rms", torch.float32, rows)
-    gx = _made(gx, "gx", (rows, dim), gy.dtype, gy)
-    gweight, wsp, wsb = None, None, 0
+    gx, xp, xs = _made(gx, "gx", (rows, dim), dtype, gy)
+    gweight, gwp, wsp, wsb = None, None, None, 0
     if want_gweight:
         gweight = torch.empty(dim, dtype=torch.float32, device=gy.device)
+        gwp = gweight.data_ptr()
         wsp, wsb, workspace = _scratch(
             workspace, lib().rosetta_rms_norm_backward_workspace_bytes(rows, dim), gy)
-    xp, xs = _mat(gx, "gx")[:2]
-    _check(lib().rosetta_rms_norm_backward(yp, ys, gp, gs, hp, hs, wp, wt, ip, dt, rows, dim, xp,
-                                           xs, gweight.data_ptr() if want_gweight else None, wsp,
-                                           wsb, _stream(stream)))
+    _check(lib().rosetta_rms_norm_backward(yp, ys, gp, gs, hp, hs, wp, wt, ip, code, rows, dim, xp,
+                                           xs, gwp, wsp, wsb, _stream_of(gy, stream)))
     return gx, gweight
 
 
@@ -797,13 +799,13 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     """Rows to 8 bits: (q, scale)."""
     torch = _torch()
     xp, xs, rows, dim = _mat(x, "x")
-    dt = _type(x.dtype, "x")
-    q = _made(q, "q", (rows, dim), torch.int8, x)
+    code = _type(x.dtype, "x")
+    q, qp, qs = _made(q, "q", (rows, dim), torch.int8, x)
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    qp, qs = _mat(q, "q")[:2]
-    _check(lib().rosetta_quantize_rows(xp, xs, dt, rows, dim, qp, qs,
-                                       _vec(scale, "scale", torch.float32, rows), _stream(stream)))
+    _check(lib().rosetta_quantize_rows(xp, xs, code, rows, dim, qp, qs,
+                                       _vec(scale, "scale", torch.float32, rows),
+                                       _stream_of(x, stream)))
     return q, scale
 
 
@@ -812,33 +814,36 @@ def dequantize_rows(q, scale, dtype, out=None, stream=None):
     """The values that 8-bit rows stand for."""
     torch = _torch()
     qp, qs, rows, dim = _mat(q, "q", torch.int8)
-    dt = _type(dtype, "dtype")
     sp = _vec(scale, "scale", torch.float32, rows)
-    out = _made(out, "out", (rows, dim), dtype, q)
-    op, os_ = _mat(out, "out")[:2]
-    _check(lib().rosetta_dequantize_rows(qp, qs, sp, dt, rows, dim, op, os_, _stream(stream)))
+    out, op, os_ = _made(out, "out", (rows, dim), dtype, q)
+    _check(lib().rosetta_dequantize_rows(qp, qs, sp, _type(dtype, "dtype"), rows, dim, op, os_,
+                                         _stream_of(q, stream)))
     return out
 
 
 @_on_its_stream
-def q8_matmul(a, a_scale, b, b_scale, bias=None, out_dtype=None, out=None, stream=None):
+def q8_matmul(a, a_scale, b, b_scale, bias=None, out_dtype=None, out=None, workspace=None,
+              stream=None):
     """a [m][k] times b [n][k] (a row per channel), both int8, with a scale per
     row of each: [m][n] of out_dtype (default bfloat16)."""
     torch = _torch()
-    out_dtype = (out.dtype if out is not None else torch.bfloat16) if out_dtype is None \
-        else out_dtype
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if out is None else out.dtype
     ap, as_, m, k = _mat(a, "a", torch.int8)
     bp, bs, n, kb = _mat(b, "b", torch.int8)
     if kb != k:
         raise ValueError(f"b is {n} x {kb}, the call needs rows of {k}")
     sa = _vec(a_scale, "a_scale", torch.float32, m)
     sb = _vec(b_scale, "b_scale", torch.float32, n)
-    bi = _vec(bias, "bias", torch.float32, n) if bias is not None else None
-    dt = _type(out_dtype, "out_dtype")
-    out = _made(out, "out", (m, n), out_dtype, a)
-    op, os_ = _mat(out, "out")[:2]
-    _check(lib().rosetta_q8_matmul(ap, as_, sa, bp, bs, sb, bi, op, os_, dt, m, n, k,
-                                   _stream(stream)))
+    bi = None if bias is None else _vec(bias, "bias", torch.float32, n)
+    out, op, os_ = _made(out, "out", (m, n), out_dtype, a)
+    need = lib().rosetta_q8_matmul_workspace_bytes(m, n, k)
+    wp, wb = None, 0
+    if need:
+        wp, wb, workspace = _scratch(workspace, need, a)
+    _check(lib().rosetta_q8_matmul(ap, as_, sa, bp, bs, sb, bi, op, os_,
+                                   _type(out_dtype, "out_dtype"), m, n, k, wp, wb,
+                                   _stream_of(a, stream)))
     return out
 
 
@@ -853,12 +858,12 @@ def cross_entropy(h, w, targets, ignore_index: int = -100, workspace=None, strea
     if dw != dim:
         raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
     tp = _vec(targets, "targets", torch.int64, rows)
-    ends = torch.empty((2, rows), dtype=torch.float32, device=h.device)
-    loss, lse = ends.unbind(0)
+    loss, lse = (torch.empty(rows, dtype=torch.float32, device=h.device) for _ in range(2))
     sp, sb, workspace = _scratch(
         workspace, lib().rosetta_cross_entropy_workspace_bytes(rows, dim, vocab), h)
     _check(lib().rosetta_cross_entropy(hp, hs, wp, ws, dt, tp, ignore_index, rows, dim, vocab,
-                                       loss.data_ptr(), lse.data_ptr(), sp, sb, _stream(stream)))
+                                       loss.data_ptr(), lse.data_ptr(), sp, sb,
+                                       _stream_of(h, stream)))
     return loss, lse
 
 
@@ -877,15 +882,13 @@ def cross_entropy_backward(h, w, targets, lse, gloss, ignore_index: int = -100,
     tp = _vec(targets, "targets", torch.int64, rows)
     ep = _vec(lse, "lse", torch.float32, rows)
     gp = _vec(gloss, "gloss", torch.float32, rows)
-    gh = _made(gh, "gh", (rows, dim), h.dtype, h) if want_gh else None
-    gw = _made(gw, "gw", (vocab, dim), w.dtype, w) if want_gw else None
-    ghp, ghs = _mat(gh, "gh")[:2] if want_gh else (None, dim)
-    gwp, gws = _mat(gw, "gw")[:2] if want_gw else (None, dim)
+    gh, ghp, ghs = _made(gh, "gh", (rows, dim), h.dtype, h) if want_gh else (None, None, dim)
+    gw, gwp, gws = _made(gw, "gw", (vocab, dim), w.dtype, w) if want_gw else (None, None, dim)
     sp, sb, workspace = _scratch(
         workspace, lib().rosetta_cross_entropy_backward_workspace_bytes(rows, dim, vocab), h)
     _check(lib().rosetta_cross_entropy_backward(hp, hs, wp, ws, dt, tp, ignore_index, ep, gp, rows,
                                                 dim, vocab, ghp, ghs, gwp, gws, sp, sb,
-                                                _stream(stream)))
+                                                _stream_of(h, stream)))
     return gh, gw
 
 

@@ -71,8 +71,8 @@ def test_rows_to_8_bits_and_back(L):
 
 
 def q8(L, a=AT[0], as_=64, sa=AT[1], b=AT[2], bs=64, sb=AT[3], bias=None, o=AT[4], os=96, t=BF16,
-       m=5, n=96, k=64):
-    return L.rosetta_q8_matmul(a, as_, sa, b, bs, sb, bias, o, os, t, m, n, k, None)
+       m=5, n=96, k=64, ws=None, wsb=0):
+    return L.rosetta_q8_matmul(a, as_, sa, b, bs, sb, bias, o, os, t, m, n, k, ws, wsb, None)
 
 
 @pytest.mark.parametrize("kw,status", [
