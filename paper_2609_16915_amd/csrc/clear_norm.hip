@@ -7,6 +7,9 @@
 //   y / scale = h w inv_rms / (max|h w| inv_rms / 127) = h w * (127 / max|h w|):
 // the sum of h^2 and the maximum of |h w| are taken together, and q needs
 // neither inv_rms nor a second pass.
+#include <algorithm>
+#include <type_traits>
+
 #include "clear.hpp"
 
 namespace rosetta {
@@ -28,22 +31,58 @@ struct __attribute__((packed, aligned(1))) Pack {
   T v[VEC];
 };
 
-template <class T>
-__device__ inline void load8(const T *p, size_t left, float (&f)[VEC]) {
-  if (left >= VEC) {
+// (How many elements are left of the row: all eight, known where the row is a
+// whole number of vectors.)
+struct Whole {
+  __device__ constexpr operator size_t() const { return VEC; }
+};
+
+template <class T, class L>
+__device__ inline void load8(const T *p, L left, float (&f)[VEC]) {
+  if ((size_t)left >= VEC) {
     Pack<T> v;
     __builtin_memcpy(&v, p, sizeof v);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) f[i] = to_f(v.v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = (size_t)i < left ? to_f(p[i]) : 0.f;
+    for (int i = 0; i < VEC; ++i) f[i] = (size_t)i < (size_t)left ? to_f(p[i]) : 0.f;
   }
 }
 
+// The same as it lies, widened where it is used: a row's loads wait in few
+// registers.
 template <class T>
-__device__ inline void store8(T *p, size_t left, const float (&f)[VEC]) {
-  if (left >= VEC) {
+struct Raw {
+  static constexpr int WORDS = sizeof(T) * VEC / 4;
+  int w[WORDS];
+  __device__ float operator[](int i) const {
+    if constexpr (std::is_same_v<T, float>) {
+      return __builtin_bit_cast(float, w[i]);
+    } else if constexpr (std::is_same_v<T, bf16>) {
+      return __builtin_bit_cast(float, i % 2 ? w[i / 2] & (int)0xffff0000 : w[i / 2] << 16);
+    } else {
+      using v2h = __attribute__((ext_vector_type(2))) _Float16;
+      return (float)__builtin_bit_cast(v2h, w[i / 2])[i % 2];
+    }
+  }
+};
+
+template <class T, class L>
+__device__ inline void load8_raw(const T *p, L left, Raw<T> &v) {
+  if ((size_t)left >= VEC) {
+    __builtin_memcpy(&v, p, sizeof v);
+  } else {
+    T e[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) e[i] = (size_t)i < (size_t)left ? p[i] : (T)0.f;
+    __builtin_memcpy(&v, e, sizeof v);
+  }
+}
+
+template <class T, class L>
+__device__ inline void store8(T *p, L left, const float (&f)[VEC]) {
+  if ((size_t)left >= VEC) {
     Pack<T> v;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) v.v[i] = from_f<T>(f[i]);
@@ -51,21 +90,22 @@ __device__ inline void store8(T *p, size_t left, const float (&f)[VEC]) {
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      if ((size_t)i < left) p[i] = from_f<T>(f[i]);
+      if ((size_t)i < (size_t)left) p[i] = from_f<T>(f[i]);
   }
 }
 
-__device__ inline void store8_q(int8_t *p, size_t left, const float (&f)[VEC]) {
+template <class L>
+__device__ inline void store8_q(int8_t *p, L left, const float (&f)[VEC]) {
   int8_t b[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i)
     b[i] = (int8_t)(int)fminf(fmaxf(rintf(f[i]), -127.f), 127.f);
-  if (left >= VEC) {
+  if ((size_t)left >= VEC) {
     __builtin_memcpy(p, b, VEC);
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      if ((size_t)i < left) p[i] = b[i];
+      if ((size_t)i < (size_t)left) p[i] = b[i];
   }
 }
 
@@ -104,44 +144,24 @@ __device__ inline void q_factors(float top, float &f0, float &f1) {
   f1 = top > 0.f ? 127.f / (top * f0) : 0.f;
 }
 
-// One row per TPR threads, NV vectors of a thread in registers; NV = 0: rows
-// of any length, read again where they are used.  NORM false: x alone to
-// 8 bits.
-template <class T, class W, int TPR, int NV, bool NORM>
+// TPR threads to a row and NV vectors of a thread in registers, rows one after
+// the other with the next one's loads under way; NV = 0: rows of any length, read
+// again where they are used.  NORM false: x alone to 8 bits.
+template <class T, class W, int TPR, int NV, bool NORM, bool WHOLE>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
   __shared__ float lds[2 * 16];
-  const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-  if (row >= a.rows) return;  // (whole waves: a row of fewer threads is one wave)
+  const size_t first = (size_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const size_t step = (size_t)gridDim.x * ROWS;
   const int t = threadIdx.x % TPR;
   const size_t dim = a.dim;
-  const T *x = (const T *)a.x.p + row * a.x.stride;
-  const T *r = a.residual.p ? (const T *)a.residual.p + row * a.residual.stride : nullptr;
-  const W *w = (const W *)a.weight;
-  T *ho = a.h.p ? (T *)a.h.p + row * a.h.stride : nullptr;
-  T *yo = a.y.p ? (T *)a.y.p + row * a.y.stride : nullptr;
-  int8_t *qo = a.q.p ? (int8_t *)a.q.p + row * a.q.stride : nullptr;
-
-  float sum = 0.f, top = 0.f;
-  // h and h w of the vector at column c
-  auto get = [&](size_t c, float (&h)[VEC], float (&hw)[VEC]) {
-    load8(x + c, dim - c, h);
-    if (NORM && r) {
-      float s[VEC];
-      load8(r + c, dim - c, s);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) h[i] += s[i];
-    }
-    if (NORM && w) {
-      float s[VEC];
-      load8(w + c, dim - c, s);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) hw[i] = h[i] * s[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) hw[i] = h[i];
-    }
+  auto left = [&](size_t c) {
+    if constexpr (WHOLE) return Whole{};
+    else return dim - c;
   };
+  const W *w = (const W *)a.weight;
+
+  float sum, top, f0, f1, inv = 1.f;
   auto count = [&](const float (&h)[VEC], const float (&hw)[VEC]) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
@@ -150,8 +170,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
       top = fmaxf(top, fabsf(hw[i]));
     }
   };
-  float f0, f1, inv = 1.f;
-  auto finish = [&]() {
+  auto finish = [&](size_t row) {
     row_reduce<TPR>(sum, top, lds);
     if (NORM) inv = 1.f / sqrtf(sum / (float)dim + a.eps);
     q_factors(top, f0, f1);
@@ -160,69 +179,128 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
       if (NORM && a.inv_rms) a.inv_rms[row] = inv;
     }
   };
-  auto put = [&](size_t c, const float (&hw)[VEC]) {
+  auto put = [&](size_t row, size_t c, const float (&hw)[VEC]) {
     float o[VEC];
-    if (yo) {
+    if (a.y.p) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) o[i] = hw[i] * inv;
-      store8(yo + c, dim - c, o);
+      store8((T *)a.y.p + row * a.y.stride + c, left(c), o);
     }
-    if (qo) {
+    if (a.q.p) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) o[i] = hw[i] * f0 * f1;
-      store8_q(qo + c, dim - c, o);
+      store8_q((int8_t *)a.q.p + row * a.q.stride + c, left(c), o);
     }
   };
 
   if constexpr (NV > 0) {
-    float hw[NV][VEC];
+    Raw<T> xr[NV], rr[NV];
+    Raw<W> wr[NV];
+    auto ask = [&](size_t row) {
+      const T *x = (const T *)a.x.p + row * a.x.stride;
+      const T *r = (const T *)a.residual.p + row * a.residual.stride;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const size_t c = ((size_t)v * TPR + t) * VEC;
-      if (c < dim) {
-        float h[VEC];
-        get(c, h, hw[v]);
-        if (ho) store8(ho + c, dim - c, h);
-        count(h, hw[v]);
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) {
+          load8_raw(x + c, left(c), xr[v]);
+          if (NORM && a.residual.p) load8_raw(r + c, left(c), rr[v]);
+        }
+      }
+    };
+    if (first < a.rows) ask(first);
+    if (NORM && w) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) load8_raw(w + c, left(c), wr[v]);
       }
     }
-    finish();
+    for (size_t row = first; row < a.rows; row += step) {
+      T *ho = (T *)a.h.p + row * a.h.stride;
+      float hw[NV][VEC];
+      sum = top = 0.f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const size_t c = ((size_t)v * TPR + t) * VEC;
-      if (c < dim) put(c, hw[v]);
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) {
+          float h[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            h[i] = xr[v][i];
+            if (NORM && a.residual.p) h[i] += rr[v][i];
+            hw[v][i] = NORM && w ? h[i] * wr[v][i] : h[i];
+          }
+          if (a.h.p) store8(ho + c, left(c), h);
+          count(h, hw[v]);
+        }
+      }
+      if (row + step < a.rows) ask(row + step);
+      finish(row);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) put(row, c, hw[v]);
+      }
     }
   } else {
-    float h[VEC], hw[VEC];
-    for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
-      get(c, h, hw);
-      count(h, hw);
-    }
-    finish();
-    // h is written last, column by column as it is read: it may be x or residual
-    for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
-      get(c, h, hw);
-      if (ho) store8(ho + c, dim - c, h);
-      put(c, hw);
+    for (size_t row = first; row < a.rows; row += step) {
+      const T *x = (const T *)a.x.p + row * a.x.stride;
+      const T *r = a.residual.p ? (const T *)a.residual.p + row * a.residual.stride : nullptr;
+      T *ho = a.h.p ? (T *)a.h.p + row * a.h.stride : nullptr;
+      float h[VEC], hw[VEC];
+      // h and h w of the vector at column c
+      auto get = [&](size_t c) {
+        load8(x + c, left(c), h);
+        if (NORM && r) {
+          float s[VEC];
+          load8(r + c, left(c), s);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) h[i] += s[i];
+        }
+        float s[VEC];
+        if (NORM && w) load8(w + c, left(c), s);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) hw[i] = NORM && w ? h[i] * s[i] : h[i];
+      };
+      sum = top = 0.f;
+      for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
+        get(c);
+        count(h, hw);
+      }
+      finish(row);
+      // h is written last, column by column as it is read: it may be x or residual
+      for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
+        get(c);
+        if (ho) store8(ho + c, left(c), h);
+        put(row, c, hw);
+      }
     }
   }
 }
 
-template <class T, class W, bool NORM>
+template <class T, class W, bool NORM, bool WHOLE>
 hipError_t norm_by_size(const NormArgs &a, hipStream_t st) {
   auto go = [&](auto kernel, int tpr) {
     const int per = tpr < 256 ? 256 / tpr : 1;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + per - 1) / per)),
+    // four waves a SIMD: with their next rows under way they have enough to wait for
+    const size_t most = 1024 / (tpr < 256 ? 256 : tpr) * (size_t)std::max(1, device_cus());
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, (a.rows + per - 1) / per)),
                        dim3(tpr < 256 ? 256 : tpr), 0, st, a);
     return hipGetLastError();
   };
   const size_t d = a.dim;
-  if (d <= 64 * VEC) return go(k_rms_norm<T, W, 64, 1, NORM>, 64);
-  if (d <= 256 * VEC) return go(k_rms_norm<T, W, 256, 1, NORM>, 256);
-  if (d <= 256 * VEC * 2) return go(k_rms_norm<T, W, 256, 2, NORM>, 256);
-  if (d <= 256 * VEC * 4) return go(k_rms_norm<T, W, 256, 4, NORM>, 256);
-  if (d <= 1024 * VEC * 2) return go(k_rms_norm<T, W, 1024, 2, NORM>, 1024);
-  return go(k_rms_norm<T, W, 1024, 0, NORM>, 1024);
+  if (d <= 64 * VEC) return go(k_rms_norm<T, W, 64, 1, NORM, WHOLE>, 64);
+  if (d <= 256 * VEC) return go(k_rms_norm<T, W, 256, 1, NORM, WHOLE>, 256);
+  if (d <= 256 * VEC * 2) return go(k_rms_norm<T, W, 256, 2, NORM, WHOLE>, 256);
+  if (d <= 256 * VEC * 4) return go(k_rms_norm<T, W, 256, 4, NORM, WHOLE>, 256);
+  if (d <= 1024 * VEC * 2) return go(k_rms_norm<T, W, 1024, 2, NORM, WHOLE>, 1024);
+  return go(k_rms_norm<T, W, 1024, 0, NORM, WHOLE>, 1024);
+}
+
+template <class T, class W, bool NORM>
+hipError_t norm_by_length(const NormArgs &a, hipStream_t st) {
+  return a.dim % VEC ? norm_by_size<T, W, NORM, false>(a, st) : norm_by_size<T, W, NORM, true>(a, st);
 }
 
 template <class T>
@@ -248,19 +326,19 @@ k_dequantize_rows(const int8_t *__restrict__ q, size_t q_stride, const float *__
 hipError_t launch_rms_norm(const NormArgs &a, hipStream_t st) {
   const bool wf = a.weight && a.weight_dtype == ROSETTA_F32;
   switch (a.dtype) {
-    case ROSETTA_F32: return norm_by_size<float, float, true>(a, st);
+    case ROSETTA_F32: return norm_by_length<float, float, true>(a, st);
     case ROSETTA_BF16:
-      return wf ? norm_by_size<bf16, float, true>(a, st) : norm_by_size<bf16, bf16, true>(a, st);
+      return wf ? norm_by_length<bf16, float, true>(a, st) : norm_by_length<bf16, bf16, true>(a, st);
     default:
-      return wf ? norm_by_size<f16, float, true>(a, st) : norm_by_size<f16, f16, true>(a, st);
+      return wf ? norm_by_length<f16, float, true>(a, st) : norm_by_length<f16, f16, true>(a, st);
   }
 }
 
 hipError_t launch_quantize_rows(const NormArgs &a, hipStream_t st) {
   switch (a.dtype) {
-    case ROSETTA_F32: return norm_by_size<float, float, false>(a, st);
-    case ROSETTA_BF16: return norm_by_size<bf16, bf16, false>(a, st);
-    default: return norm_by_size<f16, f16, false>(a, st);
+    case ROSETTA_F32: return norm_by_length<float, float, false>(a, st);
+    case ROSETTA_BF16: return norm_by_length<bf16, bf16, false>(a, st);
+    default: return norm_by_length<f16, f16, false>(a, st);
   }
 }
 
@@ -288,17 +366,21 @@ hipError_t launch_dequantize_rows(const int8_t *q, size_t q_stride, const float 
 
 namespace {
 
-constexpr size_t BACK_GROUPS = 512;  // two workgroups of rows per CU
+constexpr size_t BACK_GROUPS = 512;  // two workgroups of rows per CU (three: 56.4 us for 53.8)
 
 // A workgroup takes rows blockIdx.x, + gridDim.x, ..; each thread keeps the sums
 // over rows of its columns' gy h inv_rms and writes them to the workgroup's
 // row of `partial`, which k_sum_partial adds up in order.  NV = 0: rows of any
 // length; the sums are then kept in `partial` itself.
-template <class T, class W, int TPR, int NV>
+template <class T, class W, int TPR, int NV, bool WHOLE>
 __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
   __shared__ float lds[2 * 16];
   const int t = threadIdx.x;
   const size_t dim = a.dim;
+  auto left = [&](size_t c) {
+    if constexpr (WHOLE) return Whole{};
+    else return dim - c;
+  };
   const W *w = (const W *)a.weight;
   float *part = a.partial ? a.partial + (size_t)blockIdx.x * dim : nullptr;
   constexpr int NS = NV > 0 ? NV : 1;
@@ -308,77 +390,110 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sums[v][i] = 0.f;
 
-  for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T *gy = (const T *)a.gy.p + row * a.gy.stride;
-    const T *gh = a.gh.p ? (const T *)a.gh.p + row * a.gh.stride : nullptr;
-    const T *h = (const T *)a.h.p + row * a.h.stride;
-    T *gx = (T *)a.gx.p + row * a.gx.stride;
-    const float inv = a.inv_rms[row];
-    float dot = 0.f, none = 0.f;
-    // h and gy w of the vector at column c, and the terms of gweight
-    auto get = [&](size_t c, float (&hv)[VEC], float (&g)[VEC], float (&s)[VEC], bool add) {
-      load8(gy + c, dim - c, g);
-      load8(h + c, dim - c, hv);
-      if (add) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) s[i] = fmaf(g[i] * inv, hv[i], s[i]);
-      }
-      if (w) {
-        float u[VEC];
-        load8(w + c, dim - c, u);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) g[i] *= u[i];
-      }
-    };
-    auto put = [&](size_t c, const float (&hv)[VEC], const float (&g)[VEC], float k) {
-      float o[VEC];
-      if (gh) {
-        load8(gh + c, dim - c, o);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) o[i] = 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) o[i] += g[i] * inv - hv[i] * k;
-      store8(gx + c, dim - c, o);
-    };
-    if constexpr (NV > 0) {
-      float hv[NV][VEC], g[NV][VEC];
+  float none = 0.f;
+  if constexpr (NV > 0) {
+    Raw<T> yr[NV], hr[NV], gr[NV];
+    Raw<W> wr[NV];
+    float inv_next = 0.f;
+    auto ask = [&](size_t row) {
+      const T *gy = (const T *)a.gy.p + row * a.gy.stride;
+      const T *h = (const T *)a.h.p + row * a.h.stride;
+      const T *gh = (const T *)a.gh.p + row * a.gh.stride;
+      inv_next = a.inv_rms[row];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
-          get(c, hv[v], g[v], sums[v], true);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) dot = fmaf(g[v][i], hv[v][i], dot);
+          load8_raw(gy + c, left(c), yr[v]);
+          load8_raw(h + c, left(c), hr[v]);
+          if (a.gh.p) load8_raw(gh + c, left(c), gr[v]);
         }
       }
+    };
+    ask(blockIdx.x);
+    if (w) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) load8_raw(w + c, left(c), wr[v]);
+      }
+    }
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+      T *gx = (T *)a.gx.p + row * a.gx.stride;
+      const float inv = inv_next;
+      float hv[NV][VEC], g[NV][VEC], o[NV][VEC], dot = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            hv[v][i] = hr[v][i];
+            g[v][i] = yr[v][i];
+            sums[v][i] = fmaf(g[v][i] * inv, hv[v][i], sums[v][i]);
+            if (w) g[v][i] *= wr[v][i];
+            dot = fmaf(g[v][i], hv[v][i], dot);
+            o[v][i] = a.gh.p ? gr[v][i] : 0.f;
+          }
+        }
+      }
+      if (row + gridDim.x < a.rows) ask(row + gridDim.x);
       row_reduce<TPR>(dot, none, lds);
       const float k = dot * inv * inv * inv / (float)dim;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
-        if (c < dim) put(c, hv[v], g[v], k);
+        if (c < dim) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) o[v][i] += g[v][i] * inv - hv[v][i] * k;
+          store8(gx + c, left(c), o[v]);
+        }
       }
-    } else {
-      float hv[VEC], g[VEC], s[VEC];
+    }
+  } else {
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+      const T *gy = (const T *)a.gy.p + row * a.gy.stride;
+      const T *gh = a.gh.p ? (const T *)a.gh.p + row * a.gh.stride : nullptr;
+      const T *h = (const T *)a.h.p + row * a.h.stride;
+      T *gx = (T *)a.gx.p + row * a.gx.stride;
+      const float inv = a.inv_rms[row];
+      float hv[VEC], g[VEC], s[VEC], dot = 0.f;
+      // h and gy w of the vector at column c, and the terms of gweight
+      auto get = [&](size_t c, bool add) {
+        load8(gy + c, left(c), g);
+        load8(h + c, left(c), hv);
+        if (add) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) s[i] = fmaf(g[i] * inv, hv[i], s[i]);
+        }
+        if (w) {
+          float u[VEC];
+          load8(w + c, left(c), u);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) g[i] *= u[i];
+        }
+      };
       for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
         if (part && row != blockIdx.x) {
-          load8(part + c, dim - c, s);
+          load8(part + c, left(c), s);
         } else {
 #pragma unroll
           for (int i = 0; i < VEC; ++i) s[i] = 0.f;
         }
-        get(c, hv, g, s, true);
-        if (part) store8(part + c, dim - c, s);
+        get(c, true);
+        if (part) store8(part + c, left(c), s);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dot = fmaf(g[i], hv[i], dot);
       }
       row_reduce<TPR>(dot, none, lds);
       const float k = dot * inv * inv * inv / (float)dim;
       for (size_t c = (size_t)t * VEC; c < dim; c += (size_t)TPR * VEC) {
-        get(c, hv, g, s, false);
-        put(c, hv, g, k);
+        get(c, false);
+        float o[VEC];
+        if (gh) load8(gh + c, left(c), o);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) o[i] = (gh ? o[i] : 0.f) + g[i] * inv - hv[i] * k;
+        store8(gx + c, left(c), o);
       }
     }
   }
@@ -387,7 +502,7 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
-        if (c < dim) store8(part + c, dim - c, sums[v]);
+        if (c < dim) store8(part + c, left(c), sums[v]);
       }
     }
   }
@@ -402,8 +517,10 @@ k_sum_partial(const float *__restrict__ partial, size_t groups, size_t dim,
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const size_t c = (size_t)blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (c < dim)
+  if (c < dim) {
+#pragma unroll 8
     for (size_t g = wave; g < groups; g += 16) s += partial[g * dim + c];
+  }
   lds[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && c < dim) {
@@ -412,7 +529,7 @@ k_sum_partial(const float *__restrict__ partial, size_t groups, size_t dim,
   }
 }
 
-template <class T, class W>
+template <class T, class W, bool WHOLE>
 hipError_t back_by_size(const NormBackArgs &a, hipStream_t st) {
   const size_t groups = norm_back_groups(a.rows);
   auto go = [&](auto kernel, int tpr) {
@@ -421,16 +538,21 @@ hipError_t back_by_size(const NormBackArgs &a, hipStream_t st) {
   };
   const size_t d = a.dim;
   hipError_t e;
-  if (d <= 64 * VEC) e = go(k_rms_norm_backward<T, W, 64, 1>, 64);
-  else if (d <= 256 * VEC) e = go(k_rms_norm_backward<T, W, 256, 1>, 256);
-  else if (d <= 256 * VEC * 2) e = go(k_rms_norm_backward<T, W, 256, 2>, 256);
-  else if (d <= 512 * VEC * 2) e = go(k_rms_norm_backward<T, W, 512, 2>, 512);
-  else if (d <= 1024 * VEC * 2) e = go(k_rms_norm_backward<T, W, 1024, 2>, 1024);
-  else e = go(k_rms_norm_backward<T, W, 1024, 0>, 1024);
+  if (d <= 64 * VEC) e = go(k_rms_norm_backward<T, W, 64, 1, WHOLE>, 64);
+  else if (d <= 256 * VEC) e = go(k_rms_norm_backward<T, W, 256, 1, WHOLE>, 256);
+  else if (d <= 256 * VEC * 2) e = go(k_rms_norm_backward<T, W, 256, 2, WHOLE>, 256);
+  else if (d <= 512 * VEC * 2) e = go(k_rms_norm_backward<T, W, 512, 2, WHOLE>, 512);
+  else if (d <= 512 * VEC * 4) e = go(k_rms_norm_backward<T, W, 512, 4, WHOLE>, 512);
+  else e = go(k_rms_norm_backward<T, W, 1024, 0, WHOLE>, 1024);
   if (e != hipSuccess || !a.gweight) return e;
   hipLaunchKernelGGL(k_sum_partial, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, st, a.partial,
                      groups, d, a.gweight);
   return hipGetLastError();
+}
+
+template <class T, class W>
+hipError_t back_by_length(const NormBackArgs &a, hipStream_t st) {
+  return a.dim % VEC ? back_by_size<T, W, false>(a, st) : back_by_size<T, W, true>(a, st);
 }
 
 }  // namespace
@@ -440,10 +562,10 @@ size_t norm_back_groups(size_t rows) { return rows < BACK_GROUPS ? rows : BACK_G
 hipError_t launch_rms_norm_backward(const NormBackArgs &a, hipStream_t st) {
   const bool wf = a.weight && a.weight_dtype == ROSETTA_F32;
   switch (a.dtype) {
-    case ROSETTA_F32: return back_by_size<float, float>(a, st);
+    case ROSETTA_F32: return back_by_length<float, float>(a, st);
     case ROSETTA_BF16:
-      return wf ? back_by_size<bf16, float>(a, st) : back_by_size<bf16, bf16>(a, st);
-    default: return wf ? back_by_size<f16, float>(a, st) : back_by_size<f16, f16>(a, st);
+      return wf ? back_by_length<bf16, float>(a, st) : back_by_length<bf16, bf16>(a, st);
+    default: return wf ? back_by_length<f16, float>(a, st) : back_by_length<f16, f16>(a, st);
   }
 }
 

@@ -24,6 +24,7 @@ using Small = Shape<128, 128, 4, 2>;
 template <class T, class S>
 using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY>;
 
+constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
 
 size_t up(size_t a, size_t b) { return (a + b - 1) / b * b; }
@@ -44,64 +45,71 @@ __device__ inline bool counts(int64_t target, int64_t ignore, size_t vocab) {
   return target != ignore && target >= 0 && target < (int64_t)vocab;
 }
 
+template <class T>
+__device__ inline Operand w_rows(const LossArgs &a) {
+  return {(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab,
+          (int64_t)(a.dim * sizeof(T))};
+}
+template <class T>
+__device__ inline Operand h_rows(const LossArgs &a) {
+  return {(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows,
+          (int64_t)(a.dim * sizeof(T))};
+}
+
 // part[tile of x][row], and the logit of each row's target
 template <class T, class S, bool ALIGNED>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) {
   using Tl = TileOf<T, S>;
-  constexpr int BX = S::BX, BY = S::BY;
+  constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
-  Stat *joint = (Stat *)(lds + Tl::LDS);  // [S::WX][BY]
   const unsigned gx = (unsigned)((a.vocab + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
-  const int64_t bytes = (int64_t)a.dim * sizeof(T);
-  auto where = [&](unsigned t) {
-    unsigned tx, ty;
-    band_tile(xcd_block(t, gx * gy), gx, gy, tx, ty);
-    return typename Tl::Place{
-        {(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab, bytes},
-        {(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows, bytes},
-        (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes};
-  };
-  auto done = [&](unsigned t, v4f(&acc)[Tl::TX][Tl::TY]) {
-    unsigned tx, ty;
-    band_tile(xcd_block(t, gx * gy), gx, gy, tx, ty);
-    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  unsigned tx, ty;
+  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  v4f acc[Tl::TX][Tl::TY];
+  Tl::template run<ALIGNED>({w_rows<T>(a), h_rows<T>(a), (int64_t)tx * BX, (int64_t)ty * BY, 0,
+                             (int64_t)(a.dim * sizeof(T))},
+                            lds, acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  Stat *joint = (Stat *)lds;  // [S::WX][BY]
+  if (x0 + RUN > (int64_t)a.vocab) {
 #pragma unroll
-    for (int j = 0; j < Tl::TY; ++j) {
-      const int y = Tl::y_at() + 16 * j;
-      const int64_t row = (int64_t)ty * BY + y;
-      const int64_t target = row < (int64_t)a.rows ? a.targets[row] : -1;
-      Stat s{-INFINITY, 0.f};
+    for (int i = 0; i < RUN; ++i)
+      if (x0 + i >= (int64_t)a.vocab) {
 #pragma unroll
-      for (int i = 0; i < Tl::TX; ++i)
+        for (int j = 0; j < Tl::TY; ++j) acc[i / 4][j][i % 4] = -INFINITY;
+      }
+  }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (x0 + 4 * i + r >= (int64_t)a.vocab) acc[i][j][r] = -INFINITY;
-          s.top = fmaxf(s.top, acc[i][j][r]);
-        }
-      const float low = s.top == -INFINITY ? 0.f : s.top;
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int y = Tl::y_at() + 16 * j;
+    const int64_t row = (int64_t)ty * BY + y;
+    const int64_t at = row < (int64_t)a.rows ? a.targets[row] - x0 : -1;
+    if (at >= 0 && at < RUN && x0 + at < (int64_t)a.vocab) {
 #pragma unroll
-      for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (x0 + 4 * i + r == target && row < (int64_t)a.rows) at_target[row] = acc[i][j][r];
-          s.sum += __expf(acc[i][j][r] - low);
-        }
-#pragma unroll
-      for (int m = 16; m <= 32; m <<= 1)
-        s = join(s, Stat{__shfl_xor(s.top, m), __shfl_xor(s.sum, m)});
-      if (threadIdx.x % 64 < 16) joint[(threadIdx.x / 64 % S::WX) * BY + y] = s;
+      for (int i = 0; i < RUN; ++i)
+        if (at == i) at_target[row] = acc[i / 4][j][i % 4];
     }
-    __syncthreads();
-    for (int y = threadIdx.x; y < BY; y += Tl::THREADS) {
-      const int64_t row = (int64_t)ty * BY + y;
-      if (row >= (int64_t)a.rows) break;
-      Stat s = joint[y];
-      for (int w = 1; w < S::WX; ++w) s = join(s, joint[w * BY + y]);
-      part[(size_t)tx * a.rows + row] = s;
-    }
-  };
-  Tl::template each<ALIGNED>(blockIdx.x, gridDim.x, gx * gy, lds, where, done);
+    Stat s{-INFINITY, 0.f};
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) s.top = fmaxf(s.top, acc[i / 4][j][i % 4]);
+    const float low = s.top == -INFINITY ? 0.f : s.top * LOG2E;
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+      s.sum += __builtin_amdgcn_exp2f(fmaf(acc[i / 4][j][i % 4], LOG2E, -low));
+#pragma unroll
+    for (int m = 16; m <= 32; m <<= 1)
+      s = join(s, Stat{__shfl_xor(s.top, m), __shfl_xor(s.sum, m)});
+    if (threadIdx.x % 64 < 16) joint[(threadIdx.x / 64 % S::WX) * BY + y] = s;
+  }
+  __syncthreads();
+  for (int y = threadIdx.x; y < BY; y += Tl::THREADS) {
+    const int64_t row = (int64_t)ty * BY + y;
+    if (row >= (int64_t)a.rows) break;
+    Stat s = joint[y];
+    for (int w = 1; w < S::WX; ++w) s = join(s, joint[w * BY + y]);
+    part[(size_t)tx * a.rows + row] = s;
+  }
 }
 
 // The same for at most 16 NY rows.
@@ -194,68 +202,74 @@ __global__ void __launch_bounds__(1024) k_loss_coef(LossArgs a, float *__restric
 
 // gl of the vocabulary rows [v0, v0 + here), `here` rounded up to whole tiles: as
 // gl [rows][vp] and as gl_t [vp][ld_t], zeros beyond the vocabulary and the rows.
-// One tile a workgroup: gl_t goes through the stages, a wave's part in turn, so
-// that its rows leave in runs of the part's height.
+// gl_t goes through the stages, each wave's part on its own, so that its rows
+// leave in runs of the part's height.
 template <class T, class S, bool ALIGNED>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                  const float *__restrict__ coef, T *__restrict__ gl, T *__restrict__ gl_t) {
   using Tl = TileOf<T, S>;
   constexpr int BX = S::BX, BY = S::BY;
+  constexpr int HX = 16 * Tl::TX, HY = 16 * Tl::TY, RUN = 4 * Tl::TX;  // a wave's part
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((here + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
-  const int64_t bytes = (int64_t)a.dim * sizeof(T);
-  auto where = [&](unsigned) {
-    return typename Tl::Place{
-        {(const char *)a.w, (int64_t)(a.w_stride * sizeof(T)), (int64_t)a.vocab, bytes},
-        {(const char *)a.h, (int64_t)(a.h_stride * sizeof(T)), (int64_t)a.rows, bytes},
-        (int64_t)(v0 + (size_t)tx * BX), (int64_t)ty * BY, 0, bytes};
-  };
-  auto done = [&](unsigned, v4f(&acc)[Tl::TX][Tl::TY]) {
-    constexpr int HX = 16 * Tl::TX, HY = 16 * Tl::TY;  // the wave's part
-    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
-    const int lane = threadIdx.x % 64, g = lane / 16;
-    T *mine = (T *)lds + threadIdx.x / 64 * (HX * HY);  // [x][y], runs of 16 y moved about
+  v4f acc[Tl::TX][Tl::TY];
+  Tl::template run<ALIGNED>({w_rows<T>(a), h_rows<T>(a), (int64_t)(v0 + (size_t)tx * BX),
+                             (int64_t)ty * BY, 0, (int64_t)(a.dim * sizeof(T))},
+                            lds, acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  const int64_t left = (int64_t)a.vocab - (int64_t)v0 - x0;  // words of the run that exist
+  const int lane = threadIdx.x % 64, g = lane / 16;
+  T *mine = (T *)lds + threadIdx.x / 64 * (HX * HY);  // [x][y], runs of 16 y moved about
 #pragma unroll
-    for (int j = 0; j < Tl::TY; ++j) {
-      const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-      const bool in = row < (int64_t)a.rows;
-      const float c = in ? coef[row] : 0.f, lse = in ? a.lse[row] : 0.f;
-      const int64_t target = in ? a.targets[row] : -1;
-      float f[4 * Tl::TX];
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    const bool in = row < (int64_t)a.rows;
+    const float c = in ? coef[row] : 0.f, lse = in ? a.lse[row] * LOG2E : 0.f;
+    const int64_t at = in ? a.targets[row] - (int64_t)v0 - x0 : -1;
+    T f[RUN];
+    // (c = 0: a row that takes no part, whatever its logits are)
 #pragma unroll
-      for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t v = (int64_t)v0 + x0 + 4 * i + r;
-          const float p = __expf(acc[i][j][r] - lse) - (v == target ? 1.f : 0.f);
-          f[4 * i + r] = in && c != 0.f && v < (int64_t)a.vocab ? p * c : 0.f;
-        }
-      if (gl && in) store_run(gl + row * (int64_t)vp + x0, 4 * Tl::TX, f);
-      // (the four lanes groups of an x each to other banks)
-      if (gl_t) {
-        const int at = (j ^ (g & (Tl::TY - 1))) * 16 + lane % 16;
-#pragma unroll
-        for (int i = 0; i < 4 * Tl::TX; ++i) mine[(g * 4 * Tl::TX + i) * HY + at] = (T)f[i];
-      }
+    for (int i = 0; i < RUN; ++i) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(acc[i / 4][j][i % 4], LOG2E, -lse));
+      acc[i / 4][j][i % 4] = c == 0.f ? 0.f : e * c;
     }
-    if (!gl_t) return;
-    // (the wave's lanes read one another's words)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int wx = threadIdx.x / 64 % S::WX, wy = threadIdx.x / 64 / S::WX;
-    const int64_t y0 = (int64_t)ty * BY + wy * HY;
-    T *out = gl_t + ((int64_t)tx * BX + wx * HX) * (int64_t)ld_t + y0;
+    if (at >= 0 && at < RUN) {
 #pragma unroll
-    for (int i = 0; i < HX * HY / 512; ++i) {
-      const int x = (i * 64 + lane) / (HY / 8), y = (i * 64 + lane) % (HY / 8) * 8;
-      const int at = ((y / 16) ^ (x / (4 * Tl::TX) & (Tl::TY - 1))) * 16 + y % 16;
-      if (y0 + y < (int64_t)ld_t) *(v4i *)(out + x * (int64_t)ld_t + y) = *(const v4i *)(mine + x * HY + at);
+      for (int i = 0; i < RUN; ++i)
+        if (at == i) acc[i / 4][j][i % 4] -= c;
     }
-  };
-  Tl::template each<ALIGNED>(0, 1, 1, lds, where, done);
+    if (left < RUN) {
+#pragma unroll
+      for (int i = 0; i < RUN; ++i)
+        if (i >= left) acc[i / 4][j][i % 4] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) f[i] = (T)acc[i / 4][j][i % 4];
+    if (gl && in) __builtin_memcpy(gl + row * (int64_t)vp + x0, f, sizeof f);
+    // (the four lane groups of an x each to other banks)
+    if (gl_t) {
+      const int to = (j ^ (g & (Tl::TY - 1))) * 16 + lane % 16;
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) mine[(g * RUN + i) * HY + to] = f[i];
+    }
+  }
+  if (!gl_t) return;
+  // (the wave's lanes read one another's words)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int wx = threadIdx.x / 64 % S::WX, wy = threadIdx.x / 64 / S::WX;
+  const int64_t y0 = (int64_t)ty * BY + wy * HY;
+  T *out = gl_t + ((int64_t)tx * BX + wx * HX) * (int64_t)ld_t + y0;
+#pragma unroll
+  for (int i = 0; i < HX * HY / 512; ++i) {
+    const int x = (i * 64 + lane) / (HY / 8), y = (i * 64 + lane) % (HY / 8) * 8;
+    const int from = ((y / 16) ^ (x / RUN & (Tl::TY - 1))) * 16 + y % 16;
+    if (y0 + y < (int64_t)ld_t)
+      *(v4i *)(out + x * (int64_t)ld_t + y) = *(const v4i *)(mine + x * HY + from);
+  }
 }
 
 // out [cols][ld] = in [rows][cols] the other way round, zeros in columns
@@ -299,48 +313,35 @@ k_transpose(const T *__restrict__ in, size_t in_stride, size_t rows, size_t cols
 template <class T, class S>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restrict__ gl,
-               const T *__restrict__ w_t, float *__restrict__ part, size_t run, int splits,
-               int add) {
+               const T *__restrict__ w_t, float *__restrict__ part, size_t run, int add) {
   using Tl = TileOf<T, S>;
-  constexpr int BX = S::BX, BY = S::BY;
+  constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
-  const unsigned count = gx * gy * splits;
+  const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
+  unsigned tx, ty;
+  band_tile(b % (gx * gy), gx, gy, tx, ty);
   // (whole 16 bytes: both have zeros there)
   const int64_t ld = (int64_t)vp * sizeof(T), bytes = (int64_t)((here + 7) / 8 * 8) * sizeof(T);
-  auto where = [&](unsigned t) {
-    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
-    unsigned tx, ty;
-    band_tile(b % (gx * gy), gx, gy, tx, ty);
-    int64_t k0 = (int64_t)(split * run * sizeof(T)), k1 = k0 + (int64_t)(run * sizeof(T));
-    k1 = k1 < bytes ? k1 : bytes;
-    k0 = k0 < k1 ? k0 : k1;
-    return typename Tl::Place{{(const char *)w_t, ld, (int64_t)dim, bytes},
-                              {(const char *)gl, ld, (int64_t)rows, bytes},
-                              (int64_t)tx * BX, (int64_t)ty * BY, k0, k1};
-  };
-  auto done = [&](unsigned t, v4f(&acc)[Tl::TX][Tl::TY]) {
-    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
-    unsigned tx, ty;
-    band_tile(b % (gx * gy), gx, gy, tx, ty);
-    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  const int64_t k0 = (int64_t)(split * run * sizeof(T)), k1 = k0 + (int64_t)(run * sizeof(T));
+  v4f acc[Tl::TX][Tl::TY];
+  Tl::template run<true>({{(const char *)w_t, ld, (int64_t)dim, bytes},
+                          {(const char *)gl, ld, (int64_t)rows, bytes},
+                          (int64_t)tx * BX, (int64_t)ty * BY, k0, k1 < bytes ? k1 : bytes},
+                         lds, acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)dim - x0;
+  if (left <= 0) return;
 #pragma unroll
-    for (int j = 0; j < Tl::TY; ++j) {
-      const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-      if (row >= (int64_t)rows || x0 >= (int64_t)dim) continue;
-      float *out = part + ((size_t)split * rows + row) * dim + x0;
-      float f[4 * Tl::TX];
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    if (row >= (int64_t)rows) continue;
+    float *out = part + ((size_t)split * rows + row) * dim + x0;
+    float f[RUN] = {};
+    if (add) load_run(out, left, f);
 #pragma unroll
-      for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          f[4 * i + r] = acc[i][j][r];
-          if (add && x0 + 4 * i + r < (int64_t)dim) f[4 * i + r] += out[4 * i + r];
-        }
-      store_run(out, (int64_t)dim - x0, f);
-    }
-  };
-  Tl::template each<true>(blockIdx.x, gridDim.x, count, lds, where, done);
+    for (int i = 0; i < RUN; ++i) f[i] += acc[i / 4][j][i % 4];
+    store_run(out, left, f);
+  }
 }
 
 template <class T>
@@ -362,35 +363,29 @@ __global__ void __launch_bounds__(S::THREADS)
 k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__restrict__ coef,
                const T *__restrict__ gl_t, const T *__restrict__ h_t) {
   using Tl = TileOf<T, S>;
-  constexpr int BX = S::BX, BY = S::BY;
+  constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)((here + BY - 1) / BY);
+  unsigned tx, ty;
+  band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
   const int64_t bytes = (int64_t)ld_t * sizeof(T);
+  v4f acc[Tl::TX][Tl::TY];
+  Tl::template run<true>({{(const char *)h_t, bytes, (int64_t)a.dim, bytes},
+                          {(const char *)gl_t, bytes, (int64_t)here, bytes},
+                          (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes},
+                         lds, acc);
   const float back = coef[a.rows];
-  auto where = [&](unsigned t) {
-    unsigned tx, ty;
-    band_tile(xcd_block(t, gx * gy), gx, gy, tx, ty);
-    return typename Tl::Place{{(const char *)h_t, bytes, (int64_t)a.dim, bytes},
-                              {(const char *)gl_t, bytes, (int64_t)here, bytes},
-                              (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes};
-  };
-  auto done = [&](unsigned t, v4f(&acc)[Tl::TX][Tl::TY]) {
-    unsigned tx, ty;
-    band_tile(xcd_block(t, gx * gy), gx, gy, tx, ty);
-    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
+  if (left <= 0) return;
 #pragma unroll
-    for (int j = 0; j < Tl::TY; ++j) {
-      const int64_t v = (int64_t)v0 + (int64_t)ty * BY + Tl::y_at() + 16 * j;
-      if (v >= (int64_t)a.vocab || x0 >= (int64_t)a.dim) continue;
-      float f[4 * Tl::TX];
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t v = (int64_t)v0 + (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    if (v >= (int64_t)a.vocab) continue;
+    float f[RUN];
 #pragma unroll
-      for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) f[4 * i + r] = acc[i][j][r] * back;
-      store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, (int64_t)a.dim - x0, f);
-    }
-  };
-  Tl::template each<true>(blockIdx.x, gridDim.x, gx * gy, lds, where, done);
+    for (int i = 0; i < RUN; ++i) f[i] = acc[i / 4][j][i % 4] * back;
+    store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f);
+  }
 }
 
 // Rows of the vocabulary in a block of the forward pass; 0: Thin's, for as few
@@ -444,14 +439,6 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   return p;
 }
 
-// Blocks for `count` tiles: one a CU that go through them where a tile fills the
-// CU, one a tile where two fit.
-template <class S>
-dim3 blocks(size_t count) {
-  const size_t cus = (size_t)device_cus();
-  return dim3((unsigned)(S::BX == Large::BX && cus && count > cus ? cus : count));
-}
-
 bool aligned(const LossArgs &a) {
   const Operand X{(const char *)a.w, (int64_t)(a.w_stride * 2), (int64_t)a.vocab,
                   (int64_t)(a.dim * 2)};
@@ -479,8 +466,8 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
   auto tile = [&](auto shape) {
     using S = decltype(shape);
     auto k = aligned(a) ? k_loss_tile<T, S, true> : k_loss_tile<T, S, false>;
-    LAUNCH(k, blocks<S>(nx * tiles(a.rows, S::BY)), S::THREADS,
-           (TileOf<T, S>::LDS + S::WX * S::BY * (int)sizeof(Stat)), a, part, at_target);
+    LAUNCH(k, dim3((unsigned)(nx * tiles(a.rows, S::BY))), S::THREADS,
+           (TileOf<T, S>::LDS), a, part, at_target);
   };
   if (a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
   else if (a.rows <= 32) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
@@ -512,12 +499,10 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
     if (a.gh) {
       LAUNCH(k_transpose<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
              (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
-      LAUNCH((k_loss_gh_tile<T, S>), blocks<S>(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY)),
-             S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp, gl, w_t, part, p.run, (int)p.splits,
-             i > 0);
+      LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp, gl, w_t, part, p.run, i > 0);
     }
     if (a.gw)
-      LAUNCH((k_loss_gw_tile<T, S>), blocks<S>(tiles(a.dim, BX) * tiles(here, BY)), S::THREADS,
+      LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)(tiles(a.dim, BX) * tiles(here, BY))), S::THREADS,
              Tl::LDS, a, v0, here, p.ld_t, coef, gl_t, h_t);
   }
   if (a.gh)

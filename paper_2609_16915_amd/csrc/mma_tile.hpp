@@ -155,14 +155,12 @@ struct Tile {
     int64_t x0, y0, k0, k1;
   };
 
-  // The tiles first, first + stride, .. below count, one after the other:
-  // where(t) says where tile t is, done(t, acc) takes its sums.  The loads of a
-  // tile's first steps run while the sums of the one before are written; done()
-  // must leave the stages (the first LDS bytes) alone.
-  template <bool ALIGNED, class Where, class Done>
-  __device__ static void each(unsigned first, unsigned stride, unsigned count, char *lds,
-                              Where where, Done done) {
-    if (first >= count) return;
+  // The tile's sums.  The stages are free when it returns.  (Blocks that go through
+  // several tiles, the next one's first loads under the present one's epilogue,
+  // gained 2 % with the barest epilogue and lost 1-8 % with the real ones, whose
+  // values then no longer fit the registers.)
+  template <bool ALIGNED>
+  __device__ static void run(const Place &p, char *lds, Acc (&acc)[TX][TY]) {
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wx = wave % WX, wy = wave / WX;
@@ -172,7 +170,11 @@ struct Tile {
     const int key = (m >> 1) & 7;
     const int atx = (wx * (BX / WX) + (m / 4) * 4 * TX + m % 4) * STEP;
     const int aty = (BX + wy * (BY / WY) + m) * STEP;
-    Acc acc[TX][TY];
+#pragma unroll
+    for (int i = 0; i < TX; ++i)
+#pragma unroll
+      for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+    if (p.k0 >= p.k1) return;
     // Half s of a stage to registers; of a step's last bytes only `left` count.
     auto read = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], int left, auto tail) {
       const int c = ((s * 4 + g) ^ key) * FRAG;
@@ -223,15 +225,19 @@ struct Tile {
       return ((lane % 8) ^ (i < LX ? key_x(r) : key_y(r))) * FRAG;
     };
     // rows past the last are the last again
-    auto row_in = [&](const Place &p, int i) {
+    auto row_in = [&](int i) {
       const int64_t left = (i < LX ? p.X.rows - p.x0 : p.Y.rows - p.y0) - 1;
       const int r = row_of(i);
       return r < left ? r : (int)left;
     };
     if constexpr (ALIGNED) {
       const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-      v4i bx, by;
-      int at[LOADS], k, end, left;
+      const v4i bx = buffer_at(p.X.p + p.x0 * p.X.ld), by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
+      int at[LOADS], k = (int)p.k0;
+      const int end = (int)p.k1, left = (end - k - 1) % STEP + 1;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        at[i] = row_in(i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
       auto load = [&](int k, int stage) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
@@ -248,92 +254,64 @@ struct Tile {
                         base + stage + (i * WAVES + wave) * 1024);
         }
       };
-      auto begin = [&](const Place &p) {
-        bx = buffer_at(p.X.p + p.x0 * p.X.ld);
-        by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          at[i] = row_in(p, i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
-        k = (int)p.k0;
-        end = (int)p.k1;
-        left = (end - k - 1) % STEP + 1;
-        load_any(k, 0);
-        load_any(k + STEP, STAGE);
-      };
-      begin(where(first));
-      for (unsigned t = first; t < count; t += stride) {
-#pragma unroll
-        for (int i = 0; i < TX; ++i)
-#pragma unroll
-          for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
-        int b = 0;
+      load_any(k, 0);
+      load_any(k + STEP, STAGE);
+      int b = 0;
+      barrier_loaded();
+      // Both halves of a step in registers, one ahead: the second half's reads go
+      // with the first's products, then, the next step's loads having landed, the
+      // next first half's with the second's.
+      if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
+      for (; k + 3 * STEP <= end; k += STEP, b = STAGE - b) {
+        half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
         barrier_loaded();
-        // Both halves of a step in registers, one ahead: the second half's reads go
-        // with the first's products, then, the next step's loads having landed, the
-        // next first half's with the second's.
-        if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
-        for (; k + 3 * STEP <= end; k += STEP, b = STAGE - b) {
-          half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
-          barrier_loaded();
-          half(lds + (STAGE - b), 0, x0f, y0f, x1f, y1f, [&](int i) {
-            load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP,
-                        base + b + (i * WAVES + wave) * 1024);
-          });
-        }
-        // at most two more whole steps and a part of one
-        for (; k + STEP <= end; k += STEP, b = STAGE - b) {
-          read(lds + b, 1, x1f, y1f, STEP, whole);
-          multiply(x0f, y0f);
-          barrier_loaded();
-          load_any(k + 2 * STEP, b);
-          if (k + 2 * STEP <= end) read(lds + (STAGE - b), 0, x0f, y0f, STEP, whole);
-          multiply(x1f, y1f);
-        }
-        if (k < end) {
+        half(lds + (STAGE - b), 0, x0f, y0f, x1f, y1f, [&](int i) {
+          load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP,
+                      base + b + (i * WAVES + wave) * 1024);
+        });
+      }
+      // at most two more whole steps and a part of one
+      for (; k + STEP <= end; k += STEP, b = STAGE - b) {
+        read(lds + b, 1, x1f, y1f, STEP, whole);
+        multiply(x0f, y0f);
+        barrier_loaded();
+        load_any(k + 2 * STEP, b);
+        if (k + 2 * STEP <= end) read(lds + (STAGE - b), 0, x0f, y0f, STEP, whole);
+        multiply(x1f, y1f);
+      }
+      if (k < end) {
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            read(lds + b, s, x0f, y0f, left, std::true_type{});
-            multiply(x0f, y0f);
-          }
+        for (int s = 0; s < 2; ++s) {
+          read(lds + b, s, x0f, y0f, left, std::true_type{});
+          multiply(x0f, y0f);
         }
-        barrier_loaded();  // (nothing is read from the stages any more)
-        if (t + stride < count) begin(where(t + stride));
-        done(t, acc);
       }
     } else {
-      for (unsigned t = first; t < count; t += stride) {
-        const Place p = where(t);
-        v4i ahead[LOADS];
-        auto fetch = [&](int64_t k) {
+      v4i ahead[LOADS];
+      auto fetch = [&](int64_t k) {
 #pragma unroll
-          for (int i = 0; i < LOADS; ++i) {
-            const char *src = i < LX ? p.X.p + (p.x0 + row_in(p, i)) * p.X.ld
-                                     : p.Y.p + (p.y0 + row_in(p, i)) * p.Y.ld;
-            if (k + STEP <= p.k1) __builtin_memcpy(&ahead[i], src + k + chunk_of(i), FRAG);
-            else ahead[i] = load_frag(src, k + chunk_of(i), p.k1);
-          }
-        };
-#pragma unroll
-        for (int i = 0; i < TX; ++i)
-#pragma unroll
-          for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
-        int b = 0;
-        if (p.k0 < p.k1) fetch(p.k0);
-        for (int64_t k = p.k0; k < p.k1; k += STEP, b = STAGE - b) {
-#pragma unroll
-          for (int i = 0; i < LOADS; ++i)
-            *(v4i *)(lds + b + (i * WAVES + wave) * 1024 + lane * FRAG) = ahead[i];
-          __syncthreads();
-          if (k + STEP < p.k1) fetch(k + STEP);
-          read(lds + b, 0, x0f, y0f, STEP, whole);
-          multiply(x0f, y0f);
-          read(lds + b, 1, x0f, y0f, STEP, whole);
-          multiply(x0f, y0f);
+        for (int i = 0; i < LOADS; ++i) {
+          const char *src =
+              i < LX ? p.X.p + (p.x0 + row_in(i)) * p.X.ld : p.Y.p + (p.y0 + row_in(i)) * p.Y.ld;
+          if (k + STEP <= p.k1) __builtin_memcpy(&ahead[i], src + k + chunk_of(i), FRAG);
+          else ahead[i] = load_frag(src, k + chunk_of(i), p.k1);
         }
+      };
+      int b = 0;
+      fetch(p.k0);
+      for (int64_t k = p.k0; k < p.k1; k += STEP, b = STAGE - b) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          *(v4i *)(lds + b + (i * WAVES + wave) * 1024 + lane * FRAG) = ahead[i];
         __syncthreads();
-        done(t, acc);
+        if (k + STEP < p.k1) fetch(k + STEP);
+        read(lds + b, 0, x0f, y0f, STEP, whole);
+        multiply(x0f, y0f);
+        read(lds + b, 1, x0f, y0f, STEP, whole);
+        multiply(x0f, y0f);
       }
     }
+    __syncthreads();
   }
 
   // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r and
@@ -443,7 +421,18 @@ struct Thin {
   }
 };
 
-// n consecutive values at p, of which the first `left` are written.
+// N consecutive values at p, of which the first `left` are there (zeros after).
+template <int N>
+__device__ inline void load_run(const float *p, int64_t left, float (&f)[N]) {
+  if (left >= N) {
+    __builtin_memcpy(f, p, sizeof f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = i < left ? p[i] : 0.f;
+  }
+}
+
+// N consecutive values at p, of which the first `left` are written.
 template <class T, int N>
 __device__ inline void store_run(T *p, int64_t left, const float (&f)[N]) {
   T v[N];

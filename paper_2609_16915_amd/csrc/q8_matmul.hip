@@ -36,58 +36,42 @@ __global__ void __launch_bounds__(64 * WX *WY) k_q8_tile(Q8Args a, int splits, i
   using Tl = Tile<int8_t, BX, BY, WX, WY>;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.n + BX - 1) / BX), gy = (unsigned)((a.m + BY - 1) / BY);
-  const unsigned count = gx * gy * splits;
-  auto where = [&](unsigned t) {
-    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
-    unsigned tx, ty;
-    band_tile(b % (gx * gy), gx, gy, tx, ty);
-    const int64_t k0 = (int64_t)split * run, k1 = k0 + run < (int64_t)a.k ? k0 + run : (int64_t)a.k;
-    return typename Tl::Place{{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k},
-                              {(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k},
-                              (int64_t)tx * BX, (int64_t)ty * BY, k0, k1};
-  };
-  auto done = [&](unsigned t, v4i(&acc)[Tl::TX][Tl::TY]) {
-    const unsigned b = xcd_block(t, count), split = b / (gx * gy);
-    unsigned tx, ty;
-    band_tile(b % (gx * gy), gx, gy, tx, ty);
-    const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
-    if (splits > 1) {
-      const int64_t ld = ((int64_t)a.n + 3) / 4 * 4;
-#pragma unroll
-      for (int j = 0; j < Tl::TY; ++j) {
-        const int64_t y = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-        if (y >= (int64_t)a.m) continue;
-#pragma unroll
-        for (int i = 0; i < Tl::TX; ++i)
-          if (x0 + 4 * i < ld) *(v4i *)part_at(a, ld, split, y, x0 + 4 * i) = acc[i][j];
-      }
-      return;
-    }
-    float bs[Tl::TX][4], bias[Tl::TX][4];
-#pragma unroll
-    for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t x = x0 + 4 * i + r;
-        bs[i][r] = x < (int64_t)a.n ? a.b_scale[x] : 0.f;
-        bias[i][r] = a.bias && x < (int64_t)a.n ? a.bias[x] : 0.f;
-      }
+  const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
+  unsigned tx, ty;
+  band_tile(b % (gx * gy), gx, gy, tx, ty);
+  const int64_t k0 = (int64_t)split * run, k1 = k0 + run < (int64_t)a.k ? k0 + run : (int64_t)a.k;
+  v4i acc[Tl::TX][Tl::TY];
+  Tl::template run<ALIGNED>({{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k},
+                             {(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k},
+                             (int64_t)tx * BX, (int64_t)ty * BY, k0, k1},
+                            lds, acc);
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), y0 = (int64_t)ty * BY + Tl::y_at();
+  if (splits > 1) {
+    const int64_t ld = ((int64_t)a.n + 3) / 4 * 4;
 #pragma unroll
     for (int j = 0; j < Tl::TY; ++j) {
-      const int64_t y = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-      if (y >= (int64_t)a.m) continue;
-      const float as = a.a_scale[y];
-      O *out = (O *)a.out + y * (int64_t)a.out_stride;
-      float f[4 * Tl::TX];
+      if (y0 + 16 * j >= (int64_t)a.m) continue;
 #pragma unroll
       for (int i = 0; i < Tl::TX; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          f[4 * i + r] = (float)acc[i][j][r] * as * bs[i][r] + bias[i][r];
-      if (x0 < (int64_t)a.n) store_run(out + x0, (int64_t)a.n - x0, f);
+        if (x0 + 4 * i < ld) *(v4i *)part_at(a, ld, split, y0 + 16 * j, x0 + 4 * i) = acc[i][j];
     }
-  };
-  Tl::template each<ALIGNED>(blockIdx.x, gridDim.x, count, lds, where, done);
+    return;
+  }
+  const int64_t left = (int64_t)a.n - x0;
+  if (left <= 0) return;
+  float bs[4 * Tl::TX], bias[4 * Tl::TX] = {};
+  load_run(a.b_scale + x0, left, bs);
+  if (a.bias) load_run(a.bias + x0, left, bias);
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t y = y0 + 16 * j;
+    if (y >= (int64_t)a.m) continue;
+    const float as = a.a_scale[y];
+    float f[4 * Tl::TX];
+#pragma unroll
+    for (int i = 0; i < 4 * Tl::TX; ++i) f[i] = (float)acc[i / 4][j][i % 4] * as * bs[i] + bias[i];
+    store_run((O *)a.out + y * (int64_t)a.out_stride + x0, left, f);
+  }
 }
 
 template <class O, int NX, int NY, int WAVES>
@@ -163,13 +147,12 @@ Plan plan(size_t m, size_t n, size_t k) {
 }
 
 template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
-hipError_t tile(const Q8Args &a, const Plan &p, bool one_each, hipStream_t st) {
+hipError_t tile(const Q8Args &a, const Plan &p, hipStream_t st) {
   using Tl = Tile<int8_t, BX, BY, WX, WY>;
   auto k = k_q8_tile<O, ALIGNED, BX, BY, WX, WY>;
   const hipError_t e = allow_lds(k, Tl::LDS);
   if (e != hipSuccess) return e;
-  const size_t count = tiles(a.n, BX) * tiles(a.m, BY) * p.splits, cus = (size_t)device_cus();
-  hipLaunchKernelGGL(k, dim3((unsigned)(one_each || !cus ? count : std::min(count, cus))),
+  hipLaunchKernelGGL(k, dim3((unsigned)(tiles(a.n, BX) * tiles(a.m, BY) * p.splits)),
                      dim3(Tl::THREADS), Tl::LDS, st, a, p.splits, p.run);
   return hipGetLastError();
 }
@@ -209,12 +192,12 @@ hipError_t launch(const Q8Args &a, hipStream_t st) {
       }
       break;
     case Cut::SMALL:
-      e = al ? tile<O, true, 128, 128, 4, 2>(a, p, true, st)
-             : tile<O, false, 128, 128, 4, 2>(a, p, true, st);
+      e = al ? tile<O, true, 128, 128, 4, 2>(a, p, st)
+             : tile<O, false, 128, 128, 4, 2>(a, p, st);
       break;
     case Cut::LARGE:
-      e = al ? tile<O, true, 256, 256, 4, 2>(a, p, false, st)
-             : tile<O, false, 256, 256, 4, 2>(a, p, false, st);
+      e = al ? tile<O, true, 256, 256, 4, 2>(a, p, st)
+             : tile<O, false, 256, 256, 4, 2>(a, p, st);
       break;
   }
   if (e != hipSuccess || p.splits == 1) return e;
