@@ -80,11 +80,17 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
         for (int j = 0; j < Tl::TY; ++j) acc[i / 4][j][i % 4] = -INFINITY;
       }
   }
+  int64_t target[Tl::TY];
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    target[j] = row < (int64_t)a.rows ? a.targets[row] : -1;
+  }
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int y = Tl::y_at() + 16 * j;
     const int64_t row = (int64_t)ty * BY + y;
-    const int64_t at = row < (int64_t)a.rows ? a.targets[row] - x0 : -1;
+    const int64_t at = target[j] < 0 ? -1 : target[j] - x0;
     if (at >= 0 && at < RUN && x0 + at < (int64_t)a.vocab) {
 #pragma unroll
       for (int i = 0; i < RUN; ++i)
@@ -223,12 +229,23 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
   const int64_t left = (int64_t)a.vocab - (int64_t)v0 - x0;  // words of the run that exist
   const int lane = threadIdx.x % 64, g = lane / 16;
   T *mine = (T *)lds + threadIdx.x / 64 * (HX * HY);  // [x][y], runs of 16 y moved about
+  // (all that is read, before anything is written)
+  float coefs[Tl::TY], lses[Tl::TY];
+  int64_t target[Tl::TY];
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
     const bool in = row < (int64_t)a.rows;
-    const float c = in ? coef[row] : 0.f, lse = in ? a.lse[row] * LOG2E : 0.f;
-    const int64_t at = in ? a.targets[row] - (int64_t)v0 - x0 : -1;
+    coefs[j] = in ? coef[row] : 0.f;
+    lses[j] = in ? a.lse[row] * LOG2E : 0.f;
+    target[j] = in ? a.targets[row] : -1;
+  }
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) {
+    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
+    const bool in = row < (int64_t)a.rows;
+    const float c = coefs[j], lse = lses[j];
+    const int64_t at = target[j] < 0 ? -1 : target[j] - (int64_t)v0 - x0;
     T f[RUN];
     // (c = 0: a row that takes no part, whatever its logits are)
 #pragma unroll
@@ -340,7 +357,7 @@ k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restr
     if (add) load_run(out, left, f);
 #pragma unroll
     for (int i = 0; i < RUN; ++i) f[i] += acc[i / 4][j][i % 4];
-    store_run(out, left, f);
+    store_run<false>(out, left, f);
   }
 }
 
@@ -348,13 +365,22 @@ template <class T>
 __global__ void __launch_bounds__(256)
 k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t dim,
                const float *__restrict__ coef, T *__restrict__ out, size_t out_stride) {
-  const size_t c = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= dim) return;
-  for (size_t row = blockIdx.y; row < rows; row += gridDim.y) {
-    float s = 0.f;
-    for (int q = 0; q < splits; ++q) s += part[((size_t)q * rows + row) * dim + c];
-    out[row * out_stride + c] = (T)(s * coef[rows]);
+  const size_t quads = (dim + 3) / 4, i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads * rows) return;
+  const size_t row = i / quads, c = i % quads * 4;
+  const int64_t left = (int64_t)(dim - c);
+  float s[4] = {};
+#pragma unroll 4
+  for (int q = 0; q < splits; ++q) {
+    float f[4];
+    load_run(part + ((size_t)q * rows + row) * dim + c, left, f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += f[e];
   }
+  const float back = coef[rows];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] *= back;
+  store_run<false>(out + row * out_stride + c, left, s);
 }
 
 // gw rows [v0, v0 + here) = gl_t [here][ld_t] times h_t [dim][ld_t]
@@ -384,7 +410,7 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__r
     float f[RUN];
 #pragma unroll
     for (int i = 0; i < RUN; ++i) f[i] = acc[i / 4][j][i % 4] * back;
-    store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f);
+    store_run<true>((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f);
   }
 }
 
@@ -392,9 +418,18 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__r
 // rows of h as it takes (bound by w's bytes either way; 33 rows: see thin_rows).
 constexpr size_t THIN_ROWS = 32;
 constexpr size_t thin_x(size_t rows) { return rows <= 16 ? 64 : 32; }
-bool large(size_t rows, size_t dim) { return rows > 128 && dim > 128; }
-size_t forward_x(size_t rows, size_t dim) {
-  return rows <= THIN_ROWS ? thin_x(rows) : large(rows, dim) ? Large::BX : Small::BX;
+// Whether large tiles take the logits: one a CU at half the cost, small ones two,
+// whose ends overlap; in steps of a large tile (777 rows of 768 over 50257: 421 us
+// in all with small ones, 454 with large; 4096 of 4096 over 128000: 62 and 44 ms
+// by this count).
+bool large(size_t rows, size_t dim, size_t vocab) {
+  const double steps = (double)tiles(2 * dim, STEP);
+  const double l = (double)tiles(tiles(rows, 256) * tiles(vocab, 256), 256) * (steps + 4);
+  const double s = 0.66 * ((double)(tiles(rows, 128) * tiles(vocab, 128)) / 512 + 0.5) * (steps + 2);
+  return l <= s;
+}
+size_t forward_x(size_t rows, size_t dim, size_t vocab) {
+  return rows <= THIN_ROWS ? thin_x(rows) : large(rows, dim, vocab) ? Large::BX : Small::BX;
 }
 
 // Pieces of the vocabulary and what the workspace holds.
@@ -406,7 +441,7 @@ struct Plan {
 template <class S>
 Plan plan(size_t rows, size_t dim, size_t vocab) {
   constexpr size_t BX = S::BX, BY = S::BY;
-  constexpr size_t BUDGET = (size_t)512 << 20;
+  constexpr size_t BUDGET = (size_t)1 << 30;
   Plan p{};
   p.ld_t = up(rows, 64);
   const size_t column = 2 * (rows + p.ld_t + dim);
@@ -459,7 +494,7 @@ bool aligned(const LossArgs &a) {
 
 template <class T>
 hipError_t forward(const LossArgs &a, hipStream_t st) {
-  const size_t nx = tiles(a.vocab, forward_x(a.rows, a.dim));
+  const size_t nx = tiles(a.vocab, forward_x(a.rows, a.dim, a.vocab));
   Stat *part = (Stat *)a.workspace;
   float *at_target = (float *)(part + nx * a.rows);
   hipError_t e = hipSuccess;
@@ -471,7 +506,7 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
   };
   if (a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
   else if (a.rows <= 32) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
-  else if (large(a.rows, a.dim)) tile(Large{});
+  else if (large(a.rows, a.dim, a.vocab)) tile(Large{});
   else tile(Small{});
   LAUNCH(k_loss_join, dim3((unsigned)tiles(a.rows, 16)), 1024, 0, a, part, nx, at_target);
   return e;
@@ -506,26 +541,25 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
              Tl::LDS, a, v0, here, p.ld_t, coef, gl_t, h_t);
   }
   if (a.gh)
-    LAUNCH(k_loss_gh_join<T>,
-           dim3((unsigned)tiles(a.dim, 256), (unsigned)(a.rows < 32768 ? a.rows : 32768)), 256, 0,
-           part, (int)p.splits, a.rows, a.dim, coef, (T *)a.gh, a.gh_stride);
+    LAUNCH(k_loss_gh_join<T>, dim3((unsigned)tiles(tiles(a.dim, 4) * a.rows, 256)), 256, 0, part,
+           (int)p.splits, a.rows, a.dim, coef, (T *)a.gh, a.gh_stride);
   return e;
 }
 
 }  // namespace
 
 size_t cross_entropy_workspace(size_t rows, size_t dim, size_t vocab) {
-  return up(tiles(vocab, forward_x(rows, dim)) * rows * sizeof(Stat) + rows * 4, 16);
+  return up(tiles(vocab, forward_x(rows, dim, vocab)) * rows * sizeof(Stat) + rows * 4, 16);
 }
 size_t cross_entropy_backward_workspace(size_t rows, size_t dim, size_t vocab) {
-  return (large(rows, dim) ? plan<Large>(rows, dim, vocab) : plan<Small>(rows, dim, vocab)).bytes;
+  return (large(rows, dim, vocab) ? plan<Large>(rows, dim, vocab) : plan<Small>(rows, dim, vocab)).bytes;
 }
 
 hipError_t launch_cross_entropy(const LossArgs &a, hipStream_t st) {
   return a.dtype == ROSETTA_BF16 ? forward<bf16>(a, st) : forward<f16>(a, st);
 }
 hipError_t launch_cross_entropy_backward(const LossArgs &a, hipStream_t st) {
-  if (large(a.rows, a.dim))
+  if (large(a.rows, a.dim, a.vocab))
     return a.dtype == ROSETTA_BF16 ? backward<bf16, Large>(a, st) : backward<f16, Large>(a, st);
   return a.dtype == ROSETTA_BF16 ? backward<bf16, Small>(a, st) : backward<f16, Small>(a, st);
 }

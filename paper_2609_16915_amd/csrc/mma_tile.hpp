@@ -432,14 +432,26 @@ __device__ inline void load_run(const float *p, int64_t left, float (&f)[N]) {
   }
 }
 
-// N consecutive values at p, of which the first `left` are written.
-template <class T, int N>
+// N consecutive values at p, of which the first `left` are written.  LAST: nobody
+// reads them here again, so they need not stay in the caches (235 MB of a product's
+// outputs, 8192 x 14336: 394 us for 418).
+template <bool LAST, class T, int N>
 __device__ inline void store_run(T *p, int64_t left, const float (&f)[N]) {
   T v[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = (T)f[i];
   if (left >= N) {
-    __builtin_memcpy(p, v, sizeof v);
+    if constexpr (LAST && sizeof v % 16 == 0) {
+      using v4u = __attribute__((ext_vector_type(4), aligned(2))) int;
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof v / 16); ++i) {
+        v4u w;
+        __builtin_memcpy(&w, (const char *)v + 16 * i, 16);
+        __builtin_nontemporal_store(w, (v4u *)p + i);
+      }
+    } else {
+      __builtin_memcpy(p, v, sizeof v);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)

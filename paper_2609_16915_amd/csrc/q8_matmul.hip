@@ -22,7 +22,7 @@ __device__ inline void put4(const Q8Args &a, int64_t y, int64_t x, v4i s) {
     const int64_t c = x + r < (int64_t)a.n ? x + r : (int64_t)a.n - 1;
     f[r] = (float)s[r] * as * a.b_scale[c] + (a.bias ? a.bias[c] : 0.f);
   }
-  store_run((O *)a.out + y * (int64_t)a.out_stride + x, (int64_t)a.n - x, f);
+  store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x, (int64_t)a.n - x, f);
 }
 
 // Part `split` of the sums, rows of n rounded up to 4.
@@ -59,18 +59,22 @@ __global__ void __launch_bounds__(64 * WX *WY) k_q8_tile(Q8Args a, int splits, i
   }
   const int64_t left = (int64_t)a.n - x0;
   if (left <= 0) return;
-  float bs[4 * Tl::TX], bias[4 * Tl::TX] = {};
+  // (all that is read, before anything is written: in between, every row would
+  // wait for its own scale)
+  float bs[4 * Tl::TX], bias[4 * Tl::TX] = {}, as[Tl::TY];
   load_run(a.b_scale + x0, left, bs);
   if (a.bias) load_run(a.bias + x0, left, bias);
+#pragma unroll
+  for (int j = 0; j < Tl::TY; ++j) as[j] = y0 + 16 * j < (int64_t)a.m ? a.a_scale[y0 + 16 * j] : 0.f;
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t y = y0 + 16 * j;
     if (y >= (int64_t)a.m) continue;
-    const float as = a.a_scale[y];
     float f[4 * Tl::TX];
 #pragma unroll
-    for (int i = 0; i < 4 * Tl::TX; ++i) f[i] = (float)acc[i / 4][j][i % 4] * as * bs[i] + bias[i];
-    store_run((O *)a.out + y * (int64_t)a.out_stride + x0, left, f);
+    for (int i = 0; i < 4 * Tl::TX; ++i)
+      f[i] = (float)acc[i / 4][j][i % 4] * as[j] * bs[i] + bias[i];
+    store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x0, left, f);
   }
 }
 
