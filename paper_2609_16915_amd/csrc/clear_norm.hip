@@ -540,8 +540,12 @@ k_sum_partial(const float *__restrict__ partial, size_t groups, size_t dim,
 }
 
 template <class T, class W, bool WHOLE>
-hipError_t back_by_size(const NormBackArgs &a, hipStream_t st) {
-  const size_t groups = norm_back_groups(a.rows);
+hipError_t back_by_size(const NormBackArgs &args, hipStream_t st) {
+  NormBackArgs a = args;
+  // four rows to a group at least: the joining reads as much as a row per group.
+  // One group alone writes the sums themselves.
+  const size_t groups = std::min(norm_back_groups(a.rows), (a.rows + 3) / 4);
+  if (groups == 1) a.partial = a.gweight;
   auto go = [&](auto kernel, int tpr) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(tpr), 0, st, a);
     return hipGetLastError();
@@ -554,7 +558,7 @@ hipError_t back_by_size(const NormBackArgs &a, hipStream_t st) {
   else if (d <= 512 * VEC * 2) e = go(k_rms_norm_backward<T, W, 512, 2, WHOLE>, 512);
   else if (d <= 512 * VEC * 4) e = go(k_rms_norm_backward<T, W, 512, 4, WHOLE>, 512);
   else e = go(k_rms_norm_backward<T, W, 1024, 0, WHOLE>, 1024);
-  if (e != hipSuccess || !a.gweight) return e;
+  if (e != hipSuccess || !a.gweight || groups == 1) return e;
   hipLaunchKernelGGL(k_sum_partial, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, st, a.partial,
                      groups, d, a.gweight);
   return hipGetLastError();

@@ -160,20 +160,33 @@ k_loss_thin(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
   }
 }
 
-// The tiles' parts of 16 rows joined, 64 threads to a row.
+// The tiles' parts joined, R rows to a block of 1024 threads.
+template <int R>
 __global__ void __launch_bounds__(1024)
 k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
             const float *__restrict__ at_target) {
-  __shared__ Stat lds[64][16];
-  const int r = threadIdx.x % 16, p = threadIdx.x / 16;
-  const size_t row = (size_t)blockIdx.x * 16 + r;
+  constexpr int P = 1024 / R, AHEAD = 8;
+  __shared__ Stat lds[P][R];
+  const int r = threadIdx.x % R, p = threadIdx.x / R;
+  const size_t row = (size_t)blockIdx.x * R + r;
   Stat s{-INFINITY, 0.f};
-  if (row < a.rows)
-    for (size_t t = p; t < nt; t += 64) s = join(s, part[t * a.rows + row]);
+  if (row < a.rows) {
+    for (size_t t = p; t < nt; t += P * AHEAD) {
+      Stat f[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        f[i] = t + i * P < nt ? part[(t + i * P) * a.rows + row] : Stat{-INFINITY, 0.f};
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) s = join(s, f[i]);
+    }
+  }
   lds[p][r] = s;
-  __syncthreads();
+#pragma unroll
+  for (int h = P / 2; h >= 1; h /= 2) {
+    __syncthreads();
+    if (p < h) lds[p][r] = s = join(s, lds[p + h][r]);
+  }
   if (p == 0 && row < a.rows) {
-    for (int q = 1; q < 64; ++q) s = join(s, lds[q][r]);
     const float lse = s.top + logf(s.sum);
     a.lse[row] = lse;
     const int64_t target = a.targets[row];
@@ -189,17 +202,17 @@ k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
 // weigh the same (rounding gloss itself put one error on all of them: gradients
 // off by 0.0026 of their norm, 0.0017 so), and f16 has room for probabilities
 // down to 2^-28.
-__global__ void __launch_bounds__(1024) k_loss_coef(LossArgs a, float *__restrict__ coef) {
-  __shared__ float lds[16];
+__device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
+  const int threads = blockDim.x;
   float top = 0.f;
-  for (size_t t = threadIdx.x; t < a.rows; t += 1024)
+  for (size_t t = threadIdx.x; t < a.rows; t += threads)
     if (counts(a.targets[t], a.ignore_index, a.vocab)) top = fmaxf(top, fabsf(a.gloss[t]));
   for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = top;
   __syncthreads();
-  for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
+  for (int w = 0; w < threads / 64; ++w) top = fmaxf(top, lds[w]);
   const bool some = top > 0.f;
-  for (size_t t = threadIdx.x; t < a.rows; t += 1024) {
+  for (size_t t = threadIdx.x; t < a.rows; t += threads) {
     const float g = counts(a.targets[t], a.ignore_index, a.vocab) ? a.gloss[t] : 0.f;
     coef[t] = some ? g / top * GL_UP : g;
   }
@@ -289,20 +302,19 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
   }
 }
 
-// out [cols][ld] = in [rows][cols] the other way round, zeros in columns
-// [rows, ld); ld a multiple of 8.
-template <class T>
-__global__ void __launch_bounds__(256)
-k_transpose(const T *__restrict__ in, size_t in_stride, size_t rows, size_t cols,
-            T *__restrict__ out, size_t ld) {
-  __shared__ T lds[64][72];
-  const size_t r0 = (size_t)blockIdx.x * 64, c0 = (size_t)blockIdx.y * 64;
+// Tile (bx, by) of out [cols][ld] = in [rows][cols] the other way round, zeros in
+// columns [rows, ld) and for rows that are not `wanted`; ld a multiple of 8; 256
+// threads.
+template <class T, class Wanted>
+__device__ inline void transpose(const T *in, size_t in_stride, size_t rows, size_t cols, T *out,
+                                 size_t ld, size_t bx, size_t by, T (*lds)[72], Wanted wanted) {
+  const size_t r0 = bx * 64, c0 = by * 64;
   const int l = threadIdx.x % 8 * 8;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int i = threadIdx.x / 8 + 32 * h;
     T v[8] = {};
-    if (r0 + i < rows) {
+    if (r0 + i < rows && wanted(r0 + i)) {
       const T *src = in + (r0 + i) * in_stride + c0 + l;
       if (c0 + l + 8 <= cols) {
         __builtin_memcpy(v, src, sizeof v);
@@ -323,6 +335,32 @@ k_transpose(const T *__restrict__ in, size_t in_stride, size_t rows, size_t cols
     for (int e = 0; e < 8; ++e) v[e] = lds[l + e][i];
     if (c0 + i < cols && r0 + l < ld) *(v4i *)(out + (c0 + i) * ld + r0 + l) = *(const v4i *)v;
   }
+}
+
+// w_t of a piece of the vocabulary.
+template <class T>
+__global__ void __launch_bounds__(256)
+k_loss_wt(const T *__restrict__ w, size_t w_stride, size_t here, size_t dim, T *__restrict__ w_t,
+          size_t vp) {
+  __shared__ T lds[64][72];
+  transpose(w, w_stride, here, dim, w_t, vp, blockIdx.x, blockIdx.y, lds,
+            [](size_t) { return true; });
+}
+
+// What comes before the pieces: the factors (block 0), and h_t in tiles (the
+// others; none where gw is not wanted).
+template <class T>
+__global__ void __launch_bounds__(256)
+k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t ld_t) {
+  __shared__ T lds[64][72];
+  if (blockIdx.x == 0) {
+    loss_coef(a, coef, (float *)lds);
+    return;
+  }
+  const size_t across = (ld_t + 63) / 64, b = blockIdx.x - 1;
+  // (a row that takes no part, whatever it holds, is zeros: NaN times 0 is NaN)
+  transpose((const T *)a.h, a.h_stride, a.rows, a.dim, h_t, ld_t, b % across, b / across, lds,
+            [&](size_t row) { return counts(a.targets[row], a.ignore_index, a.vocab); });
 }
 
 // part[split][row][d] (+)= gl [rows][vp] times w_t [dim][vp] over the piece's
@@ -414,9 +452,10 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__r
   }
 }
 
-// Rows of the vocabulary in a block of the forward pass; 0: Thin's, for as few
-// rows of h as it takes (bound by w's bytes either way; 33 rows: see thin_rows).
-constexpr size_t THIN_ROWS = 32;
+// Rows of h that Thin takes, bound by w's bytes like any other way, and w's rows in
+// its blocks.  Short rows (less than half a step for each of a block's waves)
+// would leave most of its waves idle.
+size_t thin_rows(size_t dim) { return 2 * dim >= 8 * STEP ? 32 : 0; }
 constexpr size_t thin_x(size_t rows) { return rows <= 16 ? 64 : 32; }
 // Whether large tiles take the logits: one a CU at half the cost, small ones two,
 // whose ends overlap; in steps of a large tile (777 rows of 768 over 50257: 421 us
@@ -429,7 +468,7 @@ bool large(size_t rows, size_t dim, size_t vocab) {
   return l <= s;
 }
 size_t forward_x(size_t rows, size_t dim, size_t vocab) {
-  return rows <= THIN_ROWS ? thin_x(rows) : large(rows, dim, vocab) ? Large::BX : Small::BX;
+  return rows <= thin_rows(dim) ? thin_x(rows) : large(rows, dim, vocab) ? Large::BX : Small::BX;
 }
 
 // Pieces of the vocabulary and what the workspace holds.
@@ -504,11 +543,14 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
     LAUNCH(k, dim3((unsigned)(nx * tiles(a.rows, S::BY))), S::THREADS,
            (TileOf<T, S>::LDS), a, part, at_target);
   };
-  if (a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
-  else if (a.rows <= 32) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
+  const bool thin = a.rows <= thin_rows(a.dim);
+  if (thin && a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
+  else if (thin) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
   else if (large(a.rows, a.dim, a.vocab)) tile(Large{});
   else tile(Small{});
-  LAUNCH(k_loss_join, dim3((unsigned)tiles(a.rows, 16)), 1024, 0, a, part, nx, at_target);
+  // (few rows: more threads to each)
+  if (a.rows <= 64) LAUNCH(k_loss_join<2>, dim3((unsigned)tiles(a.rows, 2)), 1024, 0, a, part, nx, at_target);
+  else LAUNCH(k_loss_join<16>, dim3((unsigned)tiles(a.rows, 16)), 1024, 0, a, part, nx, at_target);
   return e;
 }
 
@@ -522,17 +564,15 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   T *gl = a.gh ? (T *)(ws + p.gl) : nullptr, *gl_t = a.gw ? (T *)(ws + p.gl_t) : nullptr;
   T *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
   hipError_t e = hipSuccess;
-  LAUNCH(k_loss_coef, dim3(1), 1024, 0, a, coef);
-  if (a.gw)
-    LAUNCH(k_transpose<T>, dim3((unsigned)tiles(p.ld_t, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
-           (const T *)a.h, a.h_stride, a.rows, a.dim, h_t, p.ld_t);
+  LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(p.ld_t, 64) * tiles(a.dim, 64) : 0))),
+         256, 0, a, coef, h_t, p.ld_t);
   for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
     auto k = aligned(a) ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
     LAUNCH(k, dim3((unsigned)(tiles(here, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a, v0, here,
            p.vp, p.ld_t, coef, gl, gl_t);
     if (a.gh) {
-      LAUNCH(k_transpose<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
+      LAUNCH(k_loss_wt<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
              (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
       LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp, gl, w_t, part, p.run, i > 0);
     }

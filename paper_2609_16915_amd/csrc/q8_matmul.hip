@@ -122,14 +122,16 @@ Plan plan(size_t m, size_t n, size_t k) {
   const size_t cus = std::max(1, device_cus());
   Plan p{Cut::THIN, 1, 1, 1, 0};
   size_t most = 1;
-  if (m <= 16) {
-    // Few tokens: bound by the channels' bytes, so every CU needs channels to
-    // read, and the more a block has the less often the tokens are read.
+  // Few tokens: bound by the channels' bytes, so every CU needs channels to read,
+  // and the more a block has the less often the tokens are read.  (Rows of less
+  // than half a step for each of a block's waves leave most of them idle: tiles.)
+  const bool thin = k >= 8 * STEP;
+  if (thin && m <= 16) {
     p.nx = tiles(n, 64) >= cus ? 4 : tiles(n, 32) >= cus ? 2 : 1;
-  } else if (m <= 32) {
+  } else if (thin && m <= 32) {
     p.ny = 2;
     p.nx = tiles(n, 32) >= cus ? 2 : 1;
-  } else if (m <= 64) {
+  } else if (thin && m <= 64) {
     p.ny = m <= 48 ? 3 : 4;
     p.nx = 4;
     most = tiles(2 * cus, tiles(n, 64));

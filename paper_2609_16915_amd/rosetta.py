@@ -674,7 +674,7 @@ def _made(out, name: str, shape, dtype, like):
     """`out` checked, or a new tensor of that shape and type: (tensor, address,
     row stride)."""
     if out is None:
-        out = _torch().empty(shape, dtype=dtype, device=like.device)
+        out = like.new_empty(shape, dtype=dtype)
         return out, out.data_ptr(), shape[1]
     return out, *_mat(out, name, dtype, shape)[:2]
 
@@ -699,7 +699,7 @@ def _stream_of(t, stream) -> int:
 def _scratch(workspace, need: int, like):
     """`workspace` checked, or a new one: (address, bytes, tensor)."""
     if workspace is None:
-        workspace = _torch().empty(need, dtype=_torch().uint8, device=like.device)
+        workspace = like.new_empty(need, dtype=_torch().uint8)
     have = workspace.numel() * workspace.element_size()
     if have < need:
         raise ValueError(f"workspace holds {have} bytes, the call needs {need}")
@@ -744,9 +744,9 @@ def _norm(x, weight, eps, residual, h, y, want_y, q, want_q, stream):
         y, yp, ys = _made(y, "y", (rows, dim), dtype, x)
     if want_q:
         q, qp, qs = _made(q, "q", (rows, dim), torch.int8, x)
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        scale = x.new_empty(rows, dtype=torch.float32)
         sp = scale.data_ptr()
-    inv_rms = torch.empty(rows, dtype=torch.float32, device=x.device)
+    inv_rms = x.new_empty(rows, dtype=torch.float32)
     _check(lib().rosetta_rms_norm(xp, xs, rp, rs, wp, wt, code, rows, dim, eps, hp, hs, yp, ys, qp,
                                   qs, sp, inv_rms.data_ptr(), _stream_of(x, stream)))
     return q, scale, h, inv_rms, y
@@ -785,7 +785,7 @@ def rms_norm_backward(gy, h, weight, inv_rms, gh=None, gx=None, want_gweight: bo
     gx, xp, xs = _made(gx, "gx", (rows, dim), dtype, gy)
     gweight, gwp, wsp, wsb = None, None, None, 0
     if want_gweight:
-        gweight = torch.empty(dim, dtype=torch.float32, device=gy.device)
+        gweight = gy.new_empty(dim, dtype=torch.float32)
         gwp = gweight.data_ptr()
         wsp, wsb, workspace = _scratch(
             workspace, lib().rosetta_rms_norm_backward_workspace_bytes(rows, dim), gy)
@@ -858,7 +858,7 @@ def cross_entropy(h, w, targets, ignore_index: int = -100, workspace=None, strea
     if dw != dim:
         raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
     tp = _vec(targets, "targets", torch.int64, rows)
-    loss, lse = (torch.empty(rows, dtype=torch.float32, device=h.device) for _ in range(2))
+    loss, lse = (h.new_empty(rows, dtype=torch.float32) for _ in range(2))
     sp, sb, workspace = _scratch(
         workspace, lib().rosetta_cross_entropy_workspace_bytes(rows, dim, vocab), h)
     _check(lib().rosetta_cross_entropy(hp, hs, wp, ws, dt, tp, ignore_index, rows, dim, vocab,

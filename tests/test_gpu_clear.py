@@ -360,7 +360,7 @@ def test_cross_entropy_large_logits_and_uneven_factors(dtype):
 def test_cross_entropy_gradients_in_pieces(dtype, dim):
     """Enough rows that gl is held for a part of the vocabulary at a time, the last
     part shorter than the others by more than a tile."""
-    rows, vocab = 16384, 8300
+    rows, vocab = 16384, 17000
     one = R.lib().rosetta_cross_entropy_backward_workspace_bytes(rows, dim, vocab)
     assert one < 2 * 2 * rows * vocab  # (not all of gl, twice)
     g = torch.full((rows,), 1.0 / rows)
@@ -391,6 +391,29 @@ def test_cross_entropy_nan_stays_in_its_row():
     g = torch.full((rows,), 0.1, device="cuda")
     gh, gw = R.cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, g)
     assert not loss.cpu()[4] and not gh[4].any() and torch.isfinite(gh).all()
+
+
+@pytest.mark.parametrize("rows,dim,vocab", [(20, 64, 300), (500, 256, 4000)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_cross_entropy_rows_without_part_leave_no_trace(dtype, rows, dim, vocab):
+    """NaN and infinities in rows whose target does not count change no bit of any
+    other row's results, or of the weights' gradient."""
+    h, w = normal(110, rows, dim, dtype), normal(111, vocab, dim, dtype, 0.2)
+    t = targets(112, rows, vocab, rows // 3)
+    t[3], t[rows - 1] = -7, vocab + 1
+    out = (t < 0) | (t >= vocab)
+    g = torch.rand(rows, generator=gen(113)).cuda()
+    got = []
+    for fill in (0.0, float("nan"), float("inf")):
+        x = h.clone()
+        x[out] = fill
+        loss, lse = R.cross_entropy(x.cuda(), w.cuda(), t.cuda())
+        gh, gw = R.cross_entropy_backward(x.cuda(), w.cuda(), t.cuda(), lse, g)
+        assert not gh[out.cuda()].any()
+        got.append((loss[~out.cuda()], gh, gw))
+    for other in got[1:]:
+        for a, b in zip(other, got[0]):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
 
 
 def test_cross_entropy_gradient_against_differences():
