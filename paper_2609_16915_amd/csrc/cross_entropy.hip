@@ -363,39 +363,49 @@ k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t l
             [&](size_t row) { return counts(a.targets[row], a.ignore_index, a.vocab); });
 }
 
-// part[split][row][d] (+)= gl [rows][vp] times w_t [dim][vp] over the piece's
-// first `here`: split s takes an equal run of them, perhaps none of the last.
-template <class T, class S>
+// part[split][row][d] (+)= gl [rows][vp] times the piece's `here` rows of w: split s
+// takes an equal run of them, perhaps none of the last.  ACROSS: w as it lies;
+// else w_t [dim][vp].
+template <class T, class S, bool ACROSS>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restrict__ gl,
-               const T *__restrict__ w_t, float *__restrict__ part, size_t run, int add) {
-  using Tl = TileOf<T, S>;
-  constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
+               const T *__restrict__ w, size_t w_stride, float *__restrict__ part, size_t run,
+               int add) {
+  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, ACROSS>;
+  constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
   const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
   unsigned tx, ty;
   band_tile(b % (gx * gy), gx, gy, tx, ty);
-  // (whole 16 bytes: both have zeros there)
-  const int64_t ld = (int64_t)vp * sizeof(T), bytes = (int64_t)((here + 7) / 8 * 8) * sizeof(T);
+  // (not ACROSS: whole 16 bytes, gl and w_t have zeros there)
+  const int64_t ld = (int64_t)vp * sizeof(T);
+  const int64_t bytes = (int64_t)(ACROSS ? here : (here + 7) / 8 * 8) * sizeof(T);
   const int64_t k0 = (int64_t)(split * run * sizeof(T)), k1 = k0 + (int64_t)(run * sizeof(T));
+  const Operand X = ACROSS ? Operand{(const char *)w, (int64_t)(w_stride * sizeof(T)),
+                                     (int64_t)here, (int64_t)(dim * sizeof(T))}
+                           : Operand{(const char *)w, ld, (int64_t)dim, bytes};
   v4f acc[Tl::TX][Tl::TY];
-  Tl::template run<true>({{(const char *)w_t, ld, (int64_t)dim, bytes},
-                          {(const char *)gl, ld, (int64_t)rows, bytes},
-                          (int64_t)tx * BX, (int64_t)ty * BY, k0, k1 < bytes ? k1 : bytes},
+  Tl::template run<true>({X, {(const char *)gl, ld, (int64_t)rows, bytes}, (int64_t)tx * BX,
+                          (int64_t)ty * BY, k0, k1 < bytes ? k1 : bytes},
                          lds, acc);
-  const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)dim - x0;
-  if (left <= 0) return;
+  constexpr int RUN = ACROSS ? 4 : 4 * Tl::TX;  // neighbouring x of a lane
+  const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
     if (row >= (int64_t)rows) continue;
-    float *out = part + ((size_t)split * rows + row) * dim + x0;
-    float f[RUN] = {};
-    if (add) load_run(out, left, f);
 #pragma unroll
-    for (int i = 0; i < RUN; ++i) f[i] += acc[i / 4][j][i % 4];
-    store_run<false>(out, left, f);
+    for (int i = 0; i < 4 * Tl::TX / RUN; ++i) {
+      const int64_t x = x0 + 16 * i, left = (int64_t)dim - x;
+      if (left <= 0) continue;
+      float *out = part + ((size_t)split * rows + row) * dim + x;
+      float f[RUN] = {};
+      if (add) load_run(out, left, f);
+#pragma unroll
+      for (int e = 0; e < RUN; ++e) f[e] += acc[i + e / 4][j][e % 4];
+      store_run<false>(out, left, f);
+    }
   }
 }
 
@@ -563,18 +573,27 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   float *coef = (float *)(ws + p.coef), *part = (float *)(ws + p.part);
   T *gl = a.gh ? (T *)(ws + p.gl) : nullptr, *gl_t = a.gw ? (T *)(ws + p.gl_t) : nullptr;
   T *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
+  const bool al = aligned(a);
   hipError_t e = hipSuccess;
   LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(p.ld_t, 64) * tiles(a.dim, 64) : 0))),
          256, 0, a, coef, h_t, p.ld_t);
   for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
-    auto k = aligned(a) ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
+    auto k = al ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
     LAUNCH(k, dim3((unsigned)(tiles(here, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a, v0, here,
            p.vp, p.ld_t, coef, gl, gl_t);
     if (a.gh) {
-      LAUNCH(k_loss_wt<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0,
-             (const T *)a.w + v0 * a.w_stride, a.w_stride, here, a.dim, w_t, p.vp);
-      LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp, gl, w_t, part, p.run, i > 0);
+      const T *w = (const T *)a.w + v0 * a.w_stride;
+      const dim3 grid((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY)));
+      if (al) {
+        LAUNCH((k_loss_gh_tile<T, S, true>), grid, S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp,
+               gl, w, a.w_stride, part, p.run, i > 0);
+      } else {
+        LAUNCH(k_loss_wt<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0, w,
+               a.w_stride, here, a.dim, w_t, p.vp);
+        LAUNCH((k_loss_gh_tile<T, S, false>), grid, S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp,
+               gl, w_t, p.vp, part, p.run, i > 0);
+      }
     }
     if (a.gw)
       LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)(tiles(a.dim, BX) * tiles(here, BY))), S::THREADS,

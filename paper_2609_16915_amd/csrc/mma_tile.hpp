@@ -77,6 +77,12 @@ __device__ inline v4i buffer_at(const char *base) {
              __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), -1, 0x00027000};
 }
 
+// The same, `ahead` bytes on.
+__device__ inline v4i buffer_on(v4i buf, int64_t ahead) {
+  const uint64_t b = ((uint64_t)(uint32_t)buf.x | (uint64_t)(uint32_t)buf.y << 32) + ahead;
+  return v4i{(int)b, (int)(b >> 32), buf.z, buf.w};
+}
+
 // 16 bytes per lane from buf + at + k to LDS address `lds` + 16 lane.  Nothing
 // waits for it but barrier_loaded().
 __device__ inline void load_to_lds(v4i buf, int at, int k, unsigned lds) {
@@ -131,7 +137,16 @@ __device__ inline v4i load_frag(const char *row, int64_t at, int64_t end) {
 // m in its fragment, which spreads the 16 rows of a fragment over all banks.
 // Row 4 g + r of fragment i of a wave's X is its row g * 4 TX + 4 i + r, so that
 // a lane's accumulators are runs of 4 TX consecutive x.
-template <class T, int BX, int BY, int WX, int WY>
+//
+// ACROSS (16-bit types, ALIGNED only): X lies the other way, k rows of nx columns
+// (X.bytes the columns' bytes, x0 a column; k1 is exact, Y's rows go on to whole 16
+// bytes with zeros).  Its stage then
+// holds 64 such rows of BX columns; chunk c (32 bytes, a fragment's 16 columns) of
+// row k lies at place c ^ key, key = (k & 3) | (k >> 1 & 4), and a fragment's
+// lanes read it turned by 4 x 4 (ds_read_b64_tr_b16: lane l of 16 gives the address
+// of row l / 4, columns 4 (l % 4) .. + 4, and gets column l of the four rows).  A
+// lane's accumulators are then runs of 4 x only.
+template <class T, int BX, int BY, int WX, int WY, bool ACROSS = false>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
@@ -146,6 +161,7 @@ struct Tile {
     return (m >> 1) & 7;
   }
   __device__ static int key_y(int row) { return (row >> 1) & 7; }
+  __device__ static int key_k(int row) { return (row & 3) | (row >> 1 & 4); }
 
   // A tile: rows [x0, x0 + BX) of X and [y0, y0 + BY) of Y over bytes [k0, k1)
   // of the rows (k0 a multiple of 16; ALIGNED: k1 too).  x0 < X.rows and y0 <
@@ -175,11 +191,36 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     if (p.k0 >= p.k1) return;
+    // ACROSS: this lane's row and column quad in a 4 x 16 block of fragment i, half 0
+    static_assert(!ACROSS || (sizeof(T) == 2 && ALIGNED), "");
+    int across[TX];
+    if constexpr (ACROSS) {
+      const int row = 8 * g + m / 4;
+#pragma unroll
+      for (int i = 0; i < TX; ++i)
+        across[i] = row * 2 * BX + ((wx * TX + i) ^ key_k(row)) * 32 + m % 4 * 8;
+    }
+    auto read_x = [&](const char *stage, int s, int i) {
+      if constexpr (ACROSS) {
+        using v4s = __attribute__((ext_vector_type(4))) short;
+        using lds_v4s = __attribute__((address_space(3))) v4s;
+        struct {
+          v4s h[2];
+        } f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_v4s *)(stage + across[i] + (s * 32 + h * 4) * 2 * BX));
+        return __builtin_bit_cast(v4i, f);
+      } else {
+        return *(const v4i *)(stage + atx + i * 4 * STEP + ((s * 4 + g) ^ key) * FRAG);
+      }
+    };
     // Half s of a stage to registers; of a step's last bytes only `left` count.
     auto read = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], int left, auto tail) {
       const int c = ((s * 4 + g) ^ key) * FRAG;
 #pragma unroll
-      for (int i = 0; i < TX; ++i) x[i] = *(const v4i *)(stage + atx + i * 4 * STEP + c);
+      for (int i = 0; i < TX; ++i) x[i] = read_x(stage, s, i);
 #pragma unroll
       for (int j = 0; j < TY; ++j) y[j] = *(const v4i *)(stage + aty + j * 16 * STEP + c);
       if (tail.value && (s * 4 + g) * FRAG >= left) {
@@ -207,7 +248,7 @@ struct Tile {
         for (int i = j * LOADS / TY; i < (j + 1) * LOADS / TY; ++i) load(i);
 #pragma unroll
         for (int i = j * READS / TY; i < (j + 1) * READS / TY; ++i) {
-          if (i < TX) x[i] = *(const v4i *)(stage + atx + i * 4 * STEP + c);
+          if (i < TX) x[i] = read_x(stage, s, i);
           else y[i - TX] = *(const v4i *)(stage + aty + (i - TX) * 16 * STEP + c);
         }
 #pragma unroll
@@ -232,26 +273,42 @@ struct Tile {
     };
     if constexpr (ALIGNED) {
       const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-      const v4i bx = buffer_at(p.X.p + p.x0 * p.X.ld), by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
+      const v4i bx = buffer_at(p.X.p + p.x0 * (ACROSS ? (int64_t)sizeof(T) : p.X.ld));
+      const v4i by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
       int at[LOADS], k = (int)p.k0;
       const int end = (int)p.k1, left = (end - k - 1) % STEP + 1;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        at[i] = row_in(i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
-      auto load = [&](int k, int stage) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          load_to_lds(i < LX ? bx : by, at[i], k, base + stage + (i * WAVES + wave) * 1024);
+      // ACROSS: row of the step and byte of the row of this lane's load i of X;
+      // columns past the last are the first again
+      auto across_row = [&](int i) { return ((i * WAVES + wave) * 64 + lane) / (BX / 8); };
+      auto across_byte = [&](int i) {
+        const int piece = ((i * WAVES + wave) * 64 + lane) % (BX / 8);
+        const int byte = ((piece / 2) ^ key_k(across_row(i))) * 32 + piece % 2 * FRAG;
+        return p.x0 * (int64_t)sizeof(T) + byte + FRAG <= p.X.bytes ? byte : 0;
       };
-      // the last step may be part of one: chunks beyond it read its first again,
-      // and read() takes them as zeros
-      auto load_any = [&](int k, int stage) {
-        if (k + STEP <= end) load(k, stage);
-        else if (k < end) {
 #pragma unroll
-          for (int i = 0; i < LOADS; ++i)
-            load_to_lds(i < LX ? bx : by, at[i] - (chunk_of(i) < left ? 0 : chunk_of(i)), k,
-                        base + stage + (i * WAVES + wave) * 1024);
+      for (int i = 0; i < LOADS; ++i) {
+        if (ACROSS && i < LX) at[i] = across_row(i) * (int)p.X.ld + across_byte(i);
+        else at[i] = row_in(i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
+      }
+      auto load_one = [&](int i, int at, int k, int stage) {
+        const unsigned to = base + stage + (i * WAVES + wave) * 1024;
+        if (ACROSS && i < LX)
+          load_to_lds(buffer_on(bx, k / (int)sizeof(T) * p.X.ld), at, 0, to);
+        else load_to_lds(i < LX ? bx : by, at, k, to);
+      };
+      // the last step may be part of one: chunks (ACROSS: rows) beyond it read its
+      // first again, and read() takes them as zeros
+      auto load_any = [&](int k, int stage) {
+        if (k + STEP <= end) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i) load_one(i, at[i], k, stage);
+        } else if (k < end) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i) {
+            if (ACROSS && i < LX)
+              load_one(i, across_row(i) * (int)sizeof(T) < left ? at[i] : across_byte(i), k, stage);
+            else load_one(i, at[i] - (chunk_of(i) < left ? 0 : chunk_of(i)), k, stage);
+          }
         }
       };
       load_any(k, 0);
@@ -266,8 +323,7 @@ struct Tile {
         half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
         barrier_loaded();
         half(lds + (STAGE - b), 0, x0f, y0f, x1f, y1f, [&](int i) {
-          load_to_lds(i < LX ? bx : by, at[i], k + 2 * STEP,
-                      base + b + (i * WAVES + wave) * 1024);
+          load_one(i, at[i], k + 2 * STEP, b);
         });
       }
       // at most two more whole steps and a part of one
@@ -314,10 +370,10 @@ struct Tile {
     __syncthreads();
   }
 
-  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r and
-  // y_at() + 16 j
+  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r (ACROSS:
+  // + 16 i + r) and y_at() + 16 j
   __device__ static int x_at() {
-    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * 4 * TX;
+    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * (ACROSS ? 4 : 4 * TX);
   }
   __device__ static int y_at() {
     return (threadIdx.x / 64) / WX * (BY / WY) + threadIdx.x % 16;
