@@ -219,17 +219,14 @@ __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
 }
 
-// gl of the vocabulary rows [v0, v0 + here), `here` rounded up to whole tiles: as
-// gl [rows][vp] and as gl_t [vp][ld_t], zeros beyond the vocabulary and the rows.
-// gl_t goes through the stages, each wave's part on its own, so that its rows
-// leave in runs of the part's height.
+// gl [rows][vp] of the vocabulary rows [v0, v0 + here), `here` rounded up to whole
+// tiles, zeros beyond the vocabulary.
 template <class T, class S, bool ALIGNED>
 __global__ void __launch_bounds__(S::THREADS)
-k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
-                 const float *__restrict__ coef, T *__restrict__ gl, T *__restrict__ gl_t) {
+k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, const float *__restrict__ coef,
+                 T *__restrict__ gl) {
   using Tl = TileOf<T, S>;
-  constexpr int BX = S::BX, BY = S::BY;
-  constexpr int HX = 16 * Tl::TX, HY = 16 * Tl::TY, RUN = 4 * Tl::TX;  // a wave's part
+  constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((here + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
@@ -240,8 +237,6 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                             lds, acc);
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
   const int64_t left = (int64_t)a.vocab - (int64_t)v0 - x0;  // words of the run that exist
-  const int lane = threadIdx.x % 64, g = lane / 16;
-  T *mine = (T *)lds + threadIdx.x / 64 * (HX * HY);  // [x][y], runs of 16 y moved about
   // (all that is read, before anything is written)
   float coefs[Tl::TY], lses[Tl::TY];
   int64_t target[Tl::TY];
@@ -256,49 +251,27 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-    const bool in = row < (int64_t)a.rows;
+    if (row >= (int64_t)a.rows) continue;
     const float c = coefs[j], lse = lses[j];
     const int64_t at = target[j] < 0 ? -1 : target[j] - (int64_t)v0 - x0;
-    T f[RUN];
+    float f[RUN];
     // (c = 0: a row that takes no part, whatever its logits are)
 #pragma unroll
     for (int i = 0; i < RUN; ++i) {
       const float e = __builtin_amdgcn_exp2f(fmaf(acc[i / 4][j][i % 4], LOG2E, -lse));
-      acc[i / 4][j][i % 4] = c == 0.f ? 0.f : e * c;
+      f[i] = c == 0.f ? 0.f : e * c;
     }
     if (at >= 0 && at < RUN) {
 #pragma unroll
       for (int i = 0; i < RUN; ++i)
-        if (at == i) acc[i / 4][j][i % 4] -= c;
+        if (at == i) f[i] -= c;
     }
     if (left < RUN) {
 #pragma unroll
       for (int i = 0; i < RUN; ++i)
-        if (i >= left) acc[i / 4][j][i % 4] = 0.f;
+        if (i >= left) f[i] = 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < RUN; ++i) f[i] = (T)acc[i / 4][j][i % 4];
-    if (gl && in) __builtin_memcpy(gl + row * (int64_t)vp + x0, f, sizeof f);
-    // (the four lane groups of an x each to other banks)
-    if (gl_t) {
-      const int to = (j ^ (g & (Tl::TY - 1))) * 16 + lane % 16;
-#pragma unroll
-      for (int i = 0; i < RUN; ++i) mine[(g * RUN + i) * HY + to] = f[i];
-    }
-  }
-  if (!gl_t) return;
-  // (the wave's lanes read one another's words)
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  const int wx = threadIdx.x / 64 % S::WX, wy = threadIdx.x / 64 / S::WX;
-  const int64_t y0 = (int64_t)ty * BY + wy * HY;
-  T *out = gl_t + ((int64_t)tx * BX + wx * HX) * (int64_t)ld_t + y0;
-#pragma unroll
-  for (int i = 0; i < HX * HY / 512; ++i) {
-    const int x = (i * 64 + lane) / (HY / 8), y = (i * 64 + lane) % (HY / 8) * 8;
-    const int from = ((y / 16) ^ (x / RUN & (Tl::TY - 1))) * 16 + y % 16;
-    if (y0 + y < (int64_t)ld_t)
-      *(v4i *)(out + x * (int64_t)ld_t + y) = *(const v4i *)(mine + x * HY + from);
+    store_run<false>(gl + row * (int64_t)vp + x0, RUN, f);
   }
 }
 
@@ -431,22 +404,23 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
   store_run<false>(out + row * out_stride + c, left, s);
 }
 
-// gw rows [v0, v0 + here) = gl_t [here][ld_t] times h_t [dim][ld_t]
+// gw rows [v0, v0 + here) = gl [rows][vp] the other way, times h_t [dim][ld_t]
 template <class T, class S>
 __global__ void __launch_bounds__(S::THREADS)
-k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t ld_t, const float *__restrict__ coef,
-               const T *__restrict__ gl_t, const T *__restrict__ h_t) {
-  using Tl = TileOf<T, S>;
+k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
+               const float *__restrict__ coef, const T *__restrict__ gl,
+               const T *__restrict__ h_t) {
+  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, false, true>;
   constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)((here + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
-  const int64_t bytes = (int64_t)ld_t * sizeof(T);
+  const int64_t ld_h = (int64_t)(ld_t * sizeof(T)), ld_g = (int64_t)(vp * sizeof(T));
   v4f acc[Tl::TX][Tl::TY];
-  Tl::template run<true>({{(const char *)h_t, bytes, (int64_t)a.dim, bytes},
-                          {(const char *)gl_t, bytes, (int64_t)here, bytes},
-                          (int64_t)tx * BX, (int64_t)ty * BY, 0, bytes},
+  Tl::template run<true>({{(const char *)h_t, ld_h, (int64_t)a.dim, ld_h},
+                          {(const char *)gl, ld_g, (int64_t)a.rows, ld_g},
+                          (int64_t)tx * BX, (int64_t)ty * BY, 0, (int64_t)(a.rows * sizeof(T))},
                          lds, acc);
   const float back = coef[a.rows];
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
@@ -484,7 +458,7 @@ size_t forward_x(size_t rows, size_t dim, size_t vocab) {
 // Pieces of the vocabulary and what the workspace holds.
 struct Plan {
   size_t vp, pieces, ld_t, splits, run;
-  size_t coef, gl, gl_t, w_t, h_t, part, bytes;
+  size_t coef, gl, w_t, h_t, part, bytes;
 };
 
 template <class S>
@@ -493,9 +467,10 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   constexpr size_t BUDGET = (size_t)1 << 30;
   Plan p{};
   p.ld_t = up(rows, 64);
-  const size_t column = 2 * (rows + p.ld_t + dim);
+  const size_t column = 2 * (rows + dim);
   size_t vp = BUDGET / column / BX * BX;
-  vp = vp < BX ? BX : vp;
+  // (at most 2^20: a tile's rows of gl within 32-bit offsets of its first)
+  vp = vp < BX ? BX : vp > ((size_t)1 << 20) ? (size_t)1 << 20 : vp;
   p.pieces = tiles(up(vocab, BX), vp);
   p.vp = up(tiles(vocab, p.pieces), BX);
   p.pieces = tiles(vocab, p.vp);
@@ -515,7 +490,6 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   };
   p.coef = take((rows + 1) * 4);
   p.gl = take(rows * p.vp * 2);
-  p.gl_t = take(p.vp * p.ld_t * 2);
   p.w_t = take(dim * p.vp * 2);
   p.h_t = take(dim * p.ld_t * 2);
   p.part = take(p.splits * rows * dim * 4);
@@ -571,8 +545,7 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   const Plan p = plan<S>(a.rows, a.dim, a.vocab);
   char *ws = (char *)a.workspace;
   float *coef = (float *)(ws + p.coef), *part = (float *)(ws + p.part);
-  T *gl = a.gh ? (T *)(ws + p.gl) : nullptr, *gl_t = a.gw ? (T *)(ws + p.gl_t) : nullptr;
-  T *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
+  T *gl = (T *)(ws + p.gl), *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
   const bool al = aligned(a);
   hipError_t e = hipSuccess;
   LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(p.ld_t, 64) * tiles(a.dim, 64) : 0))),
@@ -581,7 +554,7 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
     auto k = al ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
     LAUNCH(k, dim3((unsigned)(tiles(here, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a, v0, here,
-           p.vp, p.ld_t, coef, gl, gl_t);
+           p.vp, coef, gl);
     if (a.gh) {
       const T *w = (const T *)a.w + v0 * a.w_stride;
       const dim3 grid((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY)));
@@ -597,7 +570,7 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
     }
     if (a.gw)
       LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)(tiles(a.dim, BX) * tiles(here, BY))), S::THREADS,
-             Tl::LDS, a, v0, here, p.ld_t, coef, gl_t, h_t);
+             Tl::LDS, a, v0, here, p.vp, p.ld_t, coef, gl, h_t);
   }
   if (a.gh)
     LAUNCH(k_loss_gh_join<T>, dim3((unsigned)tiles(tiles(a.dim, 4) * a.rows, 256)), 256, 0, part,

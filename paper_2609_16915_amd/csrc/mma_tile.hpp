@@ -138,15 +138,15 @@ __device__ inline v4i load_frag(const char *row, int64_t at, int64_t end) {
 // Row 4 g + r of fragment i of a wave's X is its row g * 4 TX + 4 i + r, so that
 // a lane's accumulators are runs of 4 TX consecutive x.
 //
-// ACROSS (16-bit types, ALIGNED only): X lies the other way, k rows of nx columns
-// (X.bytes the columns' bytes, x0 a column; k1 is exact, Y's rows go on to whole 16
-// bytes with zeros).  Its stage then
-// holds 64 such rows of BX columns; chunk c (32 bytes, a fragment's 16 columns) of
-// row k lies at place c ^ key, key = (k & 3) | (k >> 1 & 4), and a fragment's
-// lanes read it turned by 4 x 4 (ds_read_b64_tr_b16: lane l of 16 gives the address
-// of row l / 4, columns 4 (l % 4) .. + 4, and gets column l of the four rows).  A
-// lane's accumulators are then runs of 4 x only.
-template <class T, int BX, int BY, int WX, int WY, bool ACROSS = false>
+// XA, YA (16-bit types, ALIGNED only): X or Y lies the other way, k rows of columns
+// (bytes: the columns'; x0 or y0 a column; k1 is then exact, and the other
+// operand's rows go on to whole 16 bytes with zeros).  Its stage holds 64 such rows
+// of BX or BY columns; chunk c (32 bytes, a fragment's 16 columns) of row k lies at
+// place c ^ key, key = (k & 3) | (k >> 1 & 4), and a fragment's lanes read it turned
+// by 4 x 4 (ds_read_b64_tr_b16: lane l of 16 gives the address of row l / 4, columns
+// 4 (l % 4) .. + 4, and gets column l of the four rows).  With XA a lane's
+// accumulators are runs of 4 x only.
+template <class T, int BX, int BY, int WX, int WY, bool XA = false, bool YA = false>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
@@ -191,38 +191,36 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     if (p.k0 >= p.k1) return;
-    // ACROSS: this lane's row and column quad in a 4 x 16 block of fragment i, half 0
-    static_assert(!ACROSS || (sizeof(T) == 2 && ALIGNED), "");
-    int across[TX];
-    if constexpr (ACROSS) {
-      const int row = 8 * g + m / 4;
+    static_assert(!(XA || YA) || (sizeof(T) == 2 && ALIGNED), "");
+    // Fragment f of this wave's part, across: rows of `width` bytes at `at`, their
+    // chunks from `first` on.
+    auto read_across = [&](const char *at, int width, int first, int s, int f) {
+      using v4s = __attribute__((ext_vector_type(4))) short;
+      using lds_v4s = __attribute__((address_space(3))) v4s;
+      const int row = 8 * g + m / 4;  // of half 0; the half and the 4 x 16 block keep its key
+      at += row * width + ((first + f) ^ key_k(row)) * 32 + m % 4 * 8 + s * 32 * width;
+      struct {
+        v4s h[2];
+      } v;
 #pragma unroll
-      for (int i = 0; i < TX; ++i)
-        across[i] = row * 2 * BX + ((wx * TX + i) ^ key_k(row)) * 32 + m % 4 * 8;
-    }
+      for (int h = 0; h < 2; ++h)
+        v.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at + h * 4 * width));
+      return __builtin_bit_cast(v4i, v);
+    };
     auto read_x = [&](const char *stage, int s, int i) {
-      if constexpr (ACROSS) {
-        using v4s = __attribute__((ext_vector_type(4))) short;
-        using lds_v4s = __attribute__((address_space(3))) v4s;
-        struct {
-          v4s h[2];
-        } f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_v4s *)(stage + across[i] + (s * 32 + h * 4) * 2 * BX));
-        return __builtin_bit_cast(v4i, f);
-      } else {
-        return *(const v4i *)(stage + atx + i * 4 * STEP + ((s * 4 + g) ^ key) * FRAG);
-      }
+      if constexpr (XA) return read_across(stage, 2 * BX, wx * TX, s, i);
+      else return *(const v4i *)(stage + atx + i * 4 * STEP + ((s * 4 + g) ^ key) * FRAG);
+    };
+    auto read_y = [&](const char *stage, int s, int j) {
+      if constexpr (YA) return read_across(stage + BX * STEP, 2 * BY, wy * TY, s, j);
+      else return *(const v4i *)(stage + aty + j * 16 * STEP + ((s * 4 + g) ^ key) * FRAG);
     };
     // Half s of a stage to registers; of a step's last bytes only `left` count.
     auto read = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], int left, auto tail) {
-      const int c = ((s * 4 + g) ^ key) * FRAG;
 #pragma unroll
       for (int i = 0; i < TX; ++i) x[i] = read_x(stage, s, i);
 #pragma unroll
-      for (int j = 0; j < TY; ++j) y[j] = *(const v4i *)(stage + aty + j * 16 * STEP + c);
+      for (int j = 0; j < TY; ++j) y[j] = read_y(stage, s, j);
       if (tail.value && (s * 4 + g) * FRAG >= left) {
 #pragma unroll
         for (int i = 0; i < TX; ++i) x[i] = v4i{0, 0, 0, 0};
@@ -240,7 +238,6 @@ struct Tile {
     // loads at a time between products.
     auto half = [&](const char *stage, int s, v4i(&x)[TX], v4i(&y)[TY], const v4i(&px)[TX],
                     const v4i(&py)[TY], auto load) {
-      const int c = ((s * 4 + g) ^ key) * FRAG;
       constexpr int READS = TX + TY;
 #pragma unroll
       for (int j = 0; j < TY; ++j) {
@@ -249,7 +246,7 @@ struct Tile {
 #pragma unroll
         for (int i = j * READS / TY; i < (j + 1) * READS / TY; ++i) {
           if (i < TX) x[i] = read_x(stage, s, i);
-          else y[i - TX] = *(const v4i *)(stage + aty + (i - TX) * 16 * STEP + c);
+          else y[i - TX] = read_y(stage, s, i - TX);
         }
 #pragma unroll
         for (int i = 0; i < TX; ++i) acc[i][j] = Mma<T>::mac(px[i], py[j], acc[i][j]);
@@ -273,30 +270,34 @@ struct Tile {
     };
     if constexpr (ALIGNED) {
       const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-      const v4i bx = buffer_at(p.X.p + p.x0 * (ACROSS ? (int64_t)sizeof(T) : p.X.ld));
-      const v4i by = buffer_at(p.Y.p + p.y0 * p.Y.ld);
+      const v4i bx = buffer_at(p.X.p + p.x0 * (XA ? (int64_t)sizeof(T) : p.X.ld));
+      const v4i by = buffer_at(p.Y.p + p.y0 * (YA ? (int64_t)sizeof(T) : p.Y.ld));
       int at[LOADS], k = (int)p.k0;
       const int end = (int)p.k1, left = (end - k - 1) % STEP + 1;
-      // ACROSS: row of the step and byte of the row of this lane's load i of X;
-      // columns past the last are the first again
-      auto across_row = [&](int i) { return ((i * WAVES + wave) * 64 + lane) / (BX / 8); };
+      auto is_across = [](int i) { return i < LX ? XA : YA; };
+      // Across: row of the step and byte of the row of this lane's load i; columns
+      // past the last are the first again.
+      auto across_piece = [&](int i) { return ((i - (i < LX ? 0 : LX)) * WAVES + wave) * 64 + lane; };
+      auto across_row = [&](int i) { return across_piece(i) / ((i < LX ? BX : BY) / 8); };
       auto across_byte = [&](int i) {
-        const int piece = ((i * WAVES + wave) * 64 + lane) % (BX / 8);
+        const int piece = across_piece(i) % ((i < LX ? BX : BY) / 8);
         const int byte = ((piece / 2) ^ key_k(across_row(i))) * 32 + piece % 2 * FRAG;
-        return p.x0 * (int64_t)sizeof(T) + byte + FRAG <= p.X.bytes ? byte : 0;
+        const int64_t first = (i < LX ? p.x0 : p.y0) * (int64_t)sizeof(T);
+        return first + byte + FRAG <= (i < LX ? p.X.bytes : p.Y.bytes) ? byte : 0;
       };
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        if (ACROSS && i < LX) at[i] = across_row(i) * (int)p.X.ld + across_byte(i);
-        else at[i] = row_in(i) * (int)(i < LX ? p.X.ld : p.Y.ld) + chunk_of(i);
+        const int ld = (int)(i < LX ? p.X.ld : p.Y.ld);
+        at[i] = is_across(i) ? across_row(i) * ld + across_byte(i) : row_in(i) * ld + chunk_of(i);
       }
       auto load_one = [&](int i, int at, int k, int stage) {
         const unsigned to = base + stage + (i * WAVES + wave) * 1024;
-        if (ACROSS && i < LX)
-          load_to_lds(buffer_on(bx, k / (int)sizeof(T) * p.X.ld), at, 0, to);
-        else load_to_lds(i < LX ? bx : by, at, k, to);
+        const v4i buf = i < LX ? bx : by;
+        if (is_across(i))
+          load_to_lds(buffer_on(buf, k / (int)sizeof(T) * (i < LX ? p.X.ld : p.Y.ld)), at, 0, to);
+        else load_to_lds(buf, at, k, to);
       };
-      // the last step may be part of one: chunks (ACROSS: rows) beyond it read its
+      // the last step may be part of one: chunks (across: rows) beyond it read its
       // first again, and read() takes them as zeros
       auto load_any = [&](int k, int stage) {
         if (k + STEP <= end) {
@@ -305,7 +306,7 @@ struct Tile {
         } else if (k < end) {
 #pragma unroll
           for (int i = 0; i < LOADS; ++i) {
-            if (ACROSS && i < LX)
+            if (is_across(i))
               load_one(i, across_row(i) * (int)sizeof(T) < left ? at[i] : across_byte(i), k, stage);
             else load_one(i, at[i] - (chunk_of(i) < left ? 0 : chunk_of(i)), k, stage);
           }
@@ -370,10 +371,10 @@ struct Tile {
     __syncthreads();
   }
 
-  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r (ACROSS:
+  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r (XA:
   // + 16 i + r) and y_at() + 16 j
   __device__ static int x_at() {
-    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * (ACROSS ? 4 : 4 * TX);
+    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * (XA ? 4 : 4 * TX);
   }
   __device__ static int y_at() {
     return (threadIdx.x / 64) / WX * (BY / WY) + threadIdx.x % 16;

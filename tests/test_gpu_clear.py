@@ -360,9 +360,9 @@ def test_cross_entropy_large_logits_and_uneven_factors(dtype):
 def test_cross_entropy_gradients_in_pieces(dtype, dim):
     """Enough rows that gl is held for a part of the vocabulary at a time, the last
     part shorter than the others by more than a tile."""
-    rows, vocab = 16384, 17000
+    rows, vocab = 16384, 40000
     one = R.lib().rosetta_cross_entropy_backward_workspace_bytes(rows, dim, vocab)
-    assert one < 2 * 2 * rows * vocab  # (not all of gl, twice)
+    assert one < 2 * rows * vocab  # (not all of gl)
     g = torch.full((rows,), 1.0 / rows)
     check_loss(normal(64, rows, dim, dtype), normal(65, vocab, dim, dtype, 1.0 / math.sqrt(dim)),
                targets(66, rows, vocab, 1000), g, -100, dtype, dev="cuda")
