@@ -119,35 +119,44 @@ struct Plan {
 size_t tiles(size_t a, size_t b) { return (a + b - 1) / b; }
 
 Plan plan(size_t m, size_t n, size_t k) {
-  const size_t cus = std::max(1, device_cus());
+  const size_t cus = std::max(1, device_cus()), steps = tiles(k, STEP);
   Plan p{Cut::THIN, 1, 1, 1, 0};
-  size_t most = 1;
+  size_t parts = 1;
   // Few tokens: bound by the channels' bytes, so every CU needs channels to read,
   // and the more a block has the less often the tokens are read.  (Rows of less
   // than half a step for each of a block's waves leave most of them idle: tiles.)
   const bool thin = k >= 8 * STEP;
   if (thin && m <= 16) {
     p.nx = tiles(n, 64) >= cus ? 4 : tiles(n, 32) >= cus ? 2 : 1;
-  } else if (thin && m <= 32) {
-    p.ny = 2;
-    p.nx = tiles(n, 32) >= cus ? 2 : 1;
   } else if (thin && m <= 64) {
-    p.ny = m <= 48 ? 3 : 4;
+    // 64 channels a block; where those are too few for the chip, parts of their
+    // sums, one round of blocks and 16 steps each at least (33 tokens, 4096 x 14336:
+    // four parts 16.9 us, eight in two rounds 19.9; 16 channels in one part 24.5)
     p.nx = 4;
-    most = tiles(2 * cus, tiles(n, 64));
+    p.ny = (int)tiles(m, 16);
+    parts = std::max((size_t)1, std::min(cus / tiles(n, 64), steps / 16));
   } else {
     // Large tiles do a product at half the cost of small ones but come one to a
     // CU, small ones two: the smaller of the two times, in steps of a large one.
-    const size_t steps = tiles(k, STEP);
     const size_t nl = tiles(n, 256) * tiles(m, 256), ns = tiles(n, 128) * tiles(m, 128);
     const double large = (double)tiles(nl, cus) * (steps + 3);
     const double small = (ns <= cus ? 0.42 : 0.63 * ((double)ns / (2 * cus) + 0.5)) * (steps + 3);
     p.cut = large <= small ? Cut::LARGE : Cut::SMALL;
-    if (p.cut == Cut::SMALL && ns <= cus) most = 2 * cus / ns;
+    // Too few small tiles for the chip: parts of their sums, as many as pay.  In us:
+    // a step 0.65 while tiles have a CU each, 0.5 for each that shares one; the
+    // joining 3 and what it writes and reads at 4 TB/s (1024 tokens, 4096 x 4096: one
+    // part 24.3, two 34.4; 128 tokens, 4096 x 14336: 14 parts 24.9, one 71).
+    if (p.cut == Cut::SMALL) {
+      double best = 1e30;
+      for (size_t q = 1; q <= std::max((size_t)1, std::min(2 * cus / ns, steps / 8)); ++q) {
+        const double each = ns * q <= cus ? 0.65 : 0.5 * (double)(ns * q) / (double)cus;
+        const double t = (double)tiles(steps, q) * each +
+                         (q > 1 ? 3 + (double)q * (double)m * (double)n * 8 / 4e6 : 0);
+        if (t < best) best = t, parts = q;
+      }
+    }
   }
-  // a part of a sum is 8 steps at least, or the joining costs more than it gives
-  const size_t parts = std::max((size_t)1, std::min(most, k / (8 * STEP)));
-  p.run = (int)(tiles(tiles(k, parts), STEP) * STEP);
+  p.run = (int)(tiles(steps, parts) * STEP);
   p.splits = k ? (int)tiles(k, (size_t)p.run) : 1;
   return p;
 }
@@ -191,8 +200,7 @@ hipError_t launch(const Q8Args &a, hipStream_t st) {
         case 9: e = thin<O, 1, 1, 16>(a, p, st); break;
         case 10: e = thin<O, 2, 1, 16>(a, p, st); break;
         case 12: e = thin<O, 4, 1, 16>(a, p, st); break;
-        case 17: e = thin<O, 1, 2, 16>(a, p, st); break;
-        case 18: e = thin<O, 2, 2, 16>(a, p, st); break;
+        case 20: e = thin<O, 4, 2, 8>(a, p, st); break;
         case 28: e = thin<O, 4, 3, 8>(a, p, st); break;
         default: e = thin<O, 4, 4, 8>(a, p, st); break;
       }
