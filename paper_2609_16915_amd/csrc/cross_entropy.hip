@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(S::THREADS)
 k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restrict__ gl,
                const T *__restrict__ w, size_t w_stride, float *__restrict__ part, size_t run,
                int add) {
-  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, ACROSS>;
+  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, 2, ACROSS>;
   constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(S::THREADS)
 k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                const float *__restrict__ coef, const T *__restrict__ gl,
                const T *__restrict__ h_t) {
-  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, false, true>;
+  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, 2, false, true>;
   constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)((here + BY - 1) / BY);

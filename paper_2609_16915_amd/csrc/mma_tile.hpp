@@ -92,9 +92,11 @@ __device__ inline void load_to_lds(v4i buf, int at, int k, unsigned lds) {
                : "memory", "m0");
 }
 
-// This wave's LDS loads have landed and its LDS reads are done; then all of them.
+// All but N of this wave's LDS loads have landed and its LDS reads are done; then
+// all waves'.
+template <int N = 0>
 __device__ inline void barrier_loaded() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // Block b of `blocks`, numbered so that each of the eight XCDs (blocks are
@@ -146,12 +148,12 @@ __device__ inline v4i load_frag(const char *row, int64_t at, int64_t end) {
 // by 4 x 4 (ds_read_b64_tr_b16: lane l of 16 gives the address of row l / 4, columns
 // 4 (l % 4) .. + 4, and gets column l of the four rows).  With XA a lane's
 // accumulators are runs of 4 x only.
-template <class T, int BX, int BY, int WX, int WY, bool XA = false, bool YA = false>
+template <class T, int BX, int BY, int WX, int WY, int STAGES = 2, bool XA = false, bool YA = false>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
   static constexpr int STAGE = (BX + BY) * STEP;
-  static constexpr int LDS = 2 * STAGE;  // what the stages take
+  static constexpr int LDS = STAGES * STAGE;  // what the stages take
   static constexpr int LOADS = (BX + BY) / 8 / WAVES;  // of 8 rows, per wave and stage
   static_assert((BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
   using Acc = typename Mma<T>::Acc;
@@ -312,28 +314,29 @@ struct Tile {
           }
         }
       };
-      load_any(k, 0);
-      load_any(k + STEP, STAGE);
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) load_any(k + i * STEP, i * STAGE);
       int b = 0;
+      auto next = [](int b) { return b + STAGE == LDS ? 0 : b + STAGE; };
       barrier_loaded();
       // Both halves of a step in registers, one ahead: the second half's reads go
       // with the first's products, then, the next step's loads having landed, the
       // next first half's with the second's.
       if (k + STEP <= end) read(lds, 0, x0f, y0f, STEP, whole);
-      for (; k + 3 * STEP <= end; k += STEP, b = STAGE - b) {
+      for (; k + (STAGES + 1) * STEP <= end; k += STEP, b = next(b)) {
         half(lds + b, 1, x1f, y1f, x0f, y0f, [](int) {});
-        barrier_loaded();
-        half(lds + (STAGE - b), 0, x0f, y0f, x1f, y1f, [&](int i) {
-          load_one(i, at[i], k + 2 * STEP, b);
+        barrier_loaded<(STAGES - 2) * LOADS>();
+        half(lds + next(b), 0, x0f, y0f, x1f, y1f, [&](int i) {
+          load_one(i, at[i], k + STAGES * STEP, b);
         });
       }
-      // at most two more whole steps and a part of one
-      for (; k + STEP <= end; k += STEP, b = STAGE - b) {
+      // at most STAGES more whole steps and a part of one
+      for (; k + STEP <= end; k += STEP, b = next(b)) {
         read(lds + b, 1, x1f, y1f, STEP, whole);
         multiply(x0f, y0f);
         barrier_loaded();
-        load_any(k + 2 * STEP, b);
-        if (k + 2 * STEP <= end) read(lds + (STAGE - b), 0, x0f, y0f, STEP, whole);
+        load_any(k + STAGES * STEP, b);
+        if (k + 2 * STEP <= end) read(lds + next(b), 0, x0f, y0f, STEP, whole);
         multiply(x1f, y1f);
       }
       if (k < end) {

@@ -31,9 +31,9 @@ __device__ inline int *part_at(const Q8Args &a, int64_t ld, unsigned split, int6
 }
 
 // `run`: bytes of the rows per split, all of them in one.
-template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
-__global__ void __launch_bounds__(64 * WX *WY) k_q8_tile(Q8Args a, int splits, int run) {
-  using Tl = Tile<int8_t, BX, BY, WX, WY>;
+template <class O, bool ALIGNED, int BX, int BY, int STAGES>
+__global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) {
+  using Tl = Tile<int8_t, BX, BY, 4, 2, STAGES>;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.n + BX - 1) / BX), gy = (unsigned)((a.m + BY - 1) / BY);
   const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
@@ -108,8 +108,10 @@ __global__ void __launch_bounds__(256) k_q8_join(Q8Args a, int splits) {
   put4<O>(a, y, x, s);
 }
 
-// How a product is cut up.
-enum class Cut { THIN, SMALL, LARGE };
+// How a product is cut up.  DEEP: small tiles with a CU each, whose steps are loaded
+// four ahead (1024 x 4096 x 4096: 21 us for 25; where two tiles share a CU they cover
+// for each other, 2200 TOP/s with two stages and 1908 with four).
+enum class Cut { THIN, SMALL, DEEP, LARGE };
 struct Plan {
   Cut cut;
   int nx, ny;  // THIN
@@ -143,17 +145,19 @@ Plan plan(size_t m, size_t n, size_t k) {
     const double small = (ns <= cus ? 0.42 : 0.63 * ((double)ns / (2 * cus) + 0.5)) * (steps + 3);
     p.cut = large <= small ? Cut::LARGE : Cut::SMALL;
     // Too few small tiles for the chip: parts of their sums, as many as pay.  In us:
-    // a step 0.65 while tiles have a CU each, 0.5 for each that shares one; the
-    // joining 3 and what it writes and reads at 4 TB/s (1024 tokens, 4096 x 4096: one
+    // a step 0.55 while tiles have a CU each, 0.5 for each that shares one; the
+    // joining 6 and what it writes and reads at 4 TB/s (1024 tokens, 4096 x 4096: one
     // part 24.3, two 34.4; 128 tokens, 4096 x 14336: 14 parts 24.9, one 71).
     if (p.cut == Cut::SMALL) {
       double best = 1e30;
+      bool alone = false;
       for (size_t q = 1; q <= std::max((size_t)1, std::min(2 * cus / ns, steps / 8)); ++q) {
-        const double each = ns * q <= cus ? 0.65 : 0.5 * (double)(ns * q) / (double)cus;
+        const double each = ns * q <= cus ? 0.55 : 0.5 * (double)(ns * q) / (double)cus;
         const double t = (double)tiles(steps, q) * each +
-                         (q > 1 ? 3 + (double)q * (double)m * (double)n * 8 / 4e6 : 0);
-        if (t < best) best = t, parts = q;
+                         (q > 1 ? 6 + (double)q * (double)m * (double)n * 8 / 4e6 : 0);
+        if (t < best) best = t, parts = q, alone = ns * q <= cus;
       }
+      if (alone) p.cut = Cut::DEEP;
     }
   }
   p.run = (int)(tiles(steps, parts) * STEP);
@@ -161,10 +165,10 @@ Plan plan(size_t m, size_t n, size_t k) {
   return p;
 }
 
-template <class O, bool ALIGNED, int BX, int BY, int WX, int WY>
+template <class O, bool ALIGNED, int BX, int BY, int STAGES>
 hipError_t tile(const Q8Args &a, const Plan &p, hipStream_t st) {
-  using Tl = Tile<int8_t, BX, BY, WX, WY>;
-  auto k = k_q8_tile<O, ALIGNED, BX, BY, WX, WY>;
+  using Tl = Tile<int8_t, BX, BY, 4, 2, STAGES>;
+  auto k = k_q8_tile<O, ALIGNED, BX, BY, STAGES>;
   const hipError_t e = allow_lds(k, Tl::LDS);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k, dim3((unsigned)(tiles(a.n, BX) * tiles(a.m, BY) * p.splits)),
@@ -206,12 +210,13 @@ hipError_t launch(const Q8Args &a, hipStream_t st) {
       }
       break;
     case Cut::SMALL:
-      e = al ? tile<O, true, 128, 128, 4, 2>(a, p, st)
-             : tile<O, false, 128, 128, 4, 2>(a, p, st);
+      e = al ? tile<O, true, 128, 128, 2>(a, p, st) : tile<O, false, 128, 128, 2>(a, p, st);
+      break;
+    case Cut::DEEP:
+      e = al ? tile<O, true, 128, 128, 4>(a, p, st) : tile<O, false, 128, 128, 2>(a, p, st);
       break;
     case Cut::LARGE:
-      e = al ? tile<O, true, 256, 256, 4, 2>(a, p, st)
-             : tile<O, false, 256, 256, 4, 2>(a, p, st);
+      e = al ? tile<O, true, 256, 256, 2>(a, p, st) : tile<O, false, 256, 256, 2>(a, p, st);
       break;
   }
   if (e != hipSuccess || p.splits == 1) return e;
