@@ -6,7 +6,8 @@
 // use.  One reduction serves both the norm and the 8-bit scale, since
 //   y / scale = h w inv_rms / (max|h w| inv_rms / 127) = h w * (127 / max|h w|):
 // the sum of h^2 and the maximum of |h w| are taken together, and q needs
-// neither inv_rms nor a second pass.
+// neither inv_rms nor a second pass.  Sums, the norm and scales are 32-bit floats;
+// what is stored in fewer bits is rounded once, from them.
 #include <algorithm>
 #include <type_traits>
 
@@ -157,6 +158,9 @@ __device__ inline void q_factors(float top, float &f0, float &f1) {
 // TPR threads to a row and NV vectors of a thread in registers, rows one after
 // the other with the next one's loads under way; NV = 0: rows of any length, read
 // again where they are used.  NORM false: x alone to 8 bits.
+//
+// Bound by memory: 7 bytes an element in bf16 with residual, h and q.  16384 x 4096
+// takes 88 us, 5.3 TB/s (a row per block without the next one's loads: 126 us).
 template <class T, class W, int TPR, int NV, bool NORM, bool WHOLE>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
@@ -313,6 +317,7 @@ hipError_t norm_by_length(const NormArgs &a, hipStream_t st) {
   return a.dim % VEC ? norm_by_size<T, W, NORM, false>(a, st) : norm_by_size<T, W, NORM, true>(a, st);
 }
 
+// Bound by memory: 3 bytes an element to bf16; 16384 x 4096 takes 35 us.
 template <class T>
 __global__ void __launch_bounds__(256)
 k_dequantize_rows(const int8_t *__restrict__ q, size_t q_stride, const float *__restrict__ scale,
@@ -378,10 +383,17 @@ namespace {
 
 constexpr size_t BACK_GROUPS = 512;  // two workgroups of rows per CU (three: 56.4 us for 53.8)
 
+// With y = h inv w, inv = (mean h^2 + eps)^(-1/2):
+//   gx = gh + inv gy w - h inv^3 mean(gy w h),  gweight = sum over rows of gy h inv.
+//
 // A workgroup takes rows blockIdx.x, + gridDim.x, ..; each thread keeps the sums
 // over rows of its columns' gy h inv_rms and writes them to the workgroup's
 // row of `partial`, which k_sum_partial adds up in order.  NV = 0: rows of any
 // length; the sums are then kept in `partial` itself.
+//
+// Bound by memory: 8 bytes an element in bf16.  8192 x 4096 takes 53 us with the
+// sums, 5.0 TB/s (without the next row's loads under way 113 us: eight waves a CU
+// wait for a row, reduce it and write it, in turn).
 template <class T, class W, int TPR, int NV, bool WHOLE>
 __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
   __shared__ float lds[2 * 16];
