@@ -250,6 +250,20 @@ def test_q8_matmul(m, n, k, pad, offset, dtype):
         assert torch.isnan(beside).all()
 
 
+@pytest.mark.parametrize("m,n,k,pad", [(4090, 4095, 300, 0), (4090, 4095, 304, 16),
+                                       (3968, 4096, 512, 0), (2049, 2047, 4112, 0),
+                                       (700, 1111, 9008, 16), (100, 300, 20001, 0)])
+def test_q8_matmul_large(m, n, k, pad):
+    """Enough outputs for the large tiles, and few enough that small ones have a CU
+    each; products taken in 64 bits on the GPU."""
+    a, b = int8(35, m, k), int8(36, n, k)
+    sa, sb = 0.01 + torch.rand(m, generator=gen(37)), 0.01 + torch.rand(n, generator=gen(38))
+    got = R.q8_matmul(placed(a, pad), sa.cuda(), placed(b, pad), sb.cuda(), out_dtype=F32)
+    prod = a.cuda().to(D) @ b.cuda().to(D).t().contiguous()
+    want = prod * sa.cuda().to(D)[:, None] * sb.cuda().to(D)
+    within(got, want, 4 * E * want.abs())
+
+
 @pytest.mark.parametrize("m", [1, 40, 200])
 def test_q8_matmul_largest_sums(m):
     k = 131071
@@ -368,6 +382,15 @@ def test_cross_entropy_gradients_in_pieces(dtype, dim):
                targets(66, rows, vocab, 1000), g, -100, dtype, dev="cuda")
 
 
+@pytest.mark.parametrize("dtype,rows,dim,vocab,pad", [
+    (BF16, 4000, 640, 8100, 0), (F16, 4001, 648, 8111, 8), (BF16, 4001, 649, 8111, 0)])
+def test_cross_entropy_large(dtype, rows, dim, vocab, pad):
+    """Enough rows and words for the large tiles."""
+    g = torch.rand(rows, generator=gen(67)) / rows
+    check_loss(normal(68, rows, dim, dtype), normal(69, vocab, dim, dtype, 2.0 / math.sqrt(dim)),
+               targets(70, rows, vocab, 500), g, -100, dtype, pad, dev="cuda")
+
+
 def test_cross_entropy_targets_out_of_range():
     rows, dim, vocab = 40, 64, 100
     t = targets(70, rows, vocab)
@@ -467,8 +490,8 @@ def _chain(x, r, w, wq, ws, head, t, stream=None):
     return loss, gw, gx, gn
 
 
-def test_another_stream_and_a_captured_graph():
-    rows, dim, vocab = 90, 256, 1000
+@pytest.mark.parametrize("rows,dim,vocab", [(90, 256, 1000), (4000, 640, 8100)])
+def test_another_stream_and_a_captured_graph(rows, dim, vocab):
     args = [normal(90, rows, dim, BF16), normal(91, rows, dim, BF16),
             normal(92, 1, dim, BF16)[0], int8(93, dim, dim),
             1e-3 * torch.rand(dim, generator=gen(94)),
