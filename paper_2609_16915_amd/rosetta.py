@@ -637,34 +637,42 @@ def _type(dtype, name: str) -> int:
     return code
 
 
+@functools.lru_cache(maxsize=None)
+def _tensor_class():
+    return _torch().Tensor
+
+
 def _mat(t, name: str, dtype=None, shape=None):
     """(address, row stride, rows, columns) of a device matrix with contiguous
     rows; a vector is one row.  TypeError for the wrong kind of tensor,
     ValueError for the wrong size, before any library call."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _tensor_class()):
         raise TypeError(f"{name} must be a torch tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() > 2 or t.dim() < 1:
-        raise ValueError(f"{name} must be a matrix or one row, not {tuple(t.shape)}")
-    rows, cols = t.shape if t.dim() == 2 else (1, t.shape[0])
-    if shape is not None and (rows, cols) != tuple(shape):
+    size, strides = t.shape, t.stride()
+    if len(size) == 2:
+        rows, cols = size
+        stride = strides[0] if rows > 1 else cols
+    elif len(size) == 1:
+        rows, cols, stride = 1, size[0], size[0]
+    else:
+        raise ValueError(f"{name} must be a matrix or one row, not {tuple(size)}")
+    if shape is not None and (rows != shape[0] or cols != shape[1]):
         raise ValueError(f"{name} is {rows} x {cols}, the call needs {shape[0]} x {shape[1]}")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a torch tensor on a ROCm device")
-    if cols > 1 and t.stride(-1) != 1:
+    if cols > 1 and strides[-1] != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    stride = t.stride(0) if t.dim() == 2 and rows > 1 else cols
     return t.data_ptr(), stride, rows, cols
 
 
 def _vec(t, name: str, dtype, count: int) -> int:
     """Address of a contiguous device vector of `count` elements."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+    if not isinstance(t, _tensor_class()) or t.dtype != dtype:
         raise TypeError(f"{name} must be a torch tensor of {dtype}")
-    _expect(t, name, count)
+    if t.numel() != count:
+        _expect(t, name, count)
     if not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous on a ROCm device")
     return t.data_ptr()

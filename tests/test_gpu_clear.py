@@ -463,6 +463,49 @@ def test_cross_entropy_gradient_against_differences():
 
 # -------------------------------------------------- streams and memory ---
 
+def far(t, stride):
+    """The same rows `stride` elements apart: a stride that takes the last row past
+    what 32 bits count."""
+    rows, cols = t.shape
+    buf = torch.empty((rows - 1) * stride + cols, dtype=t.dtype, device="cuda")
+    m = torch.as_strided(buf, (rows, cols), (stride, 1))
+    m.copy_(t)
+    return m
+
+
+@pytest.mark.parametrize("dim", [72, 20000])
+def test_norm_of_rows_far_apart(dim):
+    x, r, w = normal(120, 3, dim, BF16).cuda(), normal(121, 3, dim, BF16).cuda(), None
+    want = R.rms_norm_q8(x, w, EPS, residual=r)
+    got = R.rms_norm_q8(far(x, (1 << 31) + 8), w, EPS, residual=r,
+                        q=far(torch.zeros_like(want.q), (1 << 31) + 24))
+    assert torch.equal(got.h, want.h) and torch.equal(got.q, want.q)
+    assert torch.equal(R.dequantize_rows(got.q, got.scale, F32),
+                       R.dequantize_rows(want.q, want.scale, F32))
+    back = R.rms_norm_backward(r, want.h, w, want.inv_rms)
+    over = R.rms_norm_backward(r, far(want.h, (1 << 31) + 8), w, want.inv_rms,
+                               gx=far(torch.zeros_like(r), 1 << 31))
+    assert torch.equal(back[0], over[0]) and torch.equal(back[1], over[1])
+
+
+@pytest.mark.parametrize("m", [2, 70])
+def test_products_of_rows_far_apart(m):
+    a, b = int8(122, m, 1040).cuda(), int8(123, 5, 1040).cuda()
+    sa, sb = torch.rand(m, device="cuda"), torch.rand(5, device="cuda")
+    want = R.q8_matmul(a, sa, b, sb, out_dtype=F32)
+    assert torch.equal(R.q8_matmul(a, sa, far(b, (1 << 30) + 16), sb, out_dtype=F32), want)
+    h, w = normal(124, m, 520, BF16).cuda(), normal(125, 5, 520, BF16).cuda()
+    t, g = targets(126, m, 5).cuda(), torch.rand(m, generator=gen(127)).cuda()
+    wf = far(w, (1 << 30) + 8)
+    loss, lse = R.cross_entropy(h, w, t)
+    loss2, lse2 = R.cross_entropy(h, wf, t)
+    assert torch.allclose(lse, lse2, rtol=0, atol=1e-5) and torch.allclose(loss, loss2, atol=1e-5)
+    gh, gw = R.cross_entropy_backward(h, w, t, lse, g)
+    gh2, gw2 = R.cross_entropy_backward(h, wf, t, lse, g, gw=far(torch.zeros_like(w), 1 << 30))
+    assert torch.equal(gh, gh2) and torch.equal(gw, gw2)
+
+
+
 def test_rows_of_none():
     e = torch.empty((0, 64), dtype=BF16, device="cuda")
     one = torch.ones(64, dtype=BF16, device="cuda")
