@@ -156,7 +156,14 @@ __device__ inline v4i load_frag(const char *row, int64_t at, int64_t end) {
 // by 4 x 4 (ds_read_b64_tr_b16: lane l of 16 gives the address of row l / 4, columns
 // 4 (l % 4) .. + 4, and gets column l of the four rows).  With XA a lane's
 // accumulators are runs of 4 x only.
-template <class T, int BX, int BY, int WX, int WY, int STAGES = 2, bool XA = false, bool YA = false>
+//
+// RUNS false: row m of fragment i of a wave's X is its row 16 i + m, and a lane's
+// accumulators are runs of 4 x, four lanes' next to each other: 32-bit outputs then
+// leave 64 bytes together (4096 x 4096 x 4096 bytes to f32: 68 us for 152 with each
+// lane's 16 bytes alone in their 64; in 16 bits a lane's runs are 32 bytes, and lanes
+// that trade halves for 64 gained nothing).
+template <class T, int BX, int BY, int WX, int WY, int STAGES = 2, bool XA = false, bool YA = false,
+          bool RUNS = !XA>
 struct Tile {
   static constexpr int WAVES = WX * WY, THREADS = 64 * WAVES;
   static constexpr int TX = BX / WX / 16, TY = BY / WY / 16;
@@ -167,7 +174,7 @@ struct Tile {
   using Acc = typename Mma<T>::Acc;
 
   __device__ static int key_x(int row) {
-    const int m = (row / (4 * TX) & 3) * 4 + (row & 3);
+    const int m = RUNS ? (row / (4 * TX) & 3) * 4 + (row & 3) : row;
     return (m >> 1) & 7;
   }
   __device__ static int key_y(int row) { return (row >> 1) & 7; }
@@ -194,7 +201,7 @@ struct Tile {
     // this lane's place in fragment 0 of its wave's X and Y
     const int m = lane % 16, g = lane / 16;
     const int key = (m >> 1) & 7;
-    const int atx = (wx * (BX / WX) + (m / 4) * 4 * TX + m % 4) * STEP;
+    const int atx = (wx * (BX / WX) + (RUNS ? (m / 4) * 4 * TX + m % 4 : m)) * STEP;
     const int aty = (BX + wy * (BY / WY) + m) * STEP;
 #pragma unroll
     for (int i = 0; i < TX; ++i)
@@ -219,7 +226,7 @@ struct Tile {
     };
     auto read_x = [&](const char *stage, int s, int i) {
       if constexpr (XA) return read_across(stage, 2 * BX, wx * TX, s, i);
-      else return *(const v4i *)(stage + atx + i * 4 * STEP + ((s * 4 + g) ^ key) * FRAG);
+      else return *(const v4i *)(stage + atx + i * (RUNS ? 4 : 16) * STEP + ((s * 4 + g) ^ key) * FRAG);
     };
     auto read_y = [&](const char *stage, int s, int j) {
       if constexpr (YA) return read_across(stage + BX * STEP, 2 * BY, wy * TY, s, j);
@@ -382,10 +389,10 @@ struct Tile {
     __syncthreads();
   }
 
-  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r (XA:
-  // + 16 i + r) and y_at() + 16 j
+  // x and y (within the tile) of acc[i][j][r] of this lane: x_at() + 4 i + r (RUNS
+  // false: + 16 i + r) and y_at() + 16 j
   __device__ static int x_at() {
-    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * (XA ? 4 : 4 * TX);
+    return (threadIdx.x / 64) % WX * (BX / WX) + (threadIdx.x % 64) / 16 * (RUNS ? 4 * TX : 4);
   }
   __device__ static int y_at() {
     return (threadIdx.x / 64) / WX * (BY / WY) + threadIdx.x % 16;

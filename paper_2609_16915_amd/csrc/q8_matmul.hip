@@ -30,11 +30,16 @@ __device__ inline int *part_at(const Q8Args &a, int64_t ld, unsigned split, int6
   return a.workspace + ((int64_t)split * (int64_t)a.m + y) * ld + x;
 }
 
+template <class O, int BX, int BY, int STAGES>
+using Q8Tile = Tile<int8_t, BX, BY, 4, 2, STAGES, false, false, sizeof(O) == 2>;
+
 // `run`: bytes of the rows per split, all of them in one.  8192 x 14336 x 4096 takes
 // 395 us (2.44 POP/s; 235 MB of outputs leave at the ends of seven rounds of tiles).
 template <class O, bool ALIGNED, int BX, int BY, int STAGES>
 __global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) {
-  using Tl = Tile<int8_t, BX, BY, 4, 2, STAGES>;
+  using Tl = Q8Tile<O, BX, BY, STAGES>;
+  // a lane's x: RUNS of RUN, 16 apart
+  constexpr int RUN = sizeof(O) == 2 ? 4 * Tl::TX : 4, RUNS = 4 * Tl::TX / RUN;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.n + BX - 1) / BX), gy = (unsigned)((a.m + BY - 1) / BY);
   const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
@@ -54,7 +59,8 @@ __global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) 
       if (y0 + 16 * j >= (int64_t)a.m) continue;
 #pragma unroll
       for (int i = 0; i < Tl::TX; ++i)
-        if (x0 + 4 * i < ld) *(v4i *)part_at(a, ld, split, y0 + 16 * j, x0 + 4 * i) = acc[i][j];
+        if (const int64_t x = x0 + (RUNS == 1 ? 4 : 16) * i; x < ld)
+          *(v4i *)part_at(a, ld, split, y0 + 16 * j, x) = acc[i][j];
     }
     return;
   }
@@ -62,20 +68,26 @@ __global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) 
   if (left <= 0) return;
   // (all that is read, before anything is written: in between, every row would
   // wait for its own scale)
-  float bs[4 * Tl::TX], bias[4 * Tl::TX] = {}, as[Tl::TY];
-  load_run(a.b_scale + x0, left, bs);
-  if (a.bias) load_run(a.bias + x0, left, bias);
+  float bs[RUNS][RUN], bias[RUNS][RUN] = {}, as[Tl::TY];
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c) {
+    load_run(a.b_scale + x0 + 16 * c, left - 16 * c, bs[c]);
+    if (a.bias) load_run(a.bias + x0 + 16 * c, left - 16 * c, bias[c]);
+  }
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) as[j] = y0 + 16 * j < (int64_t)a.m ? a.a_scale[y0 + 16 * j] : 0.f;
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t y = y0 + 16 * j;
     if (y >= (int64_t)a.m) continue;
-    float f[4 * Tl::TX];
 #pragma unroll
-    for (int i = 0; i < 4 * Tl::TX; ++i)
-      f[i] = (float)acc[i / 4][j][i % 4] * as[j] * bs[i] + bias[i];
-    store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x0, left, f);
+    for (int c = 0; c < RUNS; ++c) {
+      float f[RUN];
+#pragma unroll
+      for (int i = 0; i < RUN; ++i)
+        f[i] = (float)acc[c + i / 4][j][i % 4] * as[j] * bs[c][i] + bias[c][i];
+      store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x0 + 16 * c, left - 16 * c, f);
+    }
   }
 }
 
@@ -171,7 +183,7 @@ Plan plan(size_t m, size_t n, size_t k) {
 
 template <class O, bool ALIGNED, int BX, int BY, int STAGES>
 hipError_t tile(const Q8Args &a, const Plan &p, hipStream_t st) {
-  using Tl = Tile<int8_t, BX, BY, 4, 2, STAGES>;
+  using Tl = Q8Tile<O, BX, BY, STAGES>;
   auto k = k_q8_tile<O, ALIGNED, BX, BY, STAGES>;
   const hipError_t e = allow_lds(k, Tl::LDS);
   if (e != hipSuccess) return e;

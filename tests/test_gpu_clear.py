@@ -264,6 +264,17 @@ def test_q8_matmul_large(m, n, k, pad):
     within(got, want, 4 * E * want.abs())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("m,n,k,pad", [(4090, 4095, 304, 16), (3968, 4096, 512, 0)])
+def test_q8_matmul_large_in_16_bits(m, n, k, pad, dtype):
+    a, b = int8(39, m, k), int8(40, n, k)
+    sa, sb = 0.01 + torch.rand(m, generator=gen(41)), 1e-4 + 1e-4 * torch.rand(n, generator=gen(42))
+    got = R.q8_matmul(placed(a, pad), sa.cuda(), placed(b, pad), sb.cuda(), out_dtype=dtype)
+    prod = a.cuda().to(D) @ b.cuda().to(D).t().contiguous()
+    want = prod * sa.cuda().to(D)[:, None] * sb.cuda().to(D)
+    within(got, want, (U[dtype] + 4 * E) * want.abs() + TINY[dtype])
+
+
 @pytest.mark.parametrize("m", [1, 40, 200])
 def test_q8_matmul_largest_sums(m):
     k = 131071
