@@ -70,15 +70,40 @@ struct Raw {
   }
 };
 
+// Asked for in one load, also where the row ends inside the vector: the row's last
+// eight are then read, and settle() moves them down once they are there (a branch
+// around each load would wait for the one before).  `dim`: the row's length.
 template <class T, class L>
-__device__ inline void load8_raw(const T *p, L left, Raw<T> &v) {
-  if ((size_t)left >= VEC) {
+__device__ inline void load8_raw(const T *p, L left, size_t dim, Raw<T> &v) {
+  if constexpr (std::is_same_v<L, Whole>) {
     __builtin_memcpy(&v, p, sizeof v);
+  } else if (dim >= VEC) {
+    __builtin_memcpy(&v, p - (left < VEC ? VEC - left : 0), sizeof v);
   } else {
     T e[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) e[i] = (size_t)i < (size_t)left ? p[i] : (T)0.f;
     __builtin_memcpy(&v, e, sizeof v);
+  }
+}
+template <class T, class L>
+__device__ inline void settle(L left, size_t dim, Raw<T> &v) {
+  if constexpr (!std::is_same_v<L, Whole>) {
+    if (left < VEC && dim >= VEC) {
+      const int by = (int)(VEC - left);  // elements, zeros from above
+      constexpr int W = Raw<T>::WORDS;
+#pragma unroll
+      for (int n = 4; n >= 1; n /= 2) {
+        if (!(by & n)) continue;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          if (sizeof(T) == 2 && n == 1)
+            v.w[i] = (int)((unsigned)v.w[i] >> 16) | (i + 1 < W ? v.w[i + 1] << 16 : 0);
+          else
+            v.w[i] = i + n * W / VEC < W ? v.w[i + n * W / VEC] : 0;
+        }
+      }
+    }
   }
 }
 
@@ -121,11 +146,12 @@ __device__ inline void store8_q(int8_t *p, L left, const float (&f)[VEC]) {
 }
 
 // Sum of a and maximum of b over the `TPR` threads of a row; every thread of
-// the row gets both.  TPR is a wave or a whole workgroup of more.
+// the row gets both.  TPR is a power of two up to a wave, or a whole workgroup of
+// more.
 template <int TPR>
 __device__ inline void row_reduce(float &a, float &b, float *lds) {
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
+  for (int m = TPR < 64 ? TPR / 2 : 32; m >= 1; m >>= 1) {
     a += __shfl_xor(a, m);
     b = fmaxf(b, __shfl_xor(b, m));
   }
@@ -217,8 +243,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
-          load8_raw(x + c, left(c), xr[v]);
-          if (NORM && a.residual.p) load8_raw(r + c, left(c), rr[v]);
+          load8_raw(x + c, left(c), dim, xr[v]);
+          if (NORM && a.residual.p) load8_raw(r + c, left(c), dim, rr[v]);
         }
       }
     };
@@ -227,7 +253,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
-        if (c < dim) load8_raw(w + c, left(c), wr[v]);
+        if (c < dim) load8_raw(w + c, left(c), dim, wr[v]), settle(left(c), dim, wr[v]);
       }
     }
     for (size_t row = first; row < a.rows; row += step) {
@@ -239,6 +265,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
           float h[VEC];
+          settle(left(c), dim, xr[v]);
+          if (NORM && a.residual.p) settle(left(c), dim, rr[v]);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             h[i] = xr[v][i];
@@ -305,6 +333,8 @@ hipError_t norm_by_size(const NormArgs &a, hipStream_t st) {
   };
   const size_t d = a.dim;
   if (d <= 64 * VEC) return go(k_rms_norm<T, W, 64, 1, NORM, WHOLE>, 64);
+  // (32768 x 1024 to 8 bits and back: 55 us for 72 with 256 threads to a row)
+  if (d <= 64 * VEC * 2) return go(k_rms_norm<T, W, 64, 2, NORM, WHOLE>, 64);
   if (d <= 256 * VEC) return go(k_rms_norm<T, W, 256, 1, NORM, WHOLE>, 256);
   if (d <= 256 * VEC * 2) return go(k_rms_norm<T, W, 256, 2, NORM, WHOLE>, 256);
   if (d <= 256 * VEC * 4) return go(k_rms_norm<T, W, 256, 4, NORM, WHOLE>, 256);
@@ -386,7 +416,8 @@ constexpr size_t BACK_GROUPS = 512;  // two workgroups of rows per CU (three: 56
 // With y = h inv w, inv = (mean h^2 + eps)^(-1/2):
 //   gx = gh + inv gy w - h inv^3 mean(gy w h),  gweight = sum over rows of gy h inv.
 //
-// A workgroup takes rows blockIdx.x, + gridDim.x, ..; each thread keeps the sums
+// A workgroup takes rows in turn, one at a time or, up to a wave's to each, as many
+// as its 256 threads hold; each thread keeps the sums
 // over rows of its columns' gy h inv_rms and writes them to the workgroup's
 // row of `partial`, which k_sum_partial adds up in order.  NV = 0: rows of any
 // length; the sums are then kept in `partial` itself.
@@ -395,9 +426,12 @@ constexpr size_t BACK_GROUPS = 512;  // two workgroups of rows per CU (three: 56
 // sums, 5.0 TB/s (without the next row's loads under way 113 us: eight waves a CU
 // wait for a row, reduce it and write it, in turn).
 template <class T, class W, int TPR, int NV, bool WHOLE>
-__global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
-  __shared__ float lds[2 * 16];
-  const int t = threadIdx.x;
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(NormBackArgs a) {
+  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float lds[ROWS > 1 ? 256 * NV * VEC : 2 * 16];
+  const size_t first = (size_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const size_t step = (size_t)gridDim.x * ROWS;
+  const int t = threadIdx.x % TPR;
   const size_t dim = a.dim;
   auto left = [&](size_t c) {
     if constexpr (WHOLE) return Whole{};
@@ -426,21 +460,21 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
-          load8_raw(gy + c, left(c), yr[v]);
-          load8_raw(h + c, left(c), hr[v]);
-          if (a.gh.p) load8_raw(gh + c, left(c), gr[v]);
+          load8_raw(gy + c, left(c), dim, yr[v]);
+          load8_raw(h + c, left(c), dim, hr[v]);
+          if (a.gh.p) load8_raw(gh + c, left(c), dim, gr[v]);
         }
       }
     };
-    ask(blockIdx.x);
+    if (first < a.rows) ask(first);
     if (w) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
-        if (c < dim) load8_raw(w + c, left(c), wr[v]);
+        if (c < dim) load8_raw(w + c, left(c), dim, wr[v]), settle(left(c), dim, wr[v]);
       }
     }
-    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (size_t row = first; row < a.rows; row += step) {
       T *gx = (T *)a.gx.p + row * a.gx.stride;
       const float inv = inv_next;
       float hv[NV][VEC], g[NV][VEC], o[NV][VEC], dot = 0.f;
@@ -448,6 +482,9 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
+          settle(left(c), dim, yr[v]);
+          settle(left(c), dim, hr[v]);
+          if (a.gh.p) settle(left(c), dim, gr[v]);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             hv[v][i] = hr[v][i];
@@ -459,7 +496,7 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
           }
         }
       }
-      if (row + gridDim.x < a.rows) ask(row + gridDim.x);
+      if (row + step < a.rows) ask(row + step);
       row_reduce<TPR>(dot, none, lds);
       const float k = dot * inv * inv * inv / (float)dim;
 #pragma unroll
@@ -519,7 +556,24 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(NormBackArgs a) {
       }
     }
   }
-  if constexpr (NV > 0) {
+  if constexpr (ROWS > 1) {
+    if (part) {
+      // the sums of the rows side by side, in order
+      constexpr int COLUMNS = TPR * NV * VEC;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          lds[threadIdx.x / TPR * COLUMNS + (v * TPR + t) * VEC + i] = sums[v][i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < COLUMNS && c < (int)dim; c += 256) {
+        float s = lds[c];
+#pragma unroll
+        for (int i = 1; i < ROWS; ++i) s += lds[i * COLUMNS + c];
+        part[c] = s;
+      }
+    }
+  } else if constexpr (NV > 0) {
     if (part) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -554,17 +608,28 @@ k_sum_partial(const float *__restrict__ partial, size_t groups, size_t dim,
 template <class T, class W, bool WHOLE>
 hipError_t back_by_size(const NormBackArgs &args, hipStream_t st) {
   NormBackArgs a = args;
-  // four rows to a group at least: the joining reads as much as a row per group.
-  // One group alone writes the sums themselves.
-  const size_t groups = std::min(norm_back_groups(a.rows), (a.rows + 3) / 4);
-  if (groups == 1) a.partial = a.gweight;
+  size_t groups = 1;
   auto go = [&](auto kernel, int tpr) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(tpr), 0, st, a);
+    // Four rows to a group at least once there is one to a CU: the joining reads as
+    // much as a row per group.  One group alone writes the sums themselves (up to
+    // four rows: one after the other they cost less than the joining's launch).
+    const size_t side = std::max(1, 256 / tpr), turns = (a.rows + side - 1) / side;
+    const size_t quarter = side > 1 ? turns : (turns + 3) / 4;
+    groups = a.rows <= 4 ? 1 : std::max(quarter, std::min(turns, (size_t)std::max(1, device_cus())));
+    groups = std::min(norm_back_groups(a.rows), groups);
+    if (groups == 1) a.partial = a.gweight;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(tpr < 256 ? 256 : tpr), 0, st, a);
     return hipGetLastError();
   };
   const size_t d = a.dim;
   hipError_t e;
-  if (d <= 64 * VEC) e = go(k_rms_norm_backward<T, W, 64, 1, WHOLE>, 64);
+  // (24414 rows of 64: 15 us with the joining, the host's share, for 37 with a wave to
+  // each and one to a workgroup; 32768 of 1024: 44 for 68 with 256 threads to each)
+  if (d <= 8 * VEC) e = go(k_rms_norm_backward<T, W, 8, 1, WHOLE>, 8);
+  else if (d <= 16 * VEC) e = go(k_rms_norm_backward<T, W, 16, 1, WHOLE>, 16);
+  else if (d <= 32 * VEC) e = go(k_rms_norm_backward<T, W, 32, 1, WHOLE>, 32);
+  else if (d <= 64 * VEC) e = go(k_rms_norm_backward<T, W, 64, 1, WHOLE>, 64);
+  else if (d <= 64 * VEC * 2) e = go(k_rms_norm_backward<T, W, 64, 2, WHOLE>, 64);
   else if (d <= 256 * VEC) e = go(k_rms_norm_backward<T, W, 256, 1, WHOLE>, 256);
   else if (d <= 256 * VEC * 2) e = go(k_rms_norm_backward<T, W, 256, 2, WHOLE>, 256);
   else if (d <= 512 * VEC * 2) e = go(k_rms_norm_backward<T, W, 512, 2, WHOLE>, 512);

@@ -219,6 +219,33 @@ def test_norm_backward(dtype, rows, dim, pad, offset):
     assert torch.equal(gw, gw2)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,dim,pad,offset", [
+    (1, 3, 0, 0), (5, 8, 0, 0), (67, 15, 2, 1), (3000, 63, 1, 0), (20000, 64, 8, 0), (31, 65, 0, 0),
+    (900, 128, 0, 0), (1000, 129, 0, 1), (50, 250, 0, 0), (4100, 256, 8, 0), (600, 257, 0, 0),
+    (1030, 1000, 0, 0), (1029, 1021, 3, 1), (300, 1025, 0, 0), (60, 9001, 0, 0)])
+def test_norm_of_short_and_ragged_rows(dtype, rows, dim, pad, offset):
+    """Rows side by side in a workgroup, and rows that end at any place of a vector:
+    both directions."""
+    x, r, gy = (normal(24 + i, rows, dim, dtype, s) for i, s in ((0, 1.0), (1, 2.0), (2, 0.5)))
+    w = (1 + 0.3 * torch.randn(dim, generator=gen(27))).to(dtype)
+    y, h, inv = R.rms_norm(placed(x, pad, offset), w.cuda(), EPS, residual=placed(r, pad, offset))
+    want_h, want_inv, want_y = norm64(x, r, w, EPS)
+    e = chain(dim) * E
+    within(inv, want_inv, e * want_inv)
+    within(h, want_h, U[dtype] * want_h.abs() + TINY[dtype])
+    within(y, want_y, (U[dtype] + 2 * e) * want_y.abs() + TINY[dtype])
+    gx, gw = R.rms_norm_backward(placed(gy, pad, offset), placed(h.cpu(), pad, offset), w.cuda(), inv,
+                                 gh=placed(r, pad, offset))
+    H, GY, GH, W, I = (t.cpu().to(D) for t in (h, gy, r, w, inv))
+    want, want_w = norm_back64(GY, GH, H, I, W)
+    I = I[:, None]
+    size = GH.abs() + (GY * W * I).abs() + H.abs() * I ** 3 * (GY * W * H).abs().mean(1, keepdim=True)
+    within(gx, want, U[dtype] * want.abs() + 2 * e * size + TINY[dtype])
+    # at most rows / 512 terms to a thread, 32 rows side by side, 512 groups by 16
+    within(gw, want_w, (rows / 512 + 96) * E * (GY * H * I).abs().sum(0))
+
+
 # ------------------------------------------------------------- product ---
 
 def int8(seed, rows, cols):
