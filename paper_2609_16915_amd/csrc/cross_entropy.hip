@@ -12,6 +12,7 @@
 // Products of 16-bit numbers summed in 32 bits; statistics in 32 bits.  gl alone is
 // rounded to 16 bits between two steps, which keeps its products on the matrix
 // pipes at full rate and costs at most half a unit in its last place.
+#include <algorithm>
 #include <cmath>
 
 #include "mma_tile.hpp"
@@ -20,21 +21,26 @@ namespace rosetta {
 
 namespace {
 
-// Tiles of many rows, and of few rows or short ones.
-template <int BX_, int BY_, int WX_, int WY_>
+// Tiles of many rows, and of few rows or short ones; the latter's steps loaded four
+// ahead where there is one to a CU at most.
+template <int BX_, int BY_, int WX_, int WY_, int STAGES_>
 struct Shape {
   static constexpr int BX = BX_, BY = BY_, WX = WX_, WY = WY_, THREADS = 64 * WX * WY;
+  static constexpr int STAGES = STAGES_;
 };
-using Large = Shape<256, 256, 4, 2>;
-using Small = Shape<128, 128, 4, 2>;
-template <class T, class S>
-using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY>;
+using Large = Shape<256, 256, 4, 2, 2>;
+using Small = Shape<128, 128, 4, 2, 2>;
+using Deep = Shape<128, 128, 4, 2, 4>;
+template <class T, class S, bool YA = false>
+using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY, S::STAGES, false, YA>;
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
 
 size_t up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 size_t tiles(size_t a, size_t b) { return (a + b - 1) / b; }
+// Small tiles that have a CU each.
+size_t few_tiles() { return (size_t)std::max(1, device_cus()); }
 
 struct Stat {
   float top, sum;
@@ -49,6 +55,11 @@ __device__ inline Stat join(Stat a, Stat b) {
 
 __device__ inline bool counts(int64_t target, int64_t ignore, size_t vocab) {
   return target != ignore && target >= 0 && target < (int64_t)vocab;
+}
+
+// Row `row`, or the last where there is none: what is read for it is not used.
+__device__ inline int64_t row_in(const LossArgs &a, int64_t row) {
+  return row < (int64_t)a.rows ? row : (int64_t)a.rows - 1;
 }
 
 template <class T>
@@ -74,6 +85,13 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
   const unsigned gx = (unsigned)((a.vocab + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  int64_t target[Tl::TY];
+  auto ask = [&] {
+#pragma unroll
+    for (int j = 0; j < Tl::TY; ++j)
+      target[j] = a.targets[row_in(a, (int64_t)ty * BY + Tl::y_at() + 16 * j)];
+  };
+  if constexpr (Tl::ROOM) ask();
   v4f acc[Tl::TX][Tl::TY];
   Tl::template run<ALIGNED>({w_rows<T>(a), h_rows<T>(a), (int64_t)tx * BX, (int64_t)ty * BY, 0,
                              (int64_t)(a.dim * sizeof(T))},
@@ -88,18 +106,13 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
         for (int j = 0; j < Tl::TY; ++j) acc[i / 4][j][i % 4] = -INFINITY;
       }
   }
-  int64_t target[Tl::TY];
-#pragma unroll
-  for (int j = 0; j < Tl::TY; ++j) {
-    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-    target[j] = row < (int64_t)a.rows ? a.targets[row] : -1;
-  }
+  if constexpr (!Tl::ROOM) ask();
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int y = Tl::y_at() + 16 * j;
     const int64_t row = (int64_t)ty * BY + y;
     const int64_t at = target[j] < 0 ? -1 : target[j] - x0;
-    if (at >= 0 && at < RUN && x0 + at < (int64_t)a.vocab) {
+    if (at >= 0 && at < RUN && x0 + at < (int64_t)a.vocab && row < (int64_t)a.rows) {
 #pragma unroll
       for (int i = 0; i < RUN; ++i)
         if (at == i) at_target[row] = acc[i / 4][j][i % 4];
@@ -213,17 +226,37 @@ k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
 // down to 2^-28.
 __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   const int threads = blockDim.x;
-  float top = 0.f;
-  for (size_t t = threadIdx.x; t < a.rows; t += threads)
-    if (counts(a.targets[t], a.ignore_index, a.vocab)) top = fmaxf(top, fabsf(a.gloss[t]));
+  constexpr int AHEAD = 8;
+  // rows first, + threads, .. : gloss of those that count, else 0
+  auto read = [&](size_t first, float (&g)[AHEAD]) {
+    int64_t target[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const size_t t = first + (size_t)i * threads, in = t < a.rows ? t : a.rows - 1;
+      target[i] = t < a.rows ? a.targets[in] : -1;
+      g[i] = a.gloss[in];
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (!counts(target[i], a.ignore_index, a.vocab)) g[i] = 0.f;
+  };
+  float top = 0.f, g[AHEAD];
+  for (size_t t = threadIdx.x; t < a.rows; t += (size_t)threads * AHEAD) {
+    read(t, g);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, fabsf(g[i]));
+  }
   for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = top;
   __syncthreads();
   for (int w = 0; w < threads / 64; ++w) top = fmaxf(top, lds[w]);
   const bool some = top > 0.f;
-  for (size_t t = threadIdx.x; t < a.rows; t += threads) {
-    const float g = counts(a.targets[t], a.ignore_index, a.vocab) ? a.gloss[t] : 0.f;
-    coef[t] = some ? g / top * GL_UP : g;
+  for (size_t t = threadIdx.x; t < a.rows; t += (size_t)threads * AHEAD) {
+    if (a.rows > (size_t)threads * AHEAD) read(t, g);  // (else they are still there)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (t + (size_t)i * threads < a.rows)
+        coef[t + (size_t)i * threads] = some ? g[i] / top * GL_UP : g[i];
   }
   if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
 }
@@ -241,28 +274,31 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, const float *__r
   const unsigned gx = (unsigned)((here + BX - 1) / BX), gy = (unsigned)((a.rows + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
+  // what the epilogue reads, all before it writes anything
+  float coefs[Tl::TY], lses[Tl::TY];
+  int64_t target[Tl::TY];
+  auto ask = [&] {
+#pragma unroll
+    for (int j = 0; j < Tl::TY; ++j) {
+      const int64_t row = row_in(a, (int64_t)ty * BY + Tl::y_at() + 16 * j);
+      coefs[j] = coef[row];
+      lses[j] = a.lse[row];
+      target[j] = a.targets[row];
+    }
+  };
+  if constexpr (Tl::ROOM) ask();
   v4f acc[Tl::TX][Tl::TY];
   Tl::template run<ALIGNED>({w_rows<T>(a), h_rows<T>(a), (int64_t)(v0 + (size_t)tx * BX),
                              (int64_t)ty * BY, 0, (int64_t)(a.dim * sizeof(T))},
                             lds, acc);
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
   const int64_t left = (int64_t)a.vocab - (int64_t)v0 - x0;  // words of the run that exist
-  // (all that is read, before anything is written)
-  float coefs[Tl::TY], lses[Tl::TY];
-  int64_t target[Tl::TY];
-#pragma unroll
-  for (int j = 0; j < Tl::TY; ++j) {
-    const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
-    const bool in = row < (int64_t)a.rows;
-    coefs[j] = in ? coef[row] : 0.f;
-    lses[j] = in ? a.lse[row] * LOG2E : 0.f;
-    target[j] = in ? a.targets[row] : -1;
-  }
+  if constexpr (!Tl::ROOM) ask();
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
     if (row >= (int64_t)a.rows) continue;
-    const float c = coefs[j], lse = lses[j];
+    const float c = coefs[j], lse = lses[j] * LOG2E;
     const int64_t at = target[j] < 0 ? -1 : target[j] - (int64_t)v0 - x0;
     float f[RUN];
     // (c = 0: a row that takes no part, whatever its logits are)
@@ -393,22 +429,40 @@ k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restr
   }
 }
 
-template <class T>
+// The parts added up, four columns to each of 256 / P threads, P threads a run of the
+// parts each.  (42 rows of 256, 180 parts: 4 us with 16, 27 with one.)
+template <class T, int P>
 __global__ void __launch_bounds__(256)
 k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t dim,
                const float *__restrict__ coef, T *__restrict__ out, size_t out_stride) {
-  const size_t quads = (dim + 3) / 4, i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= quads * rows) return;
+  constexpr int Q = 256 / P;
+  __shared__ float lds[P > 1 ? P : 1][Q][4];
+  const size_t quads = (dim + 3) / 4, i = (size_t)blockIdx.x * Q + threadIdx.x % Q;
+  const int p = threadIdx.x / Q, each = (splits + P - 1) / P;
   const size_t row = i / quads, c = i % quads * 4;
   const int64_t left = (int64_t)(dim - c);
+  const bool in = i < quads * rows;
   float s[4] = {};
+  if (in) {
+    const int end = (p + 1) * each < splits ? (p + 1) * each : splits;
 #pragma unroll 4
-  for (int q = 0; q < splits; ++q) {
-    float f[4];
-    load_run(part + ((size_t)q * rows + row) * dim + c, left, f);
+    for (int q = p * each; q < end; ++q) {
+      float f[4];
+      load_run(part + ((size_t)q * rows + row) * dim + c, left, f);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += f[e];
+      for (int e = 0; e < 4; ++e) s[e] += f[e];
+    }
   }
+  if constexpr (P > 1) {
+    __builtin_memcpy(lds[p][threadIdx.x % Q], s, sizeof s);
+    __syncthreads();
+    if (p > 0) return;
+#pragma unroll
+    for (int q = 1; q < P; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += lds[q][threadIdx.x % Q][e];
+  }
+  if (!in) return;
   const float back = coef[rows];
 #pragma unroll
   for (int e = 0; e < 4; ++e) s[e] *= back;
@@ -422,19 +476,19 @@ __global__ void __launch_bounds__(S::THREADS)
 k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                const float *__restrict__ coef, const T *__restrict__ gl,
                const T *__restrict__ h_t) {
-  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, 2, false, true>;
+  using Tl = TileOf<T, S, true>;
   constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((a.dim + BX - 1) / BX), gy = (unsigned)((here + BY - 1) / BY);
   unsigned tx, ty;
   band_tile(xcd_block(blockIdx.x, gridDim.x), gx, gy, tx, ty);
   const int64_t ld_h = (int64_t)(ld_t * sizeof(T)), ld_g = (int64_t)(vp * sizeof(T));
+  const float back = coef[a.rows];
   v4f acc[Tl::TX][Tl::TY];
   Tl::template run<true>({{(const char *)h_t, ld_h, (int64_t)a.dim, ld_h},
                           {(const char *)gl, ld_g, (int64_t)a.rows, ld_g},
                           (int64_t)tx * BX, (int64_t)ty * BY, 0, (int64_t)(a.rows * sizeof(T))},
                          lds, acc);
-  const float back = coef[a.rows];
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
   if (left <= 0) return;
 #pragma unroll
@@ -448,10 +502,13 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
   }
 }
 
-// Rows of h that Thin takes, bound by w's bytes like any other way, and w's rows in
-// its blocks.  Short rows (less than half a step for each of a block's waves)
-// would leave most of its waves idle.
-size_t thin_rows(size_t dim) { return 2 * dim >= 8 * STEP ? 32 : 0; }
+// Whether Thin takes the logits, bound by w's bytes like any other way, and w's rows
+// in its blocks.  Short rows (less than half a step for each of a block's waves) would
+// leave most of its waves idle; past 16 rows it pays where w is too few tiles for the
+// chip (32 rows of 4096 over 8000: 19 us for 51; over 128000: 273 for 221).
+bool thin(size_t rows, size_t dim, size_t vocab) {
+  return 2 * dim >= 8 * STEP && (rows <= 16 || (rows <= 32 && tiles(vocab, 128) <= few_tiles()));
+}
 constexpr size_t thin_x(size_t rows) { return rows <= 16 ? 64 : 32; }
 // Whether large tiles take the logits: one a CU at half the cost, small ones two,
 // whose ends overlap; in steps of a large tile (777 rows of 768 over 50257: 421 us
@@ -464,7 +521,7 @@ bool large(size_t rows, size_t dim, size_t vocab) {
   return l <= s;
 }
 size_t forward_x(size_t rows, size_t dim, size_t vocab) {
-  return rows <= thin_rows(dim) ? thin_x(rows) : large(rows, dim, vocab) ? Large::BX : Small::BX;
+  return thin(rows, dim, vocab) ? thin_x(rows) : large(rows, dim, vocab) ? Large::BX : Small::BX;
 }
 
 // Pieces of the vocabulary and what the workspace holds.
@@ -539,10 +596,11 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
     LAUNCH(k, dim3((unsigned)(nx * tiles(a.rows, S::BY))), S::THREADS,
            (TileOf<T, S>::LDS), a, part, at_target);
   };
-  const bool thin = a.rows <= thin_rows(a.dim);
-  if (thin && a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
-  else if (thin) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
+  const bool few = thin(a.rows, a.dim, a.vocab);
+  if (few && a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
+  else if (few) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
   else if (large(a.rows, a.dim, a.vocab)) tile(Large{});
+  else if (aligned(a) && nx * tiles(a.rows, Deep::BY) <= few_tiles()) tile(Deep{});
   else tile(Small{});
   // (few rows: more threads to each)
   if (a.rows <= 64) LAUNCH(k_loss_join<2>, dim3((unsigned)tiles(a.rows, 2)), 1024, 0, a, part, nx, at_target);
@@ -564,9 +622,16 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
          256, 0, a, coef, h_t, p.ld_t);
   for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
-    auto k = al ? k_loss_grad_tile<T, S, true> : k_loss_grad_tile<T, S, false>;
-    LAUNCH(k, dim3((unsigned)(tiles(here, BX) * tiles(a.rows, BY))), S::THREADS, Tl::LDS, a, v0, here,
-           p.vp, coef, gl);
+    const size_t many = tiles(here, BX) * tiles(a.rows, BY);
+    if (BX == Deep::BX && al && many <= few_tiles())
+      LAUNCH((k_loss_grad_tile<T, Deep, true>), dim3((unsigned)many), S::THREADS,
+             (TileOf<T, Deep>::LDS), a, v0, here, p.vp, coef, gl);
+    else if (al)
+      LAUNCH((k_loss_grad_tile<T, S, true>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here,
+             p.vp, coef, gl);
+    else
+      LAUNCH((k_loss_grad_tile<T, S, false>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here,
+             p.vp, coef, gl);
     if (a.gh) {
       const T *w = (const T *)a.w + v0 * a.w_stride;
       const dim3 grid((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY)));
@@ -580,13 +645,24 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
                gl, w_t, p.vp, part, p.run, i > 0);
       }
     }
-    if (a.gw)
-      LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)(tiles(a.dim, BX) * tiles(here, BY))), S::THREADS,
-             Tl::LDS, a, v0, here, p.vp, p.ld_t, coef, gl, h_t);
+    if (a.gw) {
+      const size_t many = tiles(a.dim, BX) * tiles(here, BY);
+      if (BX == Deep::BX && many <= few_tiles())
+        LAUNCH((k_loss_gw_tile<T, Deep>), dim3((unsigned)many), S::THREADS, (TileOf<T, Deep>::LDS), a,
+               v0, here, p.vp, p.ld_t, coef, gl, h_t);
+      else
+        LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here, p.vp,
+               p.ld_t, coef, gl, h_t);
+    }
   }
-  if (a.gh)
-    LAUNCH(k_loss_gh_join<T>, dim3((unsigned)tiles(tiles(a.dim, 4) * a.rows, 256)), 256, 0, part,
-           (int)p.splits, a.rows, a.dim, coef, (T *)a.gh, a.gh_stride);
+  if (a.gh) {
+    // (many parts of few outputs: sixteen threads to each)
+    const size_t quads = tiles(a.dim, 4) * a.rows;
+    const bool few = p.splits >= 32 && quads < ((size_t)1 << 16);
+    auto k = few ? k_loss_gh_join<T, 16> : k_loss_gh_join<T, 1>;
+    LAUNCH(k, dim3((unsigned)tiles(quads, few ? 16 : 256)), 256, 0, part, (int)p.splits, a.rows,
+           a.dim, coef, (T *)a.gh, a.gh_stride);
+  }
   return e;
 }
 

@@ -171,6 +171,9 @@ struct Tile {
   static constexpr int LDS = STAGES * STAGE;  // what the stages take
   static constexpr int LOADS = (BX + BY) / 8 / WAVES;  // of 8 rows, per wave and stage
   static_assert((BX + BY) / 8 % WAVES == 0 && BX / 8 % WAVES == 0, "loads divide evenly");
+  // whether registers are left for what an epilogue reads to be asked for before the
+  // products
+  static constexpr bool ROOM = TX * TY <= 8;
   using Acc = typename Mma<T>::Acc;
 
   __device__ static int key_x(int row) {

@@ -429,6 +429,18 @@ def test_cross_entropy_large(dtype, rows, dim, vocab, pad):
                targets(70, rows, vocab, 500), g, -100, dtype, pad, dev="cuda")
 
 
+@pytest.mark.parametrize("dtype,rows,dim,vocab,pad", [
+    (BF16, 64, 1024, 3000, 0), (F16, 100, 1032, 2500, 8), (F16, 2500, 64, 500, 0),
+    (BF16, 4500, 192, 700, 0), (F16, 42, 256, 50000, 0), (BF16, 20, 520, 34000, 0),
+    (BF16, 24, 1024, 3000, 0), (F16, 3, 704, 40000, 0)])
+def test_cross_entropy_of_few_tiles_and_few_rows(dtype, rows, dim, vocab, pad):
+    """Few enough tiles that each has a CU, sums over many rows, many parts of few
+    outputs, and rows that weigh unlike each other."""
+    g = torch.exp(2 * torch.randn(rows, generator=gen(76))) / rows
+    check_loss(normal(77, rows, dim, dtype), normal(78, vocab, dim, dtype, 2.0 / math.sqrt(dim)),
+               targets(79, rows, vocab, rows // 9), g, -100, dtype, pad, dev="cuda")
+
+
 def test_cross_entropy_targets_out_of_range():
     rows, dim, vocab = 40, 64, 100
     t = targets(70, rows, vocab)
