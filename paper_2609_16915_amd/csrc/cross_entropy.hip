@@ -261,13 +261,13 @@ __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
 }
 
-// gl [rows][vp] of the vocabulary rows [v0, v0 + here), `here` rounded up to whole
+// gl [rows][vp] of the vocabulary rows [v0, v0 + here), `w`, and of h, `here` rounded up to whole
 // tiles, zeros beyond the vocabulary.  As k_loss_tile, and gl's bytes at the tiles'
 // ends: 4096 x 4096 over 128000 in 3.3-3.4 ms.
-template <class T, class S, bool ALIGNED>
+template <class T, class S>
 __global__ void __launch_bounds__(S::THREADS)
-k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, const float *__restrict__ coef,
-                 T *__restrict__ gl) {
+k_loss_grad_tile(LossArgs a, Operand w, Operand h, size_t v0, size_t here, size_t vp,
+                 const float *__restrict__ coef, T *__restrict__ gl) {
   using Tl = TileOf<T, S>;
   constexpr int BX = S::BX, BY = S::BY, RUN = 4 * Tl::TX;
   extern __shared__ char lds[];
@@ -288,9 +288,7 @@ k_loss_grad_tile(LossArgs a, size_t v0, size_t here, size_t vp, const float *__r
   };
   if constexpr (Tl::ROOM) ask();
   v4f acc[Tl::TX][Tl::TY];
-  Tl::template run<ALIGNED>({w_rows<T>(a), h_rows<T>(a), (int64_t)(v0 + (size_t)tx * BX),
-                             (int64_t)ty * BY, 0, (int64_t)(a.dim * sizeof(T))},
-                            lds, acc);
+  Tl::template run<true>({w, h, (int64_t)tx * BX, (int64_t)ty * BY, 0, w.bytes}, lds, acc);
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
   const int64_t left = (int64_t)a.vocab - (int64_t)v0 - x0;  // words of the run that exist
   if constexpr (!Tl::ROOM) ask();
@@ -356,14 +354,16 @@ __device__ inline void transpose(const T *in, size_t in_stride, size_t rows, siz
   }
 }
 
-// w_t of a piece of the vocabulary.
+// Rows that lie so that tiles can take them: `ld` apart, a multiple of 8 and the
+// next to their length, zeros at their ends.  Bound by memory.
 template <class T>
 __global__ void __launch_bounds__(256)
-k_loss_wt(const T *__restrict__ w, size_t w_stride, size_t here, size_t dim, T *__restrict__ w_t,
-          size_t vp) {
-  __shared__ T lds[64][72];
-  transpose(w, w_stride, here, dim, w_t, vp, blockIdx.x, blockIdx.y, lds,
-            [](size_t) { return true; });
+k_loss_pack(const T *__restrict__ in, size_t in_stride, size_t rows, size_t dim,
+            T *__restrict__ out, size_t ld) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / (ld / 8), c = i % (ld / 8) * 8;
+  if (row >= rows) return;
+  *(v4i *)(out + row * ld + c) = load_frag((const char *)(in + row * in_stride), c * sizeof(T),
+                                           dim * sizeof(T));
 }
 
 // What comes before the pieces: the factors (block 0), and h_t in tiles (the
@@ -383,47 +383,39 @@ k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t l
 }
 
 // part[split][row][d] (+)= gl [rows][vp] times the piece's `here` rows of w: split s
-// takes an equal run of them, perhaps none of the last.  ACROSS: w as it lies;
-// else w_t [dim][vp].  4096 x 4096 over 128000 in 2.96-3.03 ms, 1.42-1.45 PFLOP/s (with
-// w_t for aligned rows too 3.1 and 0.4 for turning it).
-template <class T, class S, bool ACROSS>
+// takes an equal run of them, perhaps none of the last.  4096 x 4096 over 128000 in
+// 2.96-3.03 ms, 1.42-1.45 PFLOP/s (with w turned first 3.1 and 0.4 for turning it).
+template <class T, class S>
 __global__ void __launch_bounds__(S::THREADS)
-k_loss_gh_tile(size_t rows, size_t dim, size_t here, size_t vp, const T *__restrict__ gl,
-               const T *__restrict__ w, size_t w_stride, float *__restrict__ part, size_t run,
-               int add) {
-  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, 2, ACROSS>;
+k_loss_gh_tile(size_t rows, size_t dim, size_t vp, const T *__restrict__ gl, Operand w,
+               float *__restrict__ part, size_t run, int add) {
+  using Tl = Tile<T, S::BX, S::BY, S::WX, S::WY, 2, true>;
   constexpr int BX = S::BX, BY = S::BY;
   extern __shared__ char lds[];
   const unsigned gx = (unsigned)((dim + BX - 1) / BX), gy = (unsigned)((rows + BY - 1) / BY);
   const unsigned b = xcd_block(blockIdx.x, gridDim.x), split = b / (gx * gy);
   unsigned tx, ty;
   band_tile(b % (gx * gy), gx, gy, tx, ty);
-  // (not ACROSS: whole 16 bytes, gl and w_t have zeros there)
-  const int64_t ld = (int64_t)vp * sizeof(T);
-  const int64_t bytes = (int64_t)(ACROSS ? here : (here + 7) / 8 * 8) * sizeof(T);
+  const int64_t ld = (int64_t)vp * sizeof(T), bytes = w.rows * (int64_t)sizeof(T);
   const int64_t k0 = (int64_t)(split * run * sizeof(T)), k1 = k0 + (int64_t)(run * sizeof(T));
-  const Operand X = ACROSS ? Operand{(const char *)w, (int64_t)(w_stride * sizeof(T)),
-                                     (int64_t)here, (int64_t)(dim * sizeof(T))}
-                           : Operand{(const char *)w, ld, (int64_t)dim, bytes};
   v4f acc[Tl::TX][Tl::TY];
-  Tl::template run<true>({X, {(const char *)gl, ld, (int64_t)rows, bytes}, (int64_t)tx * BX,
+  Tl::template run<true>({w, {(const char *)gl, ld, (int64_t)rows, bytes}, (int64_t)tx * BX,
                           (int64_t)ty * BY, k0, k1 < bytes ? k1 : bytes},
                          lds, acc);
-  constexpr int RUN = ACROSS ? 4 : 4 * Tl::TX;  // neighbouring x of a lane
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at();
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t row = (int64_t)ty * BY + Tl::y_at() + 16 * j;
     if (row >= (int64_t)rows) continue;
 #pragma unroll
-    for (int i = 0; i < 4 * Tl::TX / RUN; ++i) {
+    for (int i = 0; i < Tl::TX; ++i) {
       const int64_t x = x0 + 16 * i, left = (int64_t)dim - x;
       if (left <= 0) continue;
       float *out = part + ((size_t)split * rows + row) * dim + x;
-      float f[RUN] = {};
+      float f[4] = {};
       if (add) load_run(out, left, f);
 #pragma unroll
-      for (int e = 0; e < RUN; ++e) f[e] += acc[i + e / 4][j][e % 4];
+      for (int e = 0; e < 4; ++e) f[e] += acc[i][j][e];
       store_run<false>(out, left, f);
     }
   }
@@ -527,7 +519,7 @@ size_t forward_x(size_t rows, size_t dim, size_t vocab) {
 // Pieces of the vocabulary and what the workspace holds.
 struct Plan {
   size_t vp, pieces, ld_t, splits, run;
-  size_t coef, gl, w_t, h_t, part, bytes;
+  size_t ld, coef, gl, w, h, h_t, part, bytes;
 };
 
 template <class S>
@@ -536,7 +528,8 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   constexpr size_t BUDGET = (size_t)1 << 30;
   Plan p{};
   p.ld_t = up(rows, 64);
-  const size_t column = 2 * (rows + dim);
+  p.ld = up(dim, 8);
+  const size_t column = 2 * (rows + p.ld);
   size_t vp = BUDGET / column / BX * BX;
   // (at most 2^20: a tile's rows of gl within 32-bit offsets of its first)
   vp = vp < BX ? BX : vp > ((size_t)1 << 20) ? (size_t)1 << 20 : vp;
@@ -559,7 +552,8 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   };
   p.coef = take((rows + 1) * 4);
   p.gl = take(rows * p.vp * 2);
-  p.w_t = take(dim * p.vp * 2);
+  p.w = take(p.ld * p.vp * 2);
+  p.h = take(p.ld * rows * 2);
   p.h_t = take(dim * p.ld_t * 2);
   p.part = take(p.splits * rows * dim * 4);
   p.bytes = at;
@@ -615,36 +609,33 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   const Plan p = plan<S>(a.rows, a.dim, a.vocab);
   char *ws = (char *)a.workspace;
   float *coef = (float *)(ws + p.coef), *part = (float *)(ws + p.part);
-  T *gl = (T *)(ws + p.gl), *w_t = (T *)(ws + p.w_t), *h_t = (T *)(ws + p.h_t);
+  T *gl = (T *)(ws + p.gl), *w_p = (T *)(ws + p.w), *h_p = (T *)(ws + p.h), *h_t = (T *)(ws + p.h_t);
   const bool al = aligned(a);
   hipError_t e = hipSuccess;
   LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(p.ld_t, 64) * tiles(a.dim, 64) : 0))),
          256, 0, a, coef, h_t, p.ld_t);
+  // rows of h or of a piece of w as the tiles take them
+  auto rows_of = [&](const void *at, size_t stride, size_t rows, T *packed) {
+    const int64_t bytes = (int64_t)(p.ld * sizeof(T));
+    if (al) return Operand{(const char *)at, (int64_t)(stride * sizeof(T)), (int64_t)rows, bytes};
+    LAUNCH(k_loss_pack<T>, dim3((unsigned)tiles(rows * (p.ld / 8), 256)), 256, 0, (const T *)at,
+           stride, rows, a.dim, packed, p.ld);
+    return Operand{(const char *)packed, bytes, (int64_t)rows, bytes};
+  };
+  const Operand h = rows_of(a.h, a.h_stride, a.rows, h_p);
   for (size_t i = 0; i < p.pieces && e == hipSuccess; ++i) {
     const size_t v0 = i * p.vp, here = a.vocab - v0 < p.vp ? a.vocab - v0 : p.vp;
+    const Operand w = rows_of((const T *)a.w + v0 * a.w_stride, a.w_stride, here, w_p);
     const size_t many = tiles(here, BX) * tiles(a.rows, BY);
-    if (BX == Deep::BX && al && many <= few_tiles())
-      LAUNCH((k_loss_grad_tile<T, Deep, true>), dim3((unsigned)many), S::THREADS,
-             (TileOf<T, Deep>::LDS), a, v0, here, p.vp, coef, gl);
-    else if (al)
-      LAUNCH((k_loss_grad_tile<T, S, true>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here,
-             p.vp, coef, gl);
+    if (BX == Deep::BX && many <= few_tiles())
+      LAUNCH((k_loss_grad_tile<T, Deep>), dim3((unsigned)many), S::THREADS, (TileOf<T, Deep>::LDS), a,
+             w, h, v0, here, p.vp, coef, gl);
     else
-      LAUNCH((k_loss_grad_tile<T, S, false>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here,
+      LAUNCH((k_loss_grad_tile<T, S>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, w, h, v0, here,
              p.vp, coef, gl);
-    if (a.gh) {
-      const T *w = (const T *)a.w + v0 * a.w_stride;
-      const dim3 grid((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY)));
-      if (al) {
-        LAUNCH((k_loss_gh_tile<T, S, true>), grid, S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp,
-               gl, w, a.w_stride, part, p.run, i > 0);
-      } else {
-        LAUNCH(k_loss_wt<T>, dim3((unsigned)tiles(p.vp, 64), (unsigned)tiles(a.dim, 64)), 256, 0, w,
-               a.w_stride, here, a.dim, w_t, p.vp);
-        LAUNCH((k_loss_gh_tile<T, S, false>), grid, S::THREADS, Tl::LDS, a.rows, a.dim, here, p.vp,
-               gl, w_t, p.vp, part, p.run, i > 0);
-      }
-    }
+    if (a.gh)
+      LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))),
+             S::THREADS, Tl::LDS, a.rows, a.dim, p.vp, gl, w, part, p.run, i > 0);
     if (a.gw) {
       const size_t many = tiles(a.dim, BX) * tiles(here, BY);
       if (BX == Deep::BX && many <= few_tiles())
