@@ -315,7 +315,7 @@ k_loss_grad_tile(LossArgs a, Operand w, Operand h, size_t v0, size_t here, size_
       for (int i = 0; i < RUN; ++i)
         if (i >= left) f[i] = 0.f;
     }
-    store_run<false>(gl + row * (int64_t)vp + x0, RUN, f);
+    store_run(gl + row * (int64_t)vp + x0, RUN, f);
   }
 }
 
@@ -416,7 +416,7 @@ k_loss_gh_tile(size_t rows, size_t dim, size_t vp, const T *__restrict__ gl, Ope
       if (add) load_run(out, left, f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] += acc[i][j][e];
-      store_run<false>(out, left, f);
+      store_run(out, left, f);
     }
   }
 }
@@ -458,7 +458,7 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
   const float back = coef[rows];
 #pragma unroll
   for (int e = 0; e < 4; ++e) s[e] *= back;
-  store_run<false>(out + row * out_stride + c, left, s);
+  store_run(out + row * out_stride + c, left, s);
 }
 
 // gw rows [v0, v0 + here) = gl [rows][vp] the other way, times h_t [dim][ld_t].  4096 x
@@ -483,6 +483,7 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                          lds, acc);
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
   if (left <= 0) return;
+  const bool past = past_caches((const T *)a.gw, a.gw_stride);
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t v = (int64_t)v0 + (int64_t)ty * BY + Tl::y_at() + 16 * j;
@@ -490,7 +491,7 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
     float f[RUN];
 #pragma unroll
     for (int i = 0; i < RUN; ++i) f[i] = acc[i / 4][j][i % 4] * back;
-    store_run<true>((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f);
+    store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f, past);
   }
 }
 

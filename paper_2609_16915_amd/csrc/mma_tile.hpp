@@ -159,7 +159,7 @@ __device__ inline v4i load_frag(const char *row, int64_t at, int64_t end) {
 //
 // RUNS false: row m of fragment i of a wave's X is its row 16 i + m, and a lane's
 // accumulators are runs of 4 x, four lanes' next to each other: 32-bit outputs then
-// leave 64 bytes together (4096 x 4096 x 4096 bytes to f32: 68 us for 152 with each
+// leave 64 bytes together (4096 x 4096 x 4096 bytes to f32: 62 us for 73 with each
 // lane's 16 bytes alone in their 64; in 16 bits a lane's runs are 32 bytes, and lanes
 // that trade halves for 64 gained nothing).
 template <class T, int BX, int BY, int WX, int WY, int STAGES = 2, bool XA = false, bool YA = false,
@@ -514,25 +514,36 @@ __device__ inline void load_run(const float *p, int64_t left, float (&f)[N]) {
   }
 }
 
-// N consecutive values at p, of which the first `left` are written.  LAST: nobody
-// reads them here again, so they need not stay in the caches (235 MB of a product's
-// outputs, 8192 x 14336: 394 us for 418).
-template <bool LAST, class T, int N>
-__device__ inline void store_run(T *p, int64_t left, const float (&f)[N]) {
+// Whether rows that nobody reads here again may go past the caches: where they begin
+// and end with whole pieces of 64 bytes, or what is written of a piece goes out alone
+// (40000 rows of 3520 in 16 bits: 176 us past the caches, 198 through them; of 3511
+// 453 and 356).
+template <class T>
+__device__ inline bool past_caches(const T *p, size_t stride) {
+  return (((uintptr_t)p | stride * sizeof(T)) & 63) == 0;
+}
+
+// N consecutive values at p, of which the first `left` are written; `past`: past the
+// caches.
+template <class T, int N>
+__device__ inline void store_run(T *p, int64_t left, const float (&f)[N], bool past = false) {
   T v[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = (T)f[i];
   if (left >= N) {
-    if constexpr (LAST && sizeof v % 16 == 0) {
-      using v4u = __attribute__((ext_vector_type(4), aligned(2))) int;
+    // (16 bytes at a time, at any address)
+    using v4u = __attribute__((ext_vector_type(4), aligned(2))) int;
+    static_assert(sizeof v % 16 == 0 || N == 4);
+    if constexpr (sizeof v % 16) {
+      __builtin_memcpy(p, v, sizeof v);
+    } else {
 #pragma unroll
       for (int i = 0; i < (int)(sizeof v / 16); ++i) {
         v4u w;
         __builtin_memcpy(&w, (const char *)v + 16 * i, 16);
-        __builtin_nontemporal_store(w, (v4u *)p + i);
+        if (past) __builtin_nontemporal_store(w, (v4u *)p + i);
+        else ((v4u *)p)[i] = w;
       }
-    } else {
-      __builtin_memcpy(p, v, sizeof v);
     }
   } else {
 #pragma unroll

@@ -22,7 +22,7 @@ __device__ inline void put4(const Q8Args &a, int64_t y, int64_t x, v4i s) {
     const int64_t c = x + r < (int64_t)a.n ? x + r : (int64_t)a.n - 1;
     f[r] = (float)s[r] * as * a.b_scale[c] + (a.bias ? a.bias[c] : 0.f);
   }
-  store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x, (int64_t)a.n - x, f);
+  store_run((O *)a.out + y * (int64_t)a.out_stride + x, (int64_t)a.n - x, f);
 }
 
 // Part `split` of the sums, rows of n rounded up to 4.
@@ -34,7 +34,9 @@ template <class O, int BX, int BY, int STAGES>
 using Q8Tile = Tile<int8_t, BX, BY, 4, 2, STAGES, false, false, sizeof(O) == 2>;
 
 // `run`: bytes of the rows per split, all of them in one.  8192 x 14336 x 4096 takes
-// 395 us (2.44 POP/s; 235 MB of outputs leave at the ends of seven rounds of tiles).
+// 386 us (2.49 POP/s; 235 MB of outputs leave at the ends of seven rounds of tiles).
+// Outputs past the caches: 380 us there and 686 for 706 over 8192 bytes, but 236 for
+// 190 over 16384 x 16384 x 128 and 61 for 58 over 4096 x 4096 x 4096; so through them.
 template <class O, bool ALIGNED, int BX, int BY, int STAGES>
 __global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) {
   using Tl = Q8Tile<O, BX, BY, STAGES>;
@@ -86,7 +88,7 @@ __global__ void __launch_bounds__(512) k_q8_tile(Q8Args a, int splits, int run) 
 #pragma unroll
       for (int i = 0; i < RUN; ++i)
         f[i] = (float)acc[c + i / 4][j][i % 4] * as[j] * bs[c][i] + bias[c][i];
-      store_run<true>((O *)a.out + y * (int64_t)a.out_stride + x0 + 16 * c, left - 16 * c, f);
+      store_run((O *)a.out + y * (int64_t)a.out_stride + x0 + 16 * c, left - 16 * c, f);
     }
   }
 }
