@@ -463,7 +463,7 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
 
 // gw rows [v0, v0 + here) = gl [rows][vp] the other way, times h_t [dim][ld_t].  4096 x
 // 4096 over 128000 in 3.2-3.3 ms with gw's 1 GB, 1.30-1.34 PFLOP/s.
-template <class T, class S>
+template <class T, class S, bool PAST>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                const float *__restrict__ coef, const T *__restrict__ gl,
@@ -483,7 +483,6 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
                          lds, acc);
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
   if (left <= 0) return;
-  const bool past = past_caches((const T *)a.gw, a.gw_stride);
 #pragma unroll
   for (int j = 0; j < Tl::TY; ++j) {
     const int64_t v = (int64_t)v0 + (int64_t)ty * BY + Tl::y_at() + 16 * j;
@@ -491,7 +490,7 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
     float f[RUN];
 #pragma unroll
     for (int i = 0; i < RUN; ++i) f[i] = acc[i / 4][j][i % 4] * back;
-    store_run((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f, past);
+    store_run<PAST>((T *)a.gw + v * (int64_t)a.gw_stride + x0, left, f);
   }
 }
 
@@ -639,12 +638,15 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
              S::THREADS, Tl::LDS, a.rows, a.dim, p.vp, gl, w, part, p.run, i > 0);
     if (a.gw) {
       const size_t many = tiles(a.dim, BX) * tiles(here, BY);
-      if (BX == Deep::BX && many <= few_tiles())
-        LAUNCH((k_loss_gw_tile<T, Deep>), dim3((unsigned)many), S::THREADS, (TileOf<T, Deep>::LDS), a,
-               v0, here, p.vp, p.ld_t, coef, gl, h_t);
-      else
-        LAUNCH((k_loss_gw_tile<T, S>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, v0, here, p.vp,
+      auto gw = [&](auto shape) {
+        using G = decltype(shape);
+        auto k = past_caches((const T *)a.gw, a.gw_stride) ? k_loss_gw_tile<T, G, true>
+                                                           : k_loss_gw_tile<T, G, false>;
+        LAUNCH(k, dim3((unsigned)many), G::THREADS, (TileOf<T, G, true>::LDS), a, v0, here, p.vp,
                p.ld_t, coef, gl, h_t);
+      };
+      if (BX == Deep::BX && many <= few_tiles()) gw(Deep{});
+      else gw(S{});
     }
   }
   if (a.gh) {

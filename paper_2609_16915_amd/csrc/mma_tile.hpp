@@ -519,14 +519,15 @@ __device__ inline void load_run(const float *p, int64_t left, float (&f)[N]) {
 // (40000 rows of 3520 in 16 bits: 176 us past the caches, 198 through them; of 3511
 // 453 and 356).
 template <class T>
-__device__ inline bool past_caches(const T *p, size_t stride) {
+inline bool past_caches(const T *p, size_t stride) {
   return (((uintptr_t)p | stride * sizeof(T)) & 63) == 0;
 }
 
-// N consecutive values at p, of which the first `left` are written; `past`: past the
-// caches.
-template <class T, int N>
-__device__ inline void store_run(T *p, int64_t left, const float (&f)[N], bool past = false) {
+// N consecutive values at p, of which the first `left` are written; PAST: past the
+// caches.  (A branch at run time would leave both ways through them: the compiler
+// takes the two stores for one.)
+template <bool PAST = false, class T, int N>
+__device__ inline void store_run(T *p, int64_t left, const float (&f)[N]) {
   T v[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = (T)f[i];
@@ -541,7 +542,7 @@ __device__ inline void store_run(T *p, int64_t left, const float (&f)[N], bool p
       for (int i = 0; i < (int)(sizeof v / 16); ++i) {
         v4u w;
         __builtin_memcpy(&w, (const char *)v + 16 * i, 16);
-        if (past) __builtin_nontemporal_store(w, (v4u *)p + i);
+        if constexpr (PAST) __builtin_nontemporal_store(w, (v4u *)p + i);
         else ((v4u *)p)[i] = w;
       }
     }
