@@ -591,8 +591,12 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
            (TileOf<T, S>::LDS), a, part, at_target);
   };
   const bool few = thin(a.rows, a.dim, a.vocab);
-  if (few && a.rows <= 16) LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
-  else if (few) LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
+  if (few && a.rows <= 16)
+    LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part,
+           at_target);
+  else if (few)
+    LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part,
+           at_target);
   else if (large(a.rows, a.dim, a.vocab)) tile(Large{});
   else if (aligned(a) && nx * tiles(a.rows, Deep::BY) <= few_tiles()) tile(Deep{});
   else tile(Small{});
