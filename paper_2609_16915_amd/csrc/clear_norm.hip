@@ -454,7 +454,6 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
     auto ask = [&](size_t row) {
       const T *gy = (const T *)a.gy.p + row * a.gy.stride;
       const T *h = (const T *)a.h.p + row * a.h.stride;
-      const T *gh = (const T *)a.gh.p + row * a.gh.stride;
       inv_next = a.inv_rms[row];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -462,11 +461,22 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
         if (c < dim) {
           load8_raw(gy + c, left(c), dim, yr[v]);
           load8_raw(h + c, left(c), dim, hr[v]);
-          if (a.gh.p) load8_raw(gh + c, left(c), dim, gr[v]);
         }
       }
     };
+    // (gh is used last, so it is asked for once the row before is written and stays as
+    // it lies: widened ahead with the others, long rows no longer fit the registers,
+    // 1258 x 16320 in 32 bits 148 us for 106)
+    auto ask_gh = [&](size_t row) {
+      const T *gh = (const T *)a.gh.p + row * a.gh.stride;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const size_t c = ((size_t)v * TPR + t) * VEC;
+        if (c < dim) load8_raw(gh + c, left(c), dim, gr[v]);
+      }
+    };
     if (first < a.rows) ask(first);
+    if (first < a.rows && a.gh.p) ask_gh(first);
     if (w) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -477,14 +487,13 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
     for (size_t row = first; row < a.rows; row += step) {
       T *gx = (T *)a.gx.p + row * a.gx.stride;
       const float inv = inv_next;
-      float hv[NV][VEC], g[NV][VEC], o[NV][VEC], dot = 0.f;
+      float hv[NV][VEC], g[NV][VEC], dot = 0.f;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
           settle(left(c), dim, yr[v]);
           settle(left(c), dim, hr[v]);
-          if (a.gh.p) settle(left(c), dim, gr[v]);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             hv[v][i] = hr[v][i];
@@ -492,7 +501,6 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
             sums[v][i] = fmaf(g[v][i] * inv, hv[v][i], sums[v][i]);
             if (w) g[v][i] *= wr[v][i];
             dot = fmaf(g[v][i], hv[v][i], dot);
-            o[v][i] = a.gh.p ? gr[v][i] : 0.f;
           }
         }
       }
@@ -503,11 +511,15 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
       for (int v = 0; v < NV; ++v) {
         const size_t c = ((size_t)v * TPR + t) * VEC;
         if (c < dim) {
+          float o[VEC];
+          if (a.gh.p) settle(left(c), dim, gr[v]);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) o[v][i] += g[v][i] * inv - hv[v][i] * k;
-          store8(gx + c, left(c), o[v]);
+          for (int i = 0; i < VEC; ++i)
+            o[i] = (a.gh.p ? gr[v][i] : 0.f) + (g[v][i] * inv - hv[v][i] * k);
+          store8(gx + c, left(c), o);
         }
       }
+      if (a.gh.p && row + step < a.rows) ask_gh(row + step);
     }
   } else {
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
