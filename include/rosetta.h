@@ -608,8 +608,9 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
  *    held in 32 bits; 8-bit products are summed exactly.
  *  - 8-bit rows: value = scale[row] * q, q in [-127, 127], scale = max |value|
  *    / 127, rounded to nearest, ties to even.  A row of zeros has scale 0; a
- *    row with a NaN or an infinity (or whose squares overflow 32 bits, in
- *    the norm) has a scale that is not finite, or NaN, and unspecified q.
+ *    row with a NaN or an infinity, be it of the weight (or whose squares
+ *    overflow 32 bits, in the norm) has a scale that is not finite, or NaN,
+ *    and unspecified q.
  *  - Outputs must not overlap inputs or each other (ROSETTA_ERR_ALIAS) unless
  *    stated.  rows == 0 is a successful no-op once sizes are valid, except
  *    that gradients of weights are then zeros.

@@ -145,15 +145,18 @@ __device__ inline void store8_q(int8_t *p, L left, const float (&f)[VEC]) {
   }
 }
 
-// Sum of a and maximum of b over the `TPR` threads of a row; every thread of
-// the row gets both.  TPR is a power of two up to a wave, or a whole workgroup of
+// The larger of two, or NaN if either is (fmaxf gives the other one): one instruction.
+__device__ inline float max_or_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// Sum of a and maximum of b (NaN if any is) over the `TPR` threads of a row; every thread
+// of the row gets both.  TPR is a power of two up to a wave, or a whole workgroup of
 // more.
 template <int TPR>
 __device__ inline void row_reduce(float &a, float &b, float *lds) {
 #pragma unroll
   for (int m = TPR < 64 ? TPR / 2 : 32; m >= 1; m >>= 1) {
     a += __shfl_xor(a, m);
-    b = fmaxf(b, __shfl_xor(b, m));
+    b = max_or_nan(b, __shfl_xor(b, m));
   }
   if constexpr (TPR > 64) {
     constexpr int W = TPR / 64;
@@ -169,7 +172,7 @@ __device__ inline void row_reduce(float &a, float &b, float *lds) {
 #pragma unroll
     for (int w = 1; w < W; ++w) {
       a += lds[2 * w];
-      b = fmaxf(b, lds[2 * w + 1]);
+      b = max_or_nan(b, lds[2 * w + 1]);
     }
   }
 }
@@ -205,9 +208,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
   auto count = [&](const float (&h)[VEC], const float (&hw)[VEC]) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      // (a NaN reaches the sum, and the scale through it)
+      // (a NaN of h or of the weight reaches the maximum, and the scale through it; an
+      // infinity to 8 bits without the norm the sum, so that its scale is NaN)
       sum = NORM ? fmaf(h[i], h[i], sum) : sum + h[i] * 0.f;
-      top = fmaxf(top, fabsf(hw[i]));
+      top = max_or_nan(top, fabsf(hw[i]));
     }
   };
   auto finish = [&](size_t row) {
