@@ -36,6 +36,10 @@ using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY, S::STAGES, false, YA>;
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
+// Rows of h that are turned together: the pitch of what they give stays within a
+// tile's offsets.
+constexpr size_t H_ROWS = (size_t)1 << 20;
+static_assert((int64_t)(H_ROWS * 2) <= MAX_LD && H_ROWS % 64 == 0, "");
 
 size_t up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 size_t tiles(size_t a, size_t b) { return (a + b - 1) / b; }
@@ -367,7 +371,7 @@ k_loss_pack(const T *__restrict__ in, size_t in_stride, size_t rows, size_t dim,
 }
 
 // What comes before the pieces: the factors (block 0), and h_t in tiles (the
-// others; none where gw is not wanted).
+// others; none where gw is not wanted), [dim][ld_t] for every H_ROWS rows.
 template <class T>
 __global__ void __launch_bounds__(256)
 k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t ld_t) {
@@ -376,10 +380,12 @@ k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t l
     loss_coef(a, coef, (float *)lds);
     return;
   }
-  const size_t across = (ld_t + 63) / 64, b = blockIdx.x - 1;
+  const size_t across = (a.rows + 63) / 64, b = blockIdx.x - 1;
+  const size_t r0 = b % across * 64 / H_ROWS * H_ROWS;
   // (a row that takes no part, whatever it holds, is zeros: NaN times 0 is NaN)
-  transpose((const T *)a.h, a.h_stride, a.rows, a.dim, h_t, ld_t, b % across, b / across, lds,
-            [&](size_t row) { return counts(a.targets[row], a.ignore_index, a.vocab); });
+  transpose((const T *)a.h + r0 * a.h_stride, a.h_stride, a.rows - r0, a.dim, h_t + r0 * a.dim, ld_t,
+            b % across - r0 / 64, b / across, lds,
+            [&](size_t row) { return counts(a.targets[r0 + row], a.ignore_index, a.vocab); });
 }
 
 // part[split][row][d] (+)= gl [rows][vp] times the piece's `here` rows of w: split s
@@ -461,8 +467,8 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
   store_run(out + row * out_stride + c, left, s);
 }
 
-// gw rows [v0, v0 + here) = gl [rows][vp] the other way, times h_t [dim][ld_t].  4096 x
-// 4096 over 128000 in 3.2-3.3 ms with gw's 1 GB, 1.30-1.34 PFLOP/s.
+// gw rows [v0, v0 + here) = gl [rows][vp] the other way, times h_t [dim][ld_t] of every
+// H_ROWS rows.  4096 x 4096 over 128000 in 3.2-3.3 ms with gw's 1 GB, 1.30-1.34 PFLOP/s.
 template <class T, class S, bool PAST>
 __global__ void __launch_bounds__(S::THREADS)
 k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
@@ -477,10 +483,14 @@ k_loss_gw_tile(LossArgs a, size_t v0, size_t here, size_t vp, size_t ld_t,
   const int64_t ld_h = (int64_t)(ld_t * sizeof(T)), ld_g = (int64_t)(vp * sizeof(T));
   const float back = coef[a.rows];
   v4f acc[Tl::TX][Tl::TY];
-  Tl::template run<true>({{(const char *)h_t, ld_h, (int64_t)a.dim, ld_h},
-                          {(const char *)gl, ld_g, (int64_t)a.rows, ld_g},
-                          (int64_t)tx * BX, (int64_t)ty * BY, 0, (int64_t)(a.rows * sizeof(T))},
-                         lds, acc);
+  Tl::clear(acc);
+  for (size_t r0 = 0; r0 < a.rows; r0 += H_ROWS) {
+    const size_t rows = a.rows - r0 < H_ROWS ? a.rows - r0 : H_ROWS;
+    Tl::template add<true>({{(const char *)(h_t + r0 * a.dim), ld_h, (int64_t)a.dim, ld_h},
+                            {(const char *)(gl + r0 * vp), ld_g, (int64_t)rows, ld_g},
+                            (int64_t)tx * BX, (int64_t)ty * BY, 0, (int64_t)(rows * sizeof(T))},
+                           lds, acc);
+  }
   const int64_t x0 = (int64_t)tx * BX + Tl::x_at(), left = (int64_t)a.dim - x0;
   if (left <= 0) return;
 #pragma unroll
@@ -527,7 +537,7 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   constexpr size_t BX = S::BX, BY = S::BY;
   constexpr size_t BUDGET = (size_t)1 << 30;
   Plan p{};
-  p.ld_t = up(rows, 64);
+  p.ld_t = up(std::min(rows, H_ROWS), 64);
   p.ld = up(dim, 8);
   const size_t column = 2 * (rows + p.ld);
   size_t vp = BUDGET / column / BX * BX;
@@ -554,7 +564,7 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
   p.gl = take(rows * p.vp * 2);
   p.w = take(p.ld * p.vp * 2);
   p.h = take(p.ld * rows * 2);
-  p.h_t = take(dim * p.ld_t * 2);
+  p.h_t = take(tiles(rows, H_ROWS) * dim * p.ld_t * 2);
   p.part = take(p.splits * rows * dim * 4);
   p.bytes = at;
   return p;
@@ -616,7 +626,7 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   T *gl = (T *)(ws + p.gl), *w_p = (T *)(ws + p.w), *h_p = (T *)(ws + p.h), *h_t = (T *)(ws + p.h_t);
   const bool al = aligned(a);
   hipError_t e = hipSuccess;
-  LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(p.ld_t, 64) * tiles(a.dim, 64) : 0))),
+  LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(a.rows, 64) * tiles(a.dim, 64) : 0))),
          256, 0, a, coef, h_t, p.ld_t);
   // rows of h or of a piece of w as the tiles take them
   auto rows_of = [&](const void *at, size_t stride, size_t rows, T *packed) {

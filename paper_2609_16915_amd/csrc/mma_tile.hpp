@@ -63,11 +63,14 @@ struct Operand {
   int64_t bytes;
 };
 
-// Whether rows can be brought in by 16 bytes at a time straight to LDS (a
-// tile's rows within 32-bit offsets of its first).
+// The furthest that rows brought in straight to LDS may be apart: a tile's 256 then
+// lie, with their 2^30 bytes at most, within 31-bit offsets of its first.
+constexpr int64_t MAX_LD = (int64_t)1 << 22;
+
+// Whether rows can be brought in by 16 bytes at a time straight to LDS.
 inline bool rows_aligned(const Operand &o) {
-  return (uintptr_t)o.p % FRAG == 0 && o.ld % FRAG == 0 && o.bytes % FRAG == 0 &&
-         o.ld <= (int64_t)1 << 22 && o.bytes <= (int64_t)1 << 30;
+  return (uintptr_t)o.p % FRAG == 0 && o.ld % FRAG == 0 && o.bytes % FRAG == 0 && o.ld <= MAX_LD &&
+         o.bytes <= (int64_t)1 << 30;
 }
 
 // Memory at `base`, for buffer loads (raw, 32-bit offsets).
@@ -185,18 +188,33 @@ struct Tile {
 
   // A tile: rows [x0, x0 + BX) of X and [y0, y0 + BY) of Y over bytes [k0, k1)
   // of the rows (k0 a multiple of 16; ALIGNED: k1 too).  x0 < X.rows and y0 <
-  // Y.rows: a tile has a row at least, or its loads would leave the matrix.
+  // Y.rows: a tile has a row at least, or its loads would leave the matrix.  ALIGNED:
+  // ld at most MAX_LD.
   struct Place {
     Operand X, Y;
     int64_t x0, y0, k0, k1;
   };
 
-  // The tile's sums.  The stages are free when it returns.  (Blocks that go through
+  __device__ static void clear(Acc (&acc)[TX][TY]) {
+#pragma unroll
+    for (int i = 0; i < TX; ++i)
+#pragma unroll
+      for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+  }
+
+  // The tile's sums, and their addition to what is there.
+  template <bool ALIGNED>
+  __device__ static void run(const Place &p, char *lds, Acc (&acc)[TX][TY]) {
+    clear(acc);
+    add<ALIGNED>(p, lds, acc);
+  }
+
+  // The stages are free when it returns.  (Blocks that go through
   // several tiles, the next one's first loads under the present one's epilogue,
   // gained 2 % with the barest epilogue and lost 1-8 % with the real ones, whose
   // values then no longer fit the registers.)
   template <bool ALIGNED>
-  __device__ static void run(const Place &p, char *lds, Acc (&acc)[TX][TY]) {
+  __device__ static void add(const Place &p, char *lds, Acc (&acc)[TX][TY]) {
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wx = wave % WX, wy = wave / WX;
@@ -206,10 +224,6 @@ struct Tile {
     const int key = (m >> 1) & 7;
     const int atx = (wx * (BX / WX) + (RUNS ? (m / 4) * 4 * TX + m % 4 : m)) * STEP;
     const int aty = (BX + wy * (BY / WY) + m) * STEP;
-#pragma unroll
-    for (int i = 0; i < TX; ++i)
-#pragma unroll
-      for (int j = 0; j < TY; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     if (p.k0 >= p.k1) return;
     static_assert(!(XA || YA) || (sizeof(T) == 2 && ALIGNED), "");
     // Fragment f of this wave's part, across: rows of `width` bytes at `at`, their

@@ -1,10 +1,12 @@
 """Edges of the clear side on the GPU."""
+import math
+
 import pytest
 
 from paper_2609_16915_amd import rosetta as R
 
 from gpu_helpers import require_gpu
-from test_gpu_clear import BF16, EPS, F16, F32, normal
+from test_gpu_clear import BF16, D, E, EPS, F16, F32, TINY, U, normal, within
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -40,3 +42,56 @@ def test_norm_weight_of_nan_and_infinity(dtype, dim):
             if h is x:  # the weight has no part in these
                 assert torch.equal(o.inv_rms, inv0) and torch.equal(o.h, h0)
             assert not torch.isfinite(R.dequantize_rows(o.q, o.scale, F32))[:, at].any()
+
+
+# ---------------------------------------------------------------- loss ---
+
+@pytest.fixture
+def given_back():
+    """What the test took of the card's memory is free again."""
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,rows,dim,vocab", [(BF16, 8_700_001, 512, 250),
+                                                  (F16, 17_000_003, 128, 100)])
+def test_cross_entropy_gradients_of_millions_of_rows(given_back, dtype, rows, dim, vocab):
+    """More rows than a row of h, turned, may hold with 256 (128) of them in 32-bit
+    offsets; bounds as for any other sum of 32-bit terms (test_gpu_clear.check_loss).
+    A row's word goes by the sign of its last column, so that this column of gw, the
+    furthest one, is large against its bound."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    h = torch.empty((rows, dim), dtype=dtype, device="cuda")
+    for r in range(0, rows, 1 << 20):
+        h[r:r + (1 << 20)] = torch.randn(h[r:r + (1 << 20)].shape, generator=g, device="cuda")
+    w = normal(4, vocab, dim, dtype, 1.0 / math.sqrt(dim)).cuda()
+    t = torch.randint(0, vocab // 2, (rows,), generator=g, device="cuda") * 2 + (h[:, -1] > 0)
+    t[::7] = -100
+    c = torch.rand(rows, generator=g, device="cuda") / rows
+    loss, lse = R.cross_entropy(h, w, t)
+    gh, gw = R.cross_entropy_backward(h, w, t, lse, c)
+    u, W = U[dtype], w.to(D)
+    want = torch.zeros((vocab, dim), dtype=D, device="cuda")
+    bound = torch.zeros_like(want)
+    for r in range(0, rows, 1 << 19):
+        rs = slice(r, r + (1 << 19))
+        H, counts = h[rs].to(D), t[rs] >= 0
+        logits = H @ W.t().contiguous()
+        lse64 = torch.logsumexp(logits, 1)
+        delta = 4 * E * math.sqrt(dim) * H.norm(dim=1) * W.norm(dim=1).max() \
+            + 64 * E * (1 + lse64.abs() + logits.abs().amax(1))
+        within(lse[rs], lse64, delta)
+        p = torch.exp(logits - lse64[:, None])
+        f = torch.where(counts, c[rs].to(D), 0.0)[:, None]
+        gl = p.clone()
+        gl.scatter_add_(1, t[rs].clamp(min=0)[:, None], torch.full_like(f, -1.0))
+        gl, p = gl * f, p * f
+        off = u * gl.abs() + p * 2 * delta[:, None] + float(c.max()) * 2.0 ** -39
+        want_h = gl @ W
+        within(gh[rs], want_h, u * want_h.abs() + (off + 64 * E * gl.abs()) @ W.abs() + TINY[dtype])
+        want += gl.t().contiguous() @ H
+        bound += (off + 64 * E * gl.abs()).t().contiguous() @ H.abs()
+    bound += u * want.abs() + TINY[dtype]
+    assert (want[:, -1].abs() > 10 * bound[:, -1]).all()
+    within(gw, want, bound)
