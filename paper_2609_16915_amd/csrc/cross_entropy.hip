@@ -227,7 +227,8 @@ k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
 // GL_UP: the term -1 of a target is then exact in either type where all rows
 // weigh the same (rounding gloss itself put one error on all of them: gradients
 // off by 0.0026 of their norm, 0.0017 so), and f16 has room for probabilities
-// down to 2^-28.
+// down to 2^-28.  The largest of those that are finite: one that is not would be
+// everybody's factor, and stays its own row's this way.
 __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   const int threads = blockDim.x;
   constexpr int AHEAD = 8;
@@ -248,7 +249,8 @@ __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   for (size_t t = threadIdx.x; t < a.rows; t += (size_t)threads * AHEAD) {
     read(t, g);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, fabsf(g[i]));
+    for (int i = 0; i < AHEAD; ++i)
+      if (fabsf(g[i]) < INFINITY) top = fmaxf(top, fabsf(g[i]));
   }
   for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = top;

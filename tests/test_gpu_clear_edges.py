@@ -6,7 +6,7 @@ import pytest
 from paper_2609_16915_amd import rosetta as R
 
 from gpu_helpers import require_gpu
-from test_gpu_clear import BF16, D, E, EPS, F16, F32, TINY, U, normal, within
+from test_gpu_clear import BF16, D, E, EPS, F16, F32, TINY, U, gen, normal, targets, within
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -95,3 +95,61 @@ def test_cross_entropy_gradients_of_millions_of_rows(given_back, dtype, rows, di
     bound += u * want.abs() + TINY[dtype]
     assert (want[:, -1].abs() > 10 * bound[:, -1]).all()
     within(gw, want, bound)
+
+
+def loss_case(dtype, rows, dim, vocab, pad=0, mean=0.0):
+    """Hidden states, head, targets; `mean` of all words but the targets' in the head, so
+    that a row's softmax part of gh stands apart from its target's."""
+    h = normal(10, rows, dim, dtype)
+    w = normal(11, vocab, dim, D, 1.0 / math.sqrt(dim))
+    t = targets(12, rows, max(1, vocab // 8), rows // 9)
+    w[vocab // 8:] += mean
+    return h, w.to(dtype), t
+
+
+def check_gh_by_row(dtype, h, w, t, g, judged):
+    """gh of the rows `judged`, each against its own factor: f16 holds gl in half steps of
+    2^-38 of the row's factor, or of 2^-63 of the largest where that is more (bf16 in
+    relative ones)."""
+    td, gd = t.cuda(), g.cuda()
+    _, lse = R.cross_entropy(h.cuda(), w.cuda(), td)
+    gh, gw = R.cross_entropy_backward(h.cuda(), w.cuda(), td, lse, gd)
+    H, W, G = h.cuda().to(D)[judged], w.cuda().to(D), gd.to(D)
+    t, valid = td[judged], (td >= 0)[judged]
+    logits = H @ W.t().contiguous()
+    lse = torch.logsumexp(logits, 1)
+    delta = 4 * E * math.sqrt(h.shape[1]) * H.norm(dim=1) * W.norm(dim=1).max() \
+        + 64 * E * (1 + lse.abs() + logits.abs().amax(1))
+    p = torch.exp(logits - lse[:, None])
+    f = torch.where(valid, G[judged], 0.0)[:, None]
+    gl = p.clone()
+    gl.scatter_add_(1, t.clamp(min=0)[:, None], torch.full_like(f, -1.0))
+    gl, p, u = gl * f, p * f.abs(), U[dtype]
+    top = G[torch.isfinite(G) & (td >= 0)].abs().max()
+    off = u * gl.abs() + p * 2 * delta[:, None]
+    if dtype == F16:
+        off += torch.maximum(f.abs() * 2.0 ** -38, top * 2.0 ** -63)
+    want = gl @ W
+    within(gh[judged], want,
+           u * want.abs() + (off + 64 * E * gl.abs()) @ W.abs() + TINY[dtype] + 2.0 ** -140)
+    return gh, gw, want
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,dim,vocab", [(20, 64, 300), (9, 1024, 2000), (500, 256, 4000),
+                                            (4000, 640, 8100)])
+@pytest.mark.parametrize("fill", [float("inf"), float("-inf"), float("nan")])
+def test_cross_entropy_factor_of_infinity_stays_in_its_row(dtype, rows, dim, vocab, fill):
+    """A factor that is not finite: its row's gh and gw are not, the other rows' are what
+    they are without it."""
+    h, w, t = loss_case(dtype, rows, dim, vocab)
+    g = 0.5 + torch.rand(rows, generator=gen(13))
+    t[3] = 1
+    g[3] = fill
+    judged = torch.arange(rows, device="cuda") != 3
+    gh, gw, _ = check_gh_by_row(dtype, h, w, t, g, judged)
+    assert not torch.isfinite(gh[3]).any() and not torch.isfinite(gw).any()
+    # ignored, it has no part in anything
+    t[3] = -100
+    gh, gw, _ = check_gh_by_row(dtype, h, w, t, g, judged)
+    assert not gh[3].any() and torch.isfinite(gw).all()
