@@ -695,7 +695,9 @@ size_t rosetta_cross_entropy_workspace_bytes(size_t rows, size_t dim, size_t voc
  * (of type `dtype`; either may be NULL).  Rows that are ignored, or whose
  * target is outside [0, vocab), take no part.  The logits are made again, a
  * piece of the vocabulary at a time; gl is held for one piece, in multiples of
- * the largest finite |gloss|, rounded to `dtype`.  workspace:
+ * the largest finite |gloss|, rounded to `dtype`; in f16, whose range is short,
+ * gh takes each row of it on a power of two of its own (rows down to 2^-24 of
+ * the largest factor keep their precision), gw all rows on one.  workspace:
  * rosetta_cross_entropy_backward_workspace_bytes bytes. */
 rosetta_status rosetta_cross_entropy_backward(const void *h, size_t h_stride, const void *w,
                                               size_t w_stride, int dtype, const int64_t *targets,

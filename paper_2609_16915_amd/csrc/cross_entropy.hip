@@ -14,6 +14,7 @@
 // pipes at full rate and costs at most half a unit in its last place.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mma_tile.hpp"
 
@@ -36,6 +37,9 @@ using TileOf = Tile<T, S::BX, S::BY, S::WX, S::WY, S::STAGES, false, YA>;
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float GL_UP = 0x1p14f;  // largest |gl| as it is held
+// Powers of two by which a row of gl that weighs little is held larger than the others.
+template <class T>
+constexpr int ROW_UP = std::is_same_v<T, f16> ? 24 : 0;
 // Rows of h that are turned together: the pitch of what they give stays within a
 // tile's offsets.
 constexpr size_t H_ROWS = (size_t)1 << 20;
@@ -223,12 +227,17 @@ k_loss_join(LossArgs a, const Stat *__restrict__ part, size_t nt,
 }
 
 // Factors of the rows of gl, coef[row], and what their products are multiplied
-// by in the end, coef[rows].  gl is held in 16 bits as multiples of max |gloss| /
+// by in the end, coef[rows] and coef[rows + 2 + row]; coef[rows + 1]: whether any of
+// the latter is not 1.  gl is held in 16 bits as multiples of max |gloss| /
 // GL_UP: the term -1 of a target is then exact in either type where all rows
 // weigh the same (rounding gloss itself put one error on all of them: gradients
 // off by 0.0026 of their norm, 0.0017 so), and f16 has room for probabilities
 // down to 2^-28.  The largest of those that are finite: one that is not would be
-// everybody's factor, and stays its own row's this way.
+// everybody's factor, and stays its own row's this way.  In f16 a row that weighs less
+// than half of the largest is held up to 2^24 times larger for gh (at 2^-24 of the largest
+// its probabilities below 2^-15 would be lost otherwise), and brought to the common factor
+// for gw, which sums over the rows: half a step is 2^-39 of the largest factor there.
+template <class T>
 __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   const int threads = blockDim.x;
   constexpr int AHEAD = 8;
@@ -257,14 +266,32 @@ __device__ inline void loss_coef(const LossArgs &a, float *coef, float *lds) {
   __syncthreads();
   for (int w = 0; w < threads / 64; ++w) top = fmaxf(top, lds[w]);
   const bool some = top > 0.f;
+  bool unlike = false;
   for (size_t t = threadIdx.x; t < a.rows; t += (size_t)threads * AHEAD) {
     if (a.rows > (size_t)threads * AHEAD) read(t, g);  // (else they are still there)
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (t + (size_t)i * threads < a.rows)
-        coef[t + (size_t)i * threads] = some ? g[i] / top * GL_UP : g[i];
+    for (int i = 0; i < AHEAD; ++i) {
+      const size_t row = t + (size_t)i * threads;
+      if (row >= a.rows) continue;
+      float c = some ? g[i] / top * GL_UP : g[i];
+      if constexpr (ROW_UP<T> > 0) {
+        int up = 0;
+        if (some && c != 0.f && fabsf(c) < GL_UP) {
+          (void)frexpf(c / GL_UP, &up);  // (its exponent, at most 0)
+          up = up < -ROW_UP<T> ? ROW_UP<T> : -up;
+        }
+        c = ldexpf(c, up);
+        coef[a.rows + 2 + row] = ldexpf(1.f, -up);
+        unlike |= up != 0;
+      }
+      coef[row] = c;
+    }
   }
-  if (threadIdx.x == 0) coef[a.rows] = some ? top / GL_UP : 1.f;
+  unlike = __syncthreads_or(unlike);
+  if (threadIdx.x == 0) {
+    coef[a.rows] = some ? top / GL_UP : 1.f;
+    coef[a.rows + 1] = unlike ? 1.f : 0.f;
+  }
 }
 
 // gl [rows][vp] of the vocabulary rows [v0, v0 + here), `w`, and of h, `here` rounded up to whole
@@ -379,7 +406,7 @@ __global__ void __launch_bounds__(256)
 k_loss_begin(LossArgs a, float *__restrict__ coef, T *__restrict__ h_t, size_t ld_t) {
   __shared__ T lds[64][72];
   if (blockIdx.x == 0) {
-    loss_coef(a, coef, (float *)lds);
+    loss_coef<T>(a, coef, (float *)lds);
     return;
   }
   const size_t across = (a.rows + 63) / 64, b = blockIdx.x - 1;
@@ -429,13 +456,44 @@ k_loss_gh_tile(size_t rows, size_t dim, size_t vp, const T *__restrict__ gl, Ope
   }
 }
 
+// gl, `width` columns of it, to the rows' common factor; by all blocks of 256 threads.
+// Where they have it already, the usual case, nothing but a word is read.
+template <class T>
+__device__ inline void common_factor(const float *coef, size_t rows, size_t width, size_t vp, T *gl) {
+  if (coef[rows + 1] == 0.f) return;
+  const size_t each = width / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * each;
+       i += (size_t)gridDim.x * 256) {
+    const size_t row = i / each;
+    const float down = coef[rows + 2 + row];
+    if (down == 1.f) continue;
+    T v[8], *at = gl + row * vp + i % each * 8;
+    *(v4i *)v = *(const v4i *)at;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (T)((float)v[e] * down);
+    *(v4i *)at = *(const v4i *)v;
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+k_loss_common(const float *__restrict__ coef, size_t rows, size_t width, size_t vp,
+              T *__restrict__ gl) {
+  common_factor(coef, rows, width, vp, gl);
+}
+
 // The parts added up, four columns to each of 256 / P threads, P threads a run of the
-// parts each.  (42 rows of 256, 180 parts: 4 us with 16, 27 with one.)
+// parts each.  (42 rows of 256, 180 parts: 4 us with 16, 27 with one.)  With `gl`, the
+// last piece of it also goes to the common factor: a launch of its own would take 4 us.
 template <class T, int P>
 __global__ void __launch_bounds__(256)
 k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t dim,
-               const float *__restrict__ coef, T *__restrict__ out, size_t out_stride) {
+               const float *__restrict__ coef, T *__restrict__ out, size_t out_stride,
+               T *__restrict__ gl, size_t width, size_t vp) {
   constexpr int Q = 256 / P;
+  if constexpr (ROW_UP<T> > 0) {
+    if (gl) common_factor(coef, rows, width, vp, gl);
+  }
   __shared__ float lds[P > 1 ? P : 1][Q][4];
   const size_t quads = (dim + 3) / 4, i = (size_t)blockIdx.x * Q + threadIdx.x % Q;
   const int p = threadIdx.x / Q, each = (splits + P - 1) / P;
@@ -466,6 +524,11 @@ k_loss_gh_join(const float *__restrict__ part, int splits, size_t rows, size_t d
   const float back = coef[rows];
 #pragma unroll
   for (int e = 0; e < 4; ++e) s[e] *= back;
+  if constexpr (ROW_UP<T> > 0) {
+    const float down = coef[rows + 2 + row];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] *= down;
+  }
   store_run(out + row * out_stride + c, left, s);
 }
 
@@ -562,7 +625,7 @@ Plan plan(size_t rows, size_t dim, size_t vocab) {
     at += up(bytes, 256);
     return here;
   };
-  p.coef = take((rows + 1) * 4);
+  p.coef = take((2 * rows + 2) * 4);
   p.gl = take(rows * p.vp * 2);
   p.w = take(p.ld * p.vp * 2);
   p.h = take(p.ld * rows * 2);
@@ -652,6 +715,20 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
     if (a.gh)
       LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))),
              S::THREADS, Tl::LDS, a.rows, a.dim, p.vp, gl, w, part, p.run, i > 0);
+    const size_t width = up(here, BX);
+    if (a.gh && i + 1 == p.pieces) {
+      // (many parts of few outputs: sixteen threads to each)
+      const size_t quads = tiles(a.dim, 4) * a.rows;
+      const bool few = p.splits >= 32 && quads < ((size_t)1 << 16);
+      auto k = few ? k_loss_gh_join<T, 16> : k_loss_gh_join<T, 1>;
+      LAUNCH(k, dim3((unsigned)tiles(quads, few ? 16 : 256)), 256, 0, part, (int)p.splits, a.rows,
+             a.dim, coef, (T *)a.gh, a.gh_stride, a.gw ? gl : nullptr, width, p.vp);
+    } else if constexpr (ROW_UP<T> > 0) {
+      if (a.gw)
+        LAUNCH(k_loss_common<T>,
+               dim3((unsigned)std::min((size_t)1024, tiles(a.rows * width, 8 * 256))), 256, 0, coef,
+               a.rows, width, p.vp, gl);
+    }
     if (a.gw) {
       const size_t many = tiles(a.dim, BX) * tiles(here, BY);
       auto gw = [&](auto shape) {
@@ -664,14 +741,6 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
       if (BX == Deep::BX && many <= few_tiles()) gw(Deep{});
       else gw(S{});
     }
-  }
-  if (a.gh) {
-    // (many parts of few outputs: sixteen threads to each)
-    const size_t quads = tiles(a.dim, 4) * a.rows;
-    const bool few = p.splits >= 32 && quads < ((size_t)1 << 16);
-    auto k = few ? k_loss_gh_join<T, 16> : k_loss_gh_join<T, 1>;
-    LAUNCH(k, dim3((unsigned)tiles(quads, few ? 16 : 256)), 256, 0, part, (int)p.splits, a.rows,
-           a.dim, coef, (T *)a.gh, a.gh_stride);
   }
   return e;
 }

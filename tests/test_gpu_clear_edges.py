@@ -97,9 +97,9 @@ def test_cross_entropy_gradients_of_millions_of_rows(given_back, dtype, rows, di
     within(gw, want, bound)
 
 
-def loss_case(dtype, rows, dim, vocab, pad=0, mean=0.0):
-    """Hidden states, head, targets; `mean` of all words but the targets' in the head, so
-    that a row's softmax part of gh stands apart from its target's."""
+def loss_case(dtype, rows, dim, vocab, mean=0.0):
+    """Hidden states, head, targets among the first eighth of the words; `mean`: that of
+    the other words' weights."""
     h = normal(10, rows, dim, dtype)
     w = normal(11, vocab, dim, D, 1.0 / math.sqrt(dim))
     t = targets(12, rows, max(1, vocab // 8), rows // 9)
@@ -135,6 +135,31 @@ def check_gh_by_row(dtype, h, w, t, g, judged):
     return gh, gw, want
 
 
+def gw64(dtype, h, w, t, g):
+    """gw in 64 bits and its bound: gl rounded once on its row's scale and, in f16, once
+    more in half steps of 2^-39 of the largest factor."""
+    H, W, t, f = h.cuda().to(D), w.cuda().to(D), t.cuda(), g.cuda().to(D)
+    want = torch.zeros_like(W)
+    bound = torch.zeros_like(W)
+    f = torch.where(t >= 0, f, 0.0)
+    for r in range(0, len(t), 4096):
+        X, c = H[r:r + 4096], f[r:r + 4096, None]
+        logits = X @ W.t().contiguous()
+        lse = torch.logsumexp(logits, 1)
+        delta = 4 * E * math.sqrt(h.shape[1]) * X.norm(dim=1) * W.norm(dim=1).max() \
+            + 64 * E * (1 + lse.abs() + logits.abs().amax(1))
+        p = torch.exp(logits - lse[:, None])
+        gl = p.clone()
+        gl.scatter_add_(1, t[r:r + 4096].clamp(min=0)[:, None], torch.full_like(c, -1.0))
+        gl, p = gl * c, p * c.abs()
+        off = (U[dtype] + 64 * E) * gl.abs() + p * 2 * delta[:, None]
+        if dtype == F16:
+            off += c.abs() * 2.0 ** -38 + f.abs().max() * 2.0 ** -39
+        want += gl.t().contiguous() @ X
+        bound += off.t().contiguous() @ X.abs()
+    return want, bound + U[dtype] * want.abs() + TINY[dtype]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("rows,dim,vocab", [(20, 64, 300), (9, 1024, 2000), (500, 256, 4000),
                                             (4000, 640, 8100)])
@@ -153,3 +178,25 @@ def test_cross_entropy_factor_of_infinity_stays_in_its_row(dtype, rows, dim, voc
     t[3] = -100
     gh, gw, _ = check_gh_by_row(dtype, h, w, t, g, judged)
     assert not gh[3].any() and torch.isfinite(gw).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,dim,vocab", [(20, 64, 300), (9, 1024, 2000), (500, 256, 4000),
+                                            (4000, 640, 8100), (4000, 641, 8100), (12000, 64, 50000)])
+def test_cross_entropy_of_rows_that_weigh_little(dtype, rows, dim, vocab):
+    """Row factors from 1 down to 2^-30 of the largest: gh row by row against its own
+    factor, and its softmax part there; gw against all of them."""
+    h, w, t = loss_case(dtype, rows, dim, vocab, mean=2.0)
+    g = 2.0 ** 10 * 2.0 ** -torch.randint(0, 31, (rows,), generator=gen(14)).float()
+    g *= 1 - 0.49 * torch.rand(rows, generator=gen(15))
+    g[0] = 2.0 ** 10
+    # row 1 weighs 2^-24 of row 0, and its softmax is on the words of mean 2
+    g[1], t[1], h[1] = -(2.0 ** -14), 0, h[1].abs() * 4 / dim
+    gh, gw, want = check_gh_by_row(dtype, h, w, t, g, slice(None))
+    assert float(want[1].mean()) * -(2.0 ** 14) > 1
+    want_w, bound = gw64(dtype, h, w, t, g)
+    within(gw, want_w, bound)
+    # gradients alone, bit for bit
+    args = h.cuda(), w.cuda(), t.cuda(), R.cross_entropy(h.cuda(), w.cuda(), t.cuda())[1], g.cuda()
+    assert torch.equal(R.cross_entropy_backward(*args, want_gw=False)[0], gh)
+    assert torch.equal(R.cross_entropy_backward(*args, want_gh=False)[1], gw)
