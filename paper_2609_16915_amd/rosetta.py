@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import inspect
 import os
 from typing import NamedTuple
 
@@ -719,8 +720,14 @@ def _scratch(workspace, need: int, like):
 def _on_its_stream(call):
     """With a stream given, what `call` allocates (outputs, workspaces) belongs to
     that stream, so that no memory is reused while its work still runs."""
+    at = list(inspect.signature(call).parameters).index("stream")  # (the last one)
+
     @functools.wraps(call)
     def on_stream(*args, stream=None, **kw):
+        if len(args) > at:
+            if stream is not None or len(args) > at + 1:
+                raise TypeError(f"{call.__name__} takes {at + 1} arguments, stream the last of them")
+            stream, args = args[at], args[:at]
         if stream is None:
             return call(*args, **kw)
         with _torch().cuda.stream(stream):
