@@ -206,6 +206,7 @@ def _params(p) -> Params:
 # device buffers (torch)
 # --------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
     return torch
@@ -643,10 +644,18 @@ def _tensor_class():
     return _torch().Tensor
 
 
-def _mat(t, name: str, dtype=None, shape=None):
+def _misplaced(t, name: str, device):
+    """Raises for a tensor that lies on no ROCm device (TypeError) or on another one than
+    the call's (its index; ValueError)."""
+    if t.get_device() < 0:
+        raise TypeError(f"{name} must be a torch tensor on a ROCm device")
+    raise ValueError(f"{name} lies on device {t.get_device()}, the call runs on device {device}")
+
+
+def _mat(t, name: str, dtype=None, shape=None, device=None):
     """(address, row stride, rows, columns) of a device matrix with contiguous
     rows; a vector is one row.  TypeError for the wrong kind of tensor,
-    ValueError for the wrong size, before any library call."""
+    ValueError for the wrong size or device, before any library call."""
     if not isinstance(t, _tensor_class()):
         raise TypeError(f"{name} must be a torch tensor")
     if dtype is not None and t.dtype != dtype:
@@ -661,21 +670,24 @@ def _mat(t, name: str, dtype=None, shape=None):
         raise ValueError(f"{name} must be a matrix or one row, not {tuple(size)}")
     if shape is not None and (rows != shape[0] or cols != shape[1]):
         raise ValueError(f"{name} is {rows} x {cols}, the call needs {shape[0]} x {shape[1]}")
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a torch tensor on a ROCm device")
+    at = t.get_device()
+    if at < 0 or (device is not None and at != device):
+        _misplaced(t, name, device)
     if cols > 1 and strides[-1] != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
     return t.data_ptr(), stride, rows, cols
 
 
-def _vec(t, name: str, dtype, count: int) -> int:
+def _vec(t, name: str, dtype, count: int, device) -> int:
     """Address of a contiguous device vector of `count` elements."""
     if not isinstance(t, _tensor_class()) or t.dtype != dtype:
         raise TypeError(f"{name} must be a torch tensor of {dtype}")
     if t.numel() != count:
         _expect(t, name, count)
-    if not t.is_cuda or not t.is_contiguous():
-        raise TypeError(f"{name} must be contiguous on a ROCm device")
+    if t.get_device() != device:
+        _misplaced(t, name, device)
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
@@ -685,22 +697,25 @@ def _made(out, name: str, shape, dtype, like):
     if out is None:
         out = like.new_empty(shape, dtype=dtype)
         return out, out.data_ptr(), shape[1]
-    return out, *_mat(out, name, dtype, shape)[:2]
+    return out, *_mat(out, name, dtype, shape, like.get_device())[:2]
 
 
-def _weight(weight, dtype, code: int, dim: int):
+def _weight(weight, dtype, code: int, dim: int, device):
     """(address, type) of a norm's weight, of x's type or float32; None is ones."""
     if weight is None:
         return None, code
     if weight.dtype != dtype and weight.dtype != _torch().float32:
         raise TypeError(f"weight must be {dtype} or float32, not {weight.dtype}")
-    return _vec(weight, "weight", weight.dtype, dim), _type(weight.dtype, "weight")
+    return _vec(weight, "weight", weight.dtype, dim, device), _type(weight.dtype, "weight")
 
 
 def _stream_of(t, stream) -> int:
     """The stream given, or the current one of the tensor's device (read as a plain
     number: a Stream object takes 2.6 us to make, as long as the launch)."""
     if stream is not None:
+        if stream.device_index != t.get_device():
+            raise ValueError(f"the stream is of device {stream.device_index}, the tensors lie on "
+                             f"device {t.get_device()}")
         return stream.cuda_stream
     return _torch()._C._cuda_getCurrentRawStream(t.device.index)
 
@@ -712,15 +727,19 @@ def _scratch(workspace, need: int, like):
     have = workspace.numel() * workspace.element_size()
     if have < need:
         raise ValueError(f"workspace holds {have} bytes, the call needs {need}")
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise TypeError("workspace must be contiguous on a ROCm device")
+    if workspace.get_device() != like.get_device():
+        _misplaced(workspace, "workspace", like.get_device())
+    if not workspace.is_contiguous():
+        raise TypeError("workspace must be contiguous")
     return workspace.data_ptr(), have, workspace
 
 
 def _on_its_stream(call):
     """With a stream given, what `call` allocates (outputs, workspaces) belongs to
-    that stream, so that no memory is reused while its work still runs."""
-    at = list(inspect.signature(call).parameters).index("stream")  # (the last one)
+    that stream, so that no memory is reused while its work still runs.  Without one,
+    the device of its first tensor is the current one while it runs."""
+    names = list(inspect.signature(call).parameters)
+    at = names.index("stream")  # (the last one)
 
     @functools.wraps(call)
     def on_stream(*args, stream=None, **kw):
@@ -728,9 +747,15 @@ def _on_its_stream(call):
             if stream is not None or len(args) > at + 1:
                 raise TypeError(f"{call.__name__} takes {at + 1} arguments, stream the last of them")
             stream, args = args[at], args[:at]
+        torch = _torch()
         if stream is None:
-            return call(*args, **kw)
-        with _torch().cuda.stream(stream):
+            first = args[0] if args else kw.get(names[0])
+            device = first.get_device() if isinstance(first, _tensor_class()) else -1
+            if device < 0 or device == torch._C._cuda_getDevice():
+                return call(*args, **kw)
+            with torch.cuda.device(device):
+                return call(*args, **kw)
+        with torch.cuda.stream(stream):
             return call(*args, stream=stream, **kw)
     return on_stream
 
@@ -749,9 +774,11 @@ def _norm(x, weight, eps, residual, h, y, want_y, q, want_q, stream):
     torch = _torch()
     xp, xs, rows, dim = _mat(x, "x")
     dtype = x.dtype
-    code = _type(dtype, "x")
-    rp, rs = (None, dim) if residual is None else _mat(residual, "residual", dtype, (rows, dim))[:2]
-    wp, wt = _weight(weight, dtype, code, dim)
+    code, on = _type(dtype, "x"), x.get_device()
+    rp, rs = None, dim
+    if residual is not None:
+        rp, rs = _mat(residual, "residual", dtype, (rows, dim), on)[:2]
+    wp, wt = _weight(weight, dtype, code, dim, on)
     hp, hs, yp, ys, qp, qs, scale, sp = None, dim, None, dim, None, dim, None, None
     if h is not None or residual is not None:
         h, hp, hs = _made(h, "h", (rows, dim), dtype, x)
@@ -792,11 +819,11 @@ def rms_norm_backward(gy, h, weight, inv_rms, gh=None, gx=None, want_gweight: bo
     torch = _torch()
     yp, ys, rows, dim = _mat(gy, "gy")
     dtype = gy.dtype
-    code = _type(dtype, "gy")
-    hp, hs = _mat(h, "h", dtype, (rows, dim))[:2]
-    gp, gs = (None, dim) if gh is None else _mat(gh, "gh", dtype, (rows, dim))[:2]
-    wp, wt = _weight(weight, dtype, code, dim)
-    ip = _vec(inv_rms, "inv_rms", torch.float32, rows)
+    code, on = _type(dtype, "gy"), gy.get_device()
+    hp, hs = _mat(h, "h", dtype, (rows, dim), on)[:2]
+    gp, gs = (None, dim) if gh is None else _mat(gh, "gh", dtype, (rows, dim), on)[:2]
+    wp, wt = _weight(weight, dtype, code, dim, on)
+    ip = _vec(inv_rms, "inv_rms", torch.float32, rows, on)
     gx, xp, xs = _made(gx, "gx", (rows, dim), dtype, gy)
     gweight, gwp, wsp, wsb = None, None, None, 0
     if want_gweight:
@@ -819,7 +846,7 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib().rosetta_quantize_rows(xp, xs, code, rows, dim, qp, qs,
-                                       _vec(scale, "scale", torch.float32, rows),
+                                       _vec(scale, "scale", torch.float32, rows, x.get_device()),
                                        _stream_of(x, stream)))
     return q, scale
 
@@ -829,7 +856,7 @@ def dequantize_rows(q, scale, dtype, out=None, stream=None):
     """The values that 8-bit rows stand for."""
     torch = _torch()
     qp, qs, rows, dim = _mat(q, "q", torch.int8)
-    sp = _vec(scale, "scale", torch.float32, rows)
+    sp = _vec(scale, "scale", torch.float32, rows, q.get_device())
     out, op, os_ = _made(out, "out", (rows, dim), dtype, q)
     _check(lib().rosetta_dequantize_rows(qp, qs, sp, _type(dtype, "dtype"), rows, dim, op, os_,
                                          _stream_of(q, stream)))
@@ -845,12 +872,13 @@ def q8_matmul(a, a_scale, b, b_scale, bias=None, out_dtype=None, out=None, works
     if out_dtype is None:
         out_dtype = torch.bfloat16 if out is None else out.dtype
     ap, as_, m, k = _mat(a, "a", torch.int8)
-    bp, bs, n, kb = _mat(b, "b", torch.int8)
+    on = a.get_device()
+    bp, bs, n, kb = _mat(b, "b", torch.int8, device=on)
     if kb != k:
         raise ValueError(f"b is {n} x {kb}, the call needs rows of {k}")
-    sa = _vec(a_scale, "a_scale", torch.float32, m)
-    sb = _vec(b_scale, "b_scale", torch.float32, n)
-    bi = None if bias is None else _vec(bias, "bias", torch.float32, n)
+    sa = _vec(a_scale, "a_scale", torch.float32, m, on)
+    sb = _vec(b_scale, "b_scale", torch.float32, n, on)
+    bi = None if bias is None else _vec(bias, "bias", torch.float32, n, on)
     out, op, os_ = _made(out, "out", (m, n), out_dtype, a)
     need = lib().rosetta_q8_matmul_workspace_bytes(m, n, k)
     wp, wb = None, 0
@@ -868,11 +896,11 @@ def cross_entropy(h, w, targets, ignore_index: int = -100, workspace=None, strea
     weights w [vocab][dim] (bfloat16 or float16); targets int64."""
     torch = _torch()
     hp, hs, rows, dim = _mat(h, "h")
-    dt = _type(h.dtype, "h")
-    wp, ws, vocab, dw = _mat(w, "w", h.dtype)
+    dt, on = _type(h.dtype, "h"), h.get_device()
+    wp, ws, vocab, dw = _mat(w, "w", h.dtype, device=on)
     if dw != dim:
         raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
-    tp = _vec(targets, "targets", torch.int64, rows)
+    tp = _vec(targets, "targets", torch.int64, rows, on)
     loss, lse = (h.new_empty(rows, dtype=torch.float32) for _ in range(2))
     sp, sb, workspace = _scratch(
         workspace, lib().rosetta_cross_entropy_workspace_bytes(rows, dim, vocab), h)
@@ -890,13 +918,13 @@ def cross_entropy_backward(h, w, targets, lse, gloss, ignore_index: int = -100,
     cross_entropy returned it."""
     torch = _torch()
     hp, hs, rows, dim = _mat(h, "h")
-    dt = _type(h.dtype, "h")
-    wp, ws, vocab, dw = _mat(w, "w", h.dtype)
+    dt, on = _type(h.dtype, "h"), h.get_device()
+    wp, ws, vocab, dw = _mat(w, "w", h.dtype, device=on)
     if dw != dim:
         raise ValueError(f"w is {vocab} x {dw}, the call needs rows of {dim}")
-    tp = _vec(targets, "targets", torch.int64, rows)
-    ep = _vec(lse, "lse", torch.float32, rows)
-    gp = _vec(gloss, "gloss", torch.float32, rows)
+    tp = _vec(targets, "targets", torch.int64, rows, on)
+    ep = _vec(lse, "lse", torch.float32, rows, on)
+    gp = _vec(gloss, "gloss", torch.float32, rows, on)
     gh, ghp, ghs = _made(gh, "gh", (rows, dim), h.dtype, h) if want_gh else (None, None, dim)
     gw, gwp, gws = _made(gw, "gw", (vocab, dim), w.dtype, w) if want_gw else (None, None, dim)
     sp, sb, workspace = _scratch(
