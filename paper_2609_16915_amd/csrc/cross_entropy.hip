@@ -54,10 +54,14 @@ struct Stat {
   float top, sum;
 };
 
+// What is taken off the logits before their exponentials: the maximum, or nothing where
+// that is an infinity (the sum is then 0 or infinite, as it should be).
+__device__ inline float level(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
+
 // (a, b) as one: sums of exponentials above the larger maximum
 __device__ inline Stat join(Stat a, Stat b) {
   const float top = fmaxf(a.top, b.top);
-  if (top == -INFINITY) return {top, a.sum + b.sum};
+  if (fabsf(top) == INFINITY) return {top, a.sum + b.sum};
   return {top, a.sum * __expf(a.top - top) + b.sum * __expf(b.top - top)};
 }
 
@@ -128,7 +132,7 @@ k_loss_tile(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
     Stat s{-INFINITY, 0.f};
 #pragma unroll
     for (int i = 0; i < RUN; ++i) s.top = fmaxf(s.top, acc[i / 4][j][i % 4]);
-    const float low = s.top == -INFINITY ? 0.f : s.top * LOG2E;
+    const float low = level(s.top) * LOG2E;
 #pragma unroll
     for (int i = 0; i < RUN; ++i)
       s.sum += __builtin_amdgcn_exp2f(fmaf(acc[i / 4][j][i % 4], LOG2E, -low));
@@ -173,7 +177,7 @@ k_loss_thin(LossArgs a, Stat *__restrict__ part, float *__restrict__ at_target) 
       if (x + r == target) at_target[row] = l[r];
       s.top = fmaxf(s.top, l[r]);
     }
-    const float low = s.top == -INFINITY ? 0.f : s.top;
+    const float low = level(s.top);
 #pragma unroll
     for (int r = 0; r < 4; ++r) s.sum += __expf(l[r] - low);
   }

@@ -200,3 +200,38 @@ def test_cross_entropy_of_rows_that_weigh_little(dtype, rows, dim, vocab):
     args = h.cuda(), w.cuda(), t.cuda(), R.cross_entropy(h.cuda(), w.cuda(), t.cuda())[1], g.cuda()
     assert torch.equal(R.cross_entropy_backward(*args, want_gw=False)[0], gh)
     assert torch.equal(R.cross_entropy_backward(*args, want_gh=False)[1], gw)
+
+
+@pytest.mark.parametrize("rows,dim,vocab", [(8, 512, 3000), (24, 1024, 3000), (20, 64, 300),
+                                            (130, 100, 20000), (4000, 640, 8100)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_cross_entropy_of_infinite_logits(dtype, rows, dim, vocab):
+    """Logits of either infinity give what log, exp and sum of them give in 64 bits: lse is
+    infinite where the largest logit is, and rows of finite logits are as they were."""
+    h, w = normal(20, rows, dim, dtype), normal(21, vocab, dim, dtype, 0.3)
+    t = targets(22, rows, vocab)
+    inf = float("inf")
+    big = 2.0 ** 100 if dtype == BF16 else inf
+    w[:, 0] = 2.0 ** 100 if dtype == BF16 else 1  # (their product leaves 32 bits)
+    w[vocab // 2:, 0] *= -1
+    h[:, 0] = 0
+    h[1:5, 0] = torch.tensor([big, big, -big, -big]).to(dtype)
+    t[1:5] = torch.tensor([0, vocab - 1, 0, vocab - 1])
+    loss, lse = R.cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    assert (lse[1:5] == inf).all()
+    assert torch.isnan(loss[[1, 4]]).all() and (loss[[2, 3]] == inf).all()
+    rest = torch.tensor([r for r in range(rows) if not 1 <= r < 5])
+    same = R.cross_entropy(h[:, 1:].cuda(), w[:, 1:].cuda(), t.cuda())
+    assert torch.allclose(lse[rest], same[1][rest], rtol=1e-5) and torch.isfinite(loss[rest]).all()
+    # words left out by a logit of -infinity, and rows of nothing else
+    w[:, 0] = w[:, 0].abs()
+    if dtype == BF16:  # (0 times infinity is NaN)
+        w[vocab // 3:, 0] = 0
+    loss, lse = R.cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    if dtype == BF16:
+        kept = R.cross_entropy(h[:, 1:].cuda(), w[vocab // 3:, 1:].cuda(), torch.zeros_like(t).cuda())
+        assert torch.allclose(lse[3:5], kept[1][3:5], rtol=1e-5)
+        assert loss[3] == inf and torch.isfinite(loss[4])
+        assert (lse[1:3] == inf).all() and torch.isnan(loss[1]) and loss[2] == inf
+    else:
+        assert (lse[3:5] == -inf).all() and torch.isnan(loss[3:5]).all()
