@@ -612,8 +612,10 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
  *    overflow 32 bits, in the norm) has a scale that is not finite, or NaN,
  *    and unspecified q.
  *  - Outputs must not overlap inputs or each other (ROSETTA_ERR_ALIAS) unless
- *    stated.  rows == 0 is a successful no-op once sizes are valid, except
- *    that gradients of weights are then zeros.
+ *    stated.  Columns of one buffer, their rows as far apart in bytes, do not;
+ *    any other two arrays do if their ranges from first to last byte do.
+ *  - rows == 0 is a successful no-op once sizes are valid, except that gradients
+ *    of weights are then zeros.
  *  - Every sum is taken in an order that the sizes alone decide: equal inputs
  *    give equal bits. */
 typedef enum { ROSETTA_F32 = 0, ROSETTA_BF16 = 1, ROSETTA_F16 = 2 } rosetta_dtype;

@@ -48,8 +48,22 @@ struct Array {
   const void *p;
   size_t rows, len, stride, elem;
   bool out;
-  size_t bytes() const { return rows && len ? ((rows - 1) * stride + len) * elem : 0; }
+  // (past 64 bits where a caller's sizes are: 2^31 rows 2^32 elements apart)
+  unsigned __int128 bytes() const {
+    return rows && len ? ((unsigned __int128)(rows - 1) * stride + len) * elem : 0;
+  }
 };
+
+// Whether two arrays share memory: by the whole ranges, or, rows as far apart in both
+// (columns of one buffer), by where the second's rows lie between the first's.
+bool overlap(const Array &a, const Array &b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  if (!(x < y + b.bytes() && y < x + a.bytes())) return false;
+  const size_t pitch = a.stride * a.elem;
+  if (a.rows < 2 || b.rows < 2 || pitch != b.stride * b.elem) return true;
+  const size_t at = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;
+  return at < a.len * a.elem || at + b.len * b.elem > pitch;
+}
 
 rosetta_status check_strides(std::initializer_list<Array> as) {
   for (const Array &a : as)
@@ -69,11 +83,10 @@ rosetta_status check_arrays(std::initializer_list<Array> as, const char *out = n
   for (const Array *a = as.begin(); a != as.end(); ++a)
     for (const Array *b = a + 1; b != as.end(); ++b) {
       if (!a->p || !b->p || (!a->out && !b->out)) continue;
-      const char *x = (const char *)a->p, *y = (const char *)b->p;
-      if (!(x < y + b->bytes() && y < x + a->bytes())) continue;
+      if (!overlap(*a, *b)) continue;
       bool fine = false;
       for (const char *s : same)
-        fine |= a->name == s && b->name == out && x == y && a->stride == b->stride;
+        fine |= a->name == s && b->name == out && a->p == b->p && a->stride == b->stride;
       if (!fine) return fail(ROSETTA_ERR_ALIAS, "%s overlaps %s", b->name, a->name);
     }
   return ROSETTA_OK;

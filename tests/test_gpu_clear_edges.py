@@ -235,3 +235,42 @@ def test_cross_entropy_of_infinite_logits(dtype, rows, dim, vocab):
         assert (lse[1:3] == inf).all() and torch.isnan(loss[1]) and loss[2] == inf
     else:
         assert (lse[3:5] == -inf).all() and torch.isnan(loss[3:5]).all()
+
+
+# ------------------------------------------------- shared buffers and workspaces ---
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(2, 64), (7, 600), (300, 1031), (5, 17000)])
+def test_outputs_beside_inputs_in_one_buffer(dtype, rows, dim):
+    """Columns of one buffer: rows that lie between each other's do not overlap."""
+    buf = normal(30, rows, 5 * dim + 3, dtype).cuda()
+    x, r, h, y, g = (buf[:, i * dim:(i + 1) * dim] for i in range(5))
+    w = normal(31, 1, dim, dtype)[0].cuda()
+    want = R.rms_norm(x.clone(), w, EPS, residual=r.clone())
+    R.rms_norm(x, w, EPS, residual=r, h=h, y=y)
+    assert torch.equal(y, want[0]) and torch.equal(h, want[1])
+    back = R.rms_norm_backward(y.clone(), h.clone(), w, want[2])
+    gx, gw = R.rms_norm_backward(y, h, w, want[2], gx=g)
+    assert torch.equal(g, back[0]) and torch.equal(gw, back[1])
+    a, sa = R.quantize_rows(x)
+    product = R.q8_matmul(a, sa, a, sa, out_dtype=dtype)
+    both = torch.empty((rows, 2 * max(rows, dim)), dtype=torch.int8, device="cuda")
+    both[:, :dim] = a
+    q, s = R.quantize_rows(x, q=both[:, dim:2 * dim])
+    assert torch.equal(q, a) and torch.equal(both[:, :dim], a) and torch.equal(s, sa)
+    assert torch.equal(R.q8_matmul(both[:, :dim], sa, both[:, dim:2 * dim], sa, out_dtype=dtype),
+                       product)
+    with pytest.raises(R.RosettaError) as e:  # one column of x's
+        R.rms_norm(x, w, EPS, y=buf[:, dim - 1:2 * dim - 1])
+    assert e.value.status == 4
+
+
+@pytest.mark.parametrize("rows,dim,vocab", [(40, 64, 300), (300, 256, 1000)])
+def test_gradients_beside_their_inputs(rows, dim, vocab):
+    hb, wb = normal(32, rows, 2 * dim, BF16).cuda(), normal(33, vocab, 2 * dim, BF16, 0.1).cuda()
+    t, g = targets(34, rows, vocab, 3).cuda(), torch.rand(rows, generator=gen(35)).cuda()
+    h, w = hb[:, :dim], wb[:, :dim]
+    lse = R.cross_entropy(h, w, t)[1]
+    want = R.cross_entropy_backward(h.clone(), w.clone(), t, lse, g)
+    got = R.cross_entropy_backward(h, w, t, lse, g, gh=hb[:, dim:], gw=wb[:, dim:])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
