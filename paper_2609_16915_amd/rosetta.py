@@ -704,6 +704,8 @@ def _weight(weight, dtype, code: int, dim: int, device):
     """(address, type) of a norm's weight, of x's type or float32; None is ones."""
     if weight is None:
         return None, code
+    if not isinstance(weight, _tensor_class()):
+        raise TypeError("weight must be a torch tensor")
     if weight.dtype != dtype and weight.dtype != _torch().float32:
         raise TypeError(f"weight must be {dtype} or float32, not {weight.dtype}")
     return _vec(weight, "weight", weight.dtype, dim, device), _type(weight.dtype, "weight")
@@ -724,6 +726,8 @@ def _scratch(workspace, need: int, like):
     """`workspace` checked, or a new one: (address, bytes, tensor)."""
     if workspace is None:
         workspace = like.new_empty(need, dtype=_torch().uint8)
+    if not isinstance(workspace, _tensor_class()):
+        raise TypeError("workspace must be a torch tensor")
     have = workspace.numel() * workspace.element_size()
     if have < need:
         raise ValueError(f"workspace holds {have} bytes, the call needs {need}")
@@ -870,7 +874,7 @@ def q8_matmul(a, a_scale, b, b_scale, bias=None, out_dtype=None, out=None, works
     row of each: [m][n] of out_dtype (default bfloat16)."""
     torch = _torch()
     if out_dtype is None:
-        out_dtype = torch.bfloat16 if out is None else out.dtype
+        out_dtype = getattr(out, "dtype", torch.bfloat16)
     ap, as_, m, k = _mat(a, "a", torch.int8)
     on = a.get_device()
     bp, bs, n, kb = _mat(b, "b", torch.int8, device=on)

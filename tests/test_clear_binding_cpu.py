@@ -139,3 +139,13 @@ def test_tensors_and_stream_of_one_device(machine, name):
     with pytest.raises(ValueError, match="device"):
         getattr(R, name)(**tensors, **values, stream=Stream(0))
     assert not machine.calls
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_every_operand_has_to_be_a_tensor(machine, name):
+    tensors, values = operands(0)[name]
+    for wrong in tensors:
+        for kind in ([1.0], 3, "x"):
+            with pytest.raises(TypeError, match=wrong):
+                getattr(R, name)(**{**tensors, wrong: kind}, **values)
+    assert not machine.calls
