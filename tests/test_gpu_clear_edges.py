@@ -6,7 +6,7 @@ import pytest
 from paper_2609_16915_amd import rosetta as R
 
 from gpu_helpers import require_gpu
-from test_gpu_clear import BF16, D, E, EPS, F16, F32, TINY, U, gen, normal, targets, within
+from test_gpu_clear import BF16, D, E, EPS, F16, F32, TINY, U, gen, int8, normal, targets, within
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -274,3 +274,39 @@ def test_gradients_beside_their_inputs(rows, dim, vocab):
     want = R.cross_entropy_backward(h.clone(), w.clone(), t, lse, g)
     got = R.cross_entropy_backward(h, w, t, lse, g, gh=hb[:, dim:], gw=wb[:, dim:])
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,dim", [(700, 64), (3000, 63), (900, 128), (1000, 129), (50, 250), (33, 768),
+                                      (600, 1021), (1100, 2048), (515, 4099), (1100, 4096), (540, 8191),
+                                      (20, 16384), (30, 16381), (515, 16390), (3, 40000)])
+def test_norm_gradient_in_gh_and_in_gy(dtype, rows, dim):
+    """gx at the address of gh or gy, every length class: the bits of a gx of its own."""
+    h, gy, gh = (normal(40 + i, rows, dim, dtype, s).cuda() for i, s in ((0, 2.0), (1, 0.5), (2, 0.25)))
+    w = normal(43, 1, dim, dtype)[0].cuda()
+    inv = 0.5 + torch.rand(rows, generator=gen(44)).cuda()
+    want, want_w = R.rms_norm_backward(gy, h, w, inv, gh=gh)
+    for which in (0, 1):
+        a, b = gy.clone(), gh.clone()
+        gx, gw = R.rms_norm_backward(a, h, w, inv, gh=b, gx=(a, b)[which])
+        assert gx.data_ptr() == (a, b)[which].data_ptr()
+        assert torch.equal(gx, want) and torch.equal(gw, want_w)
+        assert torch.equal((b, a)[which], (gh, gy)[which])
+
+
+@pytest.mark.parametrize("m,n,k", [(33, 4096, 14336), (17, 200, 9000), (100, 300, 20001),
+                                   (128, 512, 8192), (700, 1111, 9008)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_q8_matmul_without_a_workspace(m, n, k, dtype):
+    """Sums that a workspace would split, whole: the same bits."""
+    L = R.lib()
+    assert L.rosetta_q8_matmul_workspace_bytes(m, n, k) > 0
+    a, b = int8(50, m, k).cuda(), int8(51, n, k).cuda()
+    sa, sb = torch.rand(m, generator=gen(52)).cuda(), torch.rand(n, generator=gen(53)).cuda()
+    bias = torch.randn(n, generator=gen(54)).cuda()
+    want = R.q8_matmul(a, sa, b, sb, bias=bias, out_dtype=dtype)
+    got = torch.full_like(want, float("nan"))
+    st = L.rosetta_q8_matmul(a.data_ptr(), k, sa.data_ptr(), b.data_ptr(), k, sb.data_ptr(),
+                             bias.data_ptr(), got.data_ptr(), n, {F32: 0, BF16: 1}[dtype], m, n, k,
+                             None, 0, torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(got, want)
