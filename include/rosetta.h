@@ -608,9 +608,10 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
  *    held in 32 bits; 8-bit products are summed exactly.
  *  - 8-bit rows: value = scale[row] * q, q in [-127, 127], scale = max |value|
  *    / 127, rounded to nearest, ties to even.  A row of zeros has scale 0; a
- *    row with a NaN or an infinity, be it of the weight (or whose squares
- *    overflow 32 bits, in the norm) has a scale that is not finite, or NaN,
- *    and unspecified q.
+ *    row with a NaN or an infinity, be it of the weight, has a scale that is
+ *    not finite, or NaN, and unspecified q.  So has, in the norm, a row whose
+ *    squares overflow 32 bits (inv_rms and y are 0 then) or, with eps = 0, a
+ *    row whose squares are 0 in 32 bits (inv_rms is infinite then).
  *  - Outputs must not overlap inputs or each other (ROSETTA_ERR_ALIAS) unless
  *    stated.  Columns of one buffer, their rows as far apart in bytes, do not;
  *    any other two arrays do if their ranges from first to last byte do.

@@ -219,7 +219,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm(NormArgs a) 
     if (NORM) inv = 1.f / sqrtf(sum / (float)dim + a.eps);
     q_factors(top, f0, f1);
     if (t == 0) {
-      if (a.scale) a.scale[row] = NORM ? top * inv / 127.f : top / 127.f + sum;
+      // (sum - sum: nothing, or NaN where the squares overflowed, inv then being 0)
+      if (a.scale) a.scale[row] = NORM ? top * inv / 127.f + (sum - sum) : top / 127.f + sum;
       if (NORM && a.inv_rms) a.inv_rms[row] = inv;
     }
   };

@@ -310,3 +310,15 @@ def test_q8_matmul_without_a_workspace(m, n, k, dtype):
                              bias.data_ptr(), got.data_ptr(), n, {F32: 0, BF16: 1}[dtype], m, n, k,
                              None, 0, torch.cuda.current_stream().cuda_stream)
     assert st == 0 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype,size", [(F32, 1e20), (BF16, 1e20), (F32, 3e38), (BF16, 3e38)])
+@pytest.mark.parametrize("dim", [1, 33, 1024, 4096, 17000])
+def test_norm_whose_squares_overflow(dtype, size, dim):
+    """Such a row says so in its scale; the others do not notice."""
+    x = normal(60, 3, dim, dtype)
+    x[1] = size
+    want = R.rms_norm_q8(x[[0, 2]].cuda(), None, EPS)
+    got = R.rms_norm_q8(x.cuda(), None, EPS)
+    assert not torch.isfinite(got.scale[1])
+    assert torch.equal(got.scale[[0, 2]], want.scale) and torch.equal(got.q[[0, 2]], want.q)
