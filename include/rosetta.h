@@ -615,6 +615,9 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
  *  - Outputs must not overlap inputs or each other (ROSETTA_ERR_ALIAS) unless
  *    stated.  Columns of one buffer, their rows as far apart in bytes, do not;
  *    any other two arrays do if their ranges from first to last byte do.
+ *  - Sizes that a launch does not hold (2^32 threads: a loss of 2^26 rows,
+ *    gradients of 2^34 hidden values, a product of 2^30 channels over short
+ *    rows) are ROSETTA_ERR_UNSUPPORTED before anything is enqueued.
  *  - rows == 0 is a successful no-op once sizes are valid, except that gradients
  *    of weights are then zeros.
  *  - Every sum is taken in an order that the sizes alone decide: equal inputs

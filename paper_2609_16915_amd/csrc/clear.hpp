@@ -21,6 +21,9 @@ inline hipError_t allow_lds(K kernel, size_t bytes) {
                              (int)bytes);
 }
 
+// Whether one launch takes so many workgroups: it counts threads in 32 bits.
+inline bool grid_fits(size_t blocks, size_t threads) { return blocks * threads < (size_t)1 << 32; }
+
 using bf16 = __bf16;
 using f16 = _Float16;
 

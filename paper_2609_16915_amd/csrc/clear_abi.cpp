@@ -13,7 +13,8 @@ using namespace rosetta;
 
 namespace {
 
-// Sizes past these would leave the kernels' index types or the grid.
+// Sizes past these would leave the kernels' index types.  (What a grid does not hold, the
+// launch functions tell before they enqueue anything: hipErrorInvalidConfiguration.)
 constexpr size_t MAX_DIM = (size_t)1 << 24, MAX_LOSS_DIM = (size_t)1 << 20;
 constexpr size_t MAX_ROWS = (size_t)1 << 31;
 constexpr size_t MAX_STRIDE = (size_t)1 << 32;
@@ -37,6 +38,8 @@ rosetta_status done(hipError_t e, const char *what) {
   (void)hipGetLastError();
   if (e == hipErrorOutOfMemory)
     return fail(ROSETTA_ERR_NOMEM, "%s: %s", what, hipGetErrorString(e));
+  if (e == hipErrorInvalidConfiguration)
+    return fail(ROSETTA_ERR_UNSUPPORTED, "%s: sizes that one launch does not hold", what);
   return fail(ROSETTA_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 

@@ -647,18 +647,21 @@ bool aligned(const LossArgs &a) {
   return rows_aligned(X) && rows_aligned(Y);
 }
 
-// Launch of `kernel` with its LDS allowed, `e` the status so far.
+// Launch of `kernel` with its LDS allowed, `e` the status so far; `dry`: only whether the
+// grid holds it.
 #define LAUNCH(KERNEL, BLOCKS, THREADS, LDS, ...)                                               \
   do {                                                                                          \
-    if (e == hipSuccess) e = allow_lds(KERNEL, LDS);                                             \
-    if (e == hipSuccess) {                                                                      \
-      hipLaunchKernelGGL(KERNEL, BLOCKS, dim3(THREADS), LDS, st, __VA_ARGS__);                   \
+    const size_t blocks_ = BLOCKS;                                                              \
+    if (e == hipSuccess && !grid_fits(blocks_, THREADS)) e = hipErrorInvalidConfiguration;      \
+    if (e == hipSuccess && !dry) e = allow_lds(KERNEL, LDS);                                     \
+    if (e == hipSuccess && !dry) {                                                              \
+      hipLaunchKernelGGL(KERNEL, dim3((unsigned)blocks_), dim3(THREADS), LDS, st, __VA_ARGS__);  \
       e = hipGetLastError();                                                                    \
     }                                                                                           \
   } while (0)
 
 template <class T>
-hipError_t forward(const LossArgs &a, hipStream_t st) {
+hipError_t forward(const LossArgs &a, hipStream_t st, bool dry) {
   const size_t nx = tiles(a.vocab, forward_x(a.rows, a.dim, a.vocab));
   Stat *part = (Stat *)a.workspace;
   float *at_target = (float *)(part + nx * a.rows);
@@ -666,27 +669,24 @@ hipError_t forward(const LossArgs &a, hipStream_t st) {
   auto tile = [&](auto shape) {
     using S = decltype(shape);
     auto k = aligned(a) ? k_loss_tile<T, S, true> : k_loss_tile<T, S, false>;
-    LAUNCH(k, dim3((unsigned)(nx * tiles(a.rows, S::BY))), S::THREADS,
-           (TileOf<T, S>::LDS), a, part, at_target);
+    LAUNCH(k, nx * tiles(a.rows, S::BY), S::THREADS, (TileOf<T, S>::LDS), a, part, at_target);
   };
   const bool few = thin(a.rows, a.dim, a.vocab);
   if (few && a.rows <= 16)
-    LAUNCH((k_loss_thin<T, 4, 1>), dim3((unsigned)nx), 1024, (Thin<T, 4, 1, 16>::LDS), a, part,
-           at_target);
+    LAUNCH((k_loss_thin<T, 4, 1>), nx, 1024, (Thin<T, 4, 1, 16>::LDS), a, part, at_target);
   else if (few)
-    LAUNCH((k_loss_thin<T, 2, 2>), dim3((unsigned)nx), 1024, (Thin<T, 2, 2, 16>::LDS), a, part,
-           at_target);
+    LAUNCH((k_loss_thin<T, 2, 2>), nx, 1024, (Thin<T, 2, 2, 16>::LDS), a, part, at_target);
   else if (large(a.rows, a.dim, a.vocab)) tile(Large{});
   else if (aligned(a) && nx * tiles(a.rows, Deep::BY) <= few_tiles()) tile(Deep{});
   else tile(Small{});
   // (few rows: more threads to each)
-  if (a.rows <= 64) LAUNCH(k_loss_join<2>, dim3((unsigned)tiles(a.rows, 2)), 1024, 0, a, part, nx, at_target);
-  else LAUNCH(k_loss_join<16>, dim3((unsigned)tiles(a.rows, 16)), 1024, 0, a, part, nx, at_target);
+  if (a.rows <= 64) LAUNCH(k_loss_join<2>, tiles(a.rows, 2), 1024, 0, a, part, nx, at_target);
+  else LAUNCH(k_loss_join<16>, tiles(a.rows, 16), 1024, 0, a, part, nx, at_target);
   return e;
 }
 
 template <class T, class S>
-hipError_t backward(const LossArgs &a, hipStream_t st) {
+hipError_t backward(const LossArgs &a, hipStream_t st, bool dry) {
   constexpr size_t BX = S::BX, BY = S::BY;
   using Tl = TileOf<T, S>;
   const Plan p = plan<S>(a.rows, a.dim, a.vocab);
@@ -695,14 +695,14 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
   T *gl = (T *)(ws + p.gl), *w_p = (T *)(ws + p.w), *h_p = (T *)(ws + p.h), *h_t = (T *)(ws + p.h_t);
   const bool al = aligned(a);
   hipError_t e = hipSuccess;
-  LAUNCH(k_loss_begin<T>, dim3((unsigned)(1 + (a.gw ? tiles(a.rows, 64) * tiles(a.dim, 64) : 0))),
-         256, 0, a, coef, h_t, p.ld_t);
+  LAUNCH(k_loss_begin<T>, 1 + (a.gw ? tiles(a.rows, 64) * tiles(a.dim, 64) : 0), 256, 0, a, coef, h_t,
+         p.ld_t);
   // rows of h or of a piece of w as the tiles take them
   auto rows_of = [&](const void *at, size_t stride, size_t rows, T *packed) {
     const int64_t bytes = (int64_t)(p.ld * sizeof(T));
     if (al) return Operand{(const char *)at, (int64_t)(stride * sizeof(T)), (int64_t)rows, bytes};
-    LAUNCH(k_loss_pack<T>, dim3((unsigned)tiles(rows * (p.ld / 8), 256)), 256, 0, (const T *)at,
-           stride, rows, a.dim, packed, p.ld);
+    LAUNCH(k_loss_pack<T>, tiles(rows * (p.ld / 8), 256), 256, 0, (const T *)at, stride, rows, a.dim,
+           packed, p.ld);
     return Operand{(const char *)packed, bytes, (int64_t)rows, bytes};
   };
   const Operand h = rows_of(a.h, a.h_stride, a.rows, h_p);
@@ -711,26 +711,24 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
     const Operand w = rows_of((const T *)a.w + v0 * a.w_stride, a.w_stride, here, w_p);
     const size_t many = tiles(here, BX) * tiles(a.rows, BY);
     if (BX == Deep::BX && many <= few_tiles())
-      LAUNCH((k_loss_grad_tile<T, Deep>), dim3((unsigned)many), S::THREADS, (TileOf<T, Deep>::LDS), a,
-             w, h, v0, here, p.vp, coef, gl);
-    else
-      LAUNCH((k_loss_grad_tile<T, S>), dim3((unsigned)many), S::THREADS, Tl::LDS, a, w, h, v0, here,
+      LAUNCH((k_loss_grad_tile<T, Deep>), many, S::THREADS, (TileOf<T, Deep>::LDS), a, w, h, v0, here,
              p.vp, coef, gl);
+    else
+      LAUNCH((k_loss_grad_tile<T, S>), many, S::THREADS, Tl::LDS, a, w, h, v0, here, p.vp, coef, gl);
     if (a.gh)
-      LAUNCH((k_loss_gh_tile<T, S>), dim3((unsigned)(p.splits * tiles(a.dim, BX) * tiles(a.rows, BY))),
-             S::THREADS, Tl::LDS, a.rows, a.dim, p.vp, gl, w, part, p.run, i > 0);
+      LAUNCH((k_loss_gh_tile<T, S>), p.splits * tiles(a.dim, BX) * tiles(a.rows, BY), S::THREADS,
+             Tl::LDS, a.rows, a.dim, p.vp, gl, w, part, p.run, i > 0);
     const size_t width = up(here, BX);
     if (a.gh && i + 1 == p.pieces) {
       // (many parts of few outputs: sixteen threads to each)
       const size_t quads = tiles(a.dim, 4) * a.rows;
       const bool few = p.splits >= 32 && quads < ((size_t)1 << 16);
       auto k = few ? k_loss_gh_join<T, 16> : k_loss_gh_join<T, 1>;
-      LAUNCH(k, dim3((unsigned)tiles(quads, few ? 16 : 256)), 256, 0, part, (int)p.splits, a.rows,
-             a.dim, coef, (T *)a.gh, a.gh_stride, a.gw ? gl : nullptr, width, p.vp);
+      LAUNCH(k, tiles(quads, few ? 16 : 256), 256, 0, part, (int)p.splits, a.rows, a.dim, coef,
+             (T *)a.gh, a.gh_stride, a.gw ? gl : nullptr, width, p.vp);
     } else if constexpr (ROW_UP<T> > 0) {
       if (a.gw)
-        LAUNCH(k_loss_common<T>,
-               dim3((unsigned)std::min((size_t)1024, tiles(a.rows * width, 8 * 256))), 256, 0, coef,
+        LAUNCH(k_loss_common<T>, std::min((size_t)1024, tiles(a.rows * width, 8 * 256)), 256, 0, coef,
                a.rows, width, p.vp, gl);
     }
     if (a.gw) {
@@ -739,14 +737,27 @@ hipError_t backward(const LossArgs &a, hipStream_t st) {
         using G = decltype(shape);
         auto k = past_caches((const T *)a.gw, a.gw_stride) ? k_loss_gw_tile<T, G, true>
                                                            : k_loss_gw_tile<T, G, false>;
-        LAUNCH(k, dim3((unsigned)many), G::THREADS, (TileOf<T, G, true>::LDS), a, v0, here, p.vp,
-               p.ld_t, coef, gl, h_t);
+        LAUNCH(k, many, G::THREADS, (TileOf<T, G, true>::LDS), a, v0, here, p.vp, p.ld_t, coef, gl,
+               h_t);
       };
       if (BX == Deep::BX && many <= few_tiles()) gw(Deep{});
       else gw(S{});
     }
   }
   return e;
+}
+
+// All launches of a call, or none: every grid is looked at first, where the sizes are such
+// that one may be too large (the joining of the parts has 64 threads to a row, others less
+// than two to an element).
+hipError_t checked(hipError_t (*call)(const LossArgs &, hipStream_t, bool), const LossArgs &a,
+                   hipStream_t st) {
+  const size_t most = (size_t)1 << 31;
+  if (a.rows * a.dim >= most || a.rows * a.vocab >= most || std::max(a.rows, a.vocab) >= most / 64) {
+    const hipError_t e = call(a, st, true);
+    if (e != hipSuccess) return e;
+  }
+  return call(a, st, false);
 }
 
 }  // namespace
@@ -759,12 +770,13 @@ size_t cross_entropy_backward_workspace(size_t rows, size_t dim, size_t vocab) {
 }
 
 hipError_t launch_cross_entropy(const LossArgs &a, hipStream_t st) {
-  return a.dtype == ROSETTA_BF16 ? forward<bf16>(a, st) : forward<f16>(a, st);
+  auto k = a.dtype == ROSETTA_BF16 ? forward<bf16> : forward<f16>;
+  return checked(k, a, st);
 }
 hipError_t launch_cross_entropy_backward(const LossArgs &a, hipStream_t st) {
   if (large(a.rows, a.dim, a.vocab))
-    return a.dtype == ROSETTA_BF16 ? backward<bf16, Large>(a, st) : backward<f16, Large>(a, st);
-  return a.dtype == ROSETTA_BF16 ? backward<bf16, Small>(a, st) : backward<f16, Small>(a, st);
+    return checked(a.dtype == ROSETTA_BF16 ? backward<bf16, Large> : backward<f16, Large>, a, st);
+  return checked(a.dtype == ROSETTA_BF16 ? backward<bf16, Small> : backward<f16, Small>, a, st);
 }
 
 }  // namespace rosetta

@@ -187,10 +187,11 @@ template <class O, bool ALIGNED, int BX, int BY, int STAGES>
 hipError_t tile(const Q8Args &a, const Plan &p, hipStream_t st) {
   using Tl = Q8Tile<O, BX, BY, STAGES>;
   auto k = k_q8_tile<O, ALIGNED, BX, BY, STAGES>;
+  const size_t blocks = tiles(a.n, BX) * tiles(a.m, BY) * p.splits;
+  if (!grid_fits(blocks, Tl::THREADS)) return hipErrorInvalidConfiguration;
   const hipError_t e = allow_lds(k, Tl::LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)(tiles(a.n, BX) * tiles(a.m, BY) * p.splits)),
-                     dim3(Tl::THREADS), Tl::LDS, st, a, p.splits, p.run);
+  hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(Tl::THREADS), Tl::LDS, st, a, p.splits, p.run);
   return hipGetLastError();
 }
 
@@ -198,10 +199,11 @@ template <class O, int NX, int NY, int WAVES>
 hipError_t thin(const Q8Args &a, const Plan &p, hipStream_t st) {
   using Th = Thin<int8_t, NX, NY, WAVES>;
   auto k = k_q8_thin<O, NX, NY, WAVES>;
+  const size_t blocks = tiles(a.n, 16 * NX) * p.splits;
+  if (!grid_fits(blocks, Th::THREADS)) return hipErrorInvalidConfiguration;
   const hipError_t e = allow_lds(k, Th::LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)(tiles(a.n, 16 * NX) * p.splits)), dim3(Th::THREADS),
-                     Th::LDS, st, a, p.splits, p.run);
+  hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(Th::THREADS), Th::LDS, st, a, p.splits, p.run);
   return hipGetLastError();
 }
 
@@ -215,6 +217,8 @@ hipError_t launch(const Q8Args &a, hipStream_t st) {
   const Operand X{(const char *)a.b, (int64_t)a.b_stride, (int64_t)a.n, (int64_t)a.k};
   const Operand Y{(const char *)a.a, (int64_t)a.a_stride, (int64_t)a.m, (int64_t)a.k};
   const bool al = rows_aligned(X) && rows_aligned(Y);
+  const size_t quads = tiles(a.n, 4) * a.m;
+  if (p.splits > 1 && !grid_fits(tiles(quads, 256), 256)) return hipErrorInvalidConfiguration;
   hipError_t e = hipSuccess;
   switch (p.cut) {
     case Cut::THIN:
@@ -238,7 +242,6 @@ hipError_t launch(const Q8Args &a, hipStream_t st) {
       break;
   }
   if (e != hipSuccess || p.splits == 1) return e;
-  const size_t quads = tiles(a.n, 4) * a.m;
   hipLaunchKernelGGL(k_q8_join<O>, dim3((unsigned)tiles(quads, 256)), dim3(256), 0, st, a,
                      p.splits);
   return hipGetLastError();
