@@ -594,10 +594,10 @@ rosetta_status rosetta_encode_fixed(const double *v, size_t count, int scale_log
 
 /* ---- the clear side: 8-bit layers and the vocabulary loss ----------------
  *
- * What a hybrid program runs in the clear around the encrypted tables
- * (Sec. 2.3: norms, projections, the head), and the loss whose
- * exponential is the perplexity that Sec. 5 judges the tables by, with its
- * gradient.
+ * What it takes to judge a table without encryption: Sec. 5's measure is the
+ * perplexity of a model that uses it over that of the exact one.  Layers in 8
+ * bits around the table's lookups, and the loss whose exponential is the
+ * perplexity; with gradients, to fit a model to a table's range.
  *
  * CONVENTIONS:
  *  - Matrices are row-major device arrays with contiguous rows; a `_stride`

@@ -470,8 +470,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rms_norm_backward(Nor
       }
     };
     // (gh is used last, so it is asked for once the row before is written and stays as
-    // it lies: widened ahead with the others, long rows no longer fit the registers,
-    // 1258 x 16320 in 32 bits 148 us for 106)
+    // it lies: widened ahead with the others, rows of four vectors a thread take more
+    // registers still, 1258 x 16320 in 32 bits 148 us for 106.  Those of 32 bits, and
+    // ragged ones of 16, do not fit as it is: 36 to 208 bytes of a thread's values go
+    // through scratch memory, 3.1 TB/s at that size.)
     auto ask_gh = [&](size_t row) {
       const T *gh = (const T *)a.gh.p + row * a.gh.stride;
 #pragma unroll
