@@ -714,6 +714,137 @@ rosetta_status rosetta_cross_entropy_backward(const void *h, size_t h_stride, co
                                               size_t workspace_bytes, void *stream);
 size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, size_t vocab);
 
+/* ---- the clear side, decoding: an 8-bit cache and drafted tokens ---------
+ *
+ * What a decode in the clear needs around its layers: keys and values kept in 8
+ * bits, attention that reads them, and several tokens drafted for one step and
+ * verified against the model's probabilities.  (How many of a table's drafts the
+ * exact model accepts is a measure of the table: 1 - total variation a token.)
+ *
+ * CONVENTIONS, beside those of the clear side above:
+ *  - A batch is packed: sequence b has rows starts[b] .. starts[b + 1] - 1 of the
+ *    call's `rows`, and they are the last of its lens[b] positions: row i of n
+ *    is position lens[b] - n + i (one before the first position has no place).
+ *    Rows of no sequence (behind the last, say) are left as they were.
+ *  - Position t lies at place t % page of page table[b][t / page].  A position
+ *    outside the table, or whose entry is outside [0, pages), has no place:
+ *    nothing is written for it, it reads as zeros, and attention does not see
+ *    it.  Whatever starts, lens and the table hold, no memory outside the
+ *    call's arrays is touched.
+ *  - `starts` must ascend (where not, which of the rows a sequence gets is
+ *    unspecified).  A page that several entries name is theirs in common: rows
+ *    that one call writes to one place leave unspecified values there.
+ *  - Distinct elements of an array must lie apart; heads may lie within rows or
+ *    rows within heads. */
+
+/* The cache: k and v [pages][kv_heads][page][dim] and their scales
+ * [pages][kv_heads][page], each with the strides given, in elements (so pages of
+ * places of heads, or keys and values in one buffer, will do too).  A head's `dim`
+ * values, and a page's scales of a head, are contiguous.  value = scale * q, as
+ * for the clear side's 8-bit rows, a row being one head of one position.
+ * dim: a multiple of 16 up to 256; page: a power of two from 16 on (else
+ * ROSETTA_ERR_UNSUPPORTED); k and v start on 16 bytes, and their strides are
+ * multiples of 16. */
+typedef struct {
+  int8_t *k, *v;
+  float *k_scale, *v_scale;
+  size_t pages, kv_heads, page, dim;
+  size_t page_stride, head_stride, place_stride;
+  size_t scale_page_stride, scale_head_stride;
+} rosetta_kv_cache;
+
+/* The rows of a call: table [batch][table_len], starts [batch + 1], lens [batch]
+ * (device arrays). */
+typedef struct {
+  const int32_t *table;
+  size_t table_stride, table_len;
+  const int32_t *starts, *lens;
+  size_t batch, rows;
+} rosetta_kv_rows;
+
+/* Keys and values [rows][kv_heads][dim] of type `dtype` to the cache in 8 bits.
+ * scale = max / 127 and value / scale are rounded as divisions of 32-bit floats.
+ * Places that no row names keep what they hold. */
+rosetta_status rosetta_kv_write(const void *k, size_t k_row_stride, size_t k_head_stride,
+                                const void *v, size_t v_row_stride, size_t v_head_stride, int dtype,
+                                const rosetta_kv_cache *cache, const rosetta_kv_rows *rows,
+                                void *stream);
+
+/* The values that the rows' positions hold, rounded to `dtype`. */
+rosetta_status rosetta_kv_read(const rosetta_kv_cache *cache, const rosetta_kv_rows *rows, int dtype,
+                               void *k, size_t k_row_stride, size_t k_head_stride, void *v,
+                               size_t v_row_stride, size_t v_head_stride, void *stream);
+
+/* Of each sequence's rows, the accepted ones moved together: the position of row
+ * i takes what row path[starts[b] + i]'s holds, i < count[b]; the sequence is then
+ * lens_out[b] = lens[b] - n + count[b] positions long.  path and count are as
+ * rosetta_verify_drafts leaves them (path ascends; an entry that is not past its own
+ * place moves nothing).  lens_out must not be lens. */
+rosetta_status rosetta_kv_keep(const rosetta_kv_cache *cache, const rosetta_kv_rows *rows,
+                               const int32_t *path, const int32_t *count, int32_t *lens_out,
+                               void *stream);
+
+/* Which of a sequence's rows each of them follows: bit j % 64 of word j / 64 of
+ * masks [rows][words] says whether row i is row j or has it among its ancestors.
+ * parents [rows]: the place, among its sequence's rows, of each row's parent,
+ * which lies before it; anything else is no parent.  Rows j >= 64 words have no
+ * bit; rows of no sequence get none. */
+rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts, size_t batch,
+                                  size_t rows, size_t words, uint64_t *masks, void *stream);
+
+/* Attention of the rows' queries over the cache, their own entries among it:
+ *   out[r][h] = sum_t softmax_t(scale <q[r][h], k[t]>) v[t],
+ *   lse[r][h] = log sum_t exp(scale <q[r][h], k[t]>)   (32 bits; NULL: not wanted),
+ * head h reading head h / (heads / kv_heads) of the cache.  Row i of n sees the
+ * positions before the rows, and of the rows themselves those up to i, or, with
+ * `masks` [rows][words] (any bits; rosetta_tree_masks makes a tree's), row j where
+ * bit j is set.  A row that sees nothing gives zeros and lse = -infinity.  What a
+ * row does not see does not touch it, whatever it holds; a row of q with a NaN or an
+ * infinity gives NaN.  q, out [rows][heads][dim] of type `dtype` (ROSETTA_BF16 or
+ * ROSETTA_F16; ROSETTA_F32 is ROSETTA_ERR_UNSUPPORTED).  scale >= 0.
+ * max_rows: no sequence has more rows (those behind are left as they were; with
+ * masks, max_rows <= 64 words).  Scores, statistics and sums are 32-bit; the weights
+ * of the values are rounded to f16 with 2^15 for the largest possible (scales of
+ * values from 2^-80 to 2^100 keep their precision).  workspace:
+ * rosetta_kv_attention_workspace_bytes bytes (0 where parts of a sequence need no
+ * joining), positions being table_len * page. */
+rosetta_status rosetta_kv_attention(const void *q, size_t q_row_stride, size_t q_head_stride,
+                                    int dtype, size_t heads, const rosetta_kv_cache *cache,
+                                    const rosetta_kv_rows *rows, size_t max_rows,
+                                    const uint64_t *masks, size_t words, float scale, void *out,
+                                    size_t out_row_stride, size_t out_head_stride, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+size_t rosetta_kv_attention_workspace_bytes(size_t heads, size_t kv_heads, size_t dim, size_t batch,
+                                            size_t rows, size_t max_rows, size_t positions);
+
+/* Drafted tokens verified.  Each sequence's rows are the nodes of a tree: node 0
+ * is the last certain token, parents as for rosetta_tree_masks (NULL: each node's is
+ * the one before).  p [rows][vocab]: the target's probabilities after each node, q
+ * those that the node's children drafts[] were drawn from (both of type `dtype`;
+ * rows of q without children are not read to any effect), u [rows] numbers of [0, 1).
+ * From node 0 on the children of the node reached are tried in order: with c = 0 and
+ * z = 1 at first, child i with token x is accepted if
+ *   u[i] z q[x] < p[x] - c q[x],
+ * and the walk goes on from it; otherwise c grows by z, and z becomes the sum of
+ * r = max(p - c q, 0).  At the end one more token is drawn from the last r (of p
+ * itself where no child was rejected, or r is zero throughout): the first whose running sum is past
+ * u[0] times the whole, or -1 where p is zero throughout.  With children drawn from
+ * q independently of each other, the tokens are distributed as the target's.
+ * Sums are in 64 bits; NaN counts as nothing left.  Nodes whose token is outside
+ * [0, vocab), and those behind a sequence's 1024th, take no part.
+ *   count[b]: the nodes kept, node 0 among them, and as many new tokens (0 for a
+ *   sequence without rows); path, tokens [rows]: those nodes, and those tokens, from
+ *   the sequence's first row on, -1 behind (and before the first sequence and behind
+ *   the last).
+ * workspace: rosetta_verify_drafts_workspace_bytes bytes, on 8 bytes. */
+rosetta_status rosetta_verify_drafts(const void *p, size_t p_stride, const void *q, size_t q_stride,
+                                     int dtype, const int64_t *drafts, const int32_t *parents,
+                                     const float *u, const int32_t *starts, size_t batch,
+                                     size_t rows, size_t vocab, int64_t *tokens, int32_t *path,
+                                     int32_t *count, void *workspace, size_t workspace_bytes,
+                                     void *stream);
+size_t rosetta_verify_drafts_workspace_bytes(size_t batch, size_t vocab);
+
 /* ---- test helpers: host memory, deterministic from the seed ------------ */
 
 /* Key generation for the PBS (Sec. 2.2.2 "TFHE Scheme": LWE encryption of

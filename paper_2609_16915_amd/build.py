@@ -17,7 +17,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librosetta.so")
 SOURCES = ["kernels.hip", "exact_fft.hip", "keyswitch.hip", "lwe_ops.hip", "abi.cpp", "scratch.cpp", "noalloc.hip",
            "host_helpers.cpp", "seglut.cpp", "lookup.cpp", "clear_abi.cpp", "clear_norm.hip",
-           "q8_matmul.hip", "cross_entropy.hip"]
+           "q8_matmul.hip", "cross_entropy.hip", "decode_abi.cpp", "kv_cache.hip",
+           "kv_attention.hip", "verify_drafts.hip"]
 ARCH = os.environ.get("ROSETTA_OFFLOAD_ARCH", "gfx950")
 
 

@@ -170,6 +170,39 @@ SIGNATURES.update({
     "rosetta_cross_entropy_backward_workspace_bytes": (_sz, [_sz, _sz, _sz]),
 })
 
+
+
+class CacheStruct(C.Structure):
+    """rosetta_kv_cache (include/rosetta.h)."""
+
+    _fields_ = ([(name, C.c_void_p) for name in ("k", "v", "k_scale", "v_scale")] +
+                [(name, C.c_size_t) for name in
+                 ("pages", "kv_heads", "page", "dim", "page_stride", "head_stride",
+                  "place_stride", "scale_page_stride", "scale_head_stride")])
+
+
+class RowsStruct(C.Structure):
+    """rosetta_kv_rows (include/rosetta.h)."""
+
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_size_t), ("table_len", C.c_size_t),
+                ("starts", C.c_void_p), ("lens", C.c_void_p), ("batch", C.c_size_t),
+                ("rows", C.c_size_t)]
+
+
+_cp, _rp = C.POINTER(CacheStruct), C.POINTER(RowsStruct)
+SIGNATURES.update({
+    "rosetta_kv_write": (_ST, [_u64p, _sz, _sz, _u64p, _sz, _sz, _i32, _cp, _rp, C.c_void_p]),
+    "rosetta_kv_read": (_ST, [_cp, _rp, _i32, _u64p, _sz, _sz, _u64p, _sz, _sz, C.c_void_p]),
+    "rosetta_kv_keep": (_ST, [_cp, _rp, _u64p, _u64p, _u64p, C.c_void_p]),
+    "rosetta_tree_masks": (_ST, [_u64p, _u64p, _sz, _sz, _sz, _u64p, C.c_void_p]),
+    "rosetta_kv_attention": (_ST, [_u64p, _sz, _sz, _i32, _sz, _cp, _rp, _sz, _u64p, _sz, _f32,
+                                   _u64p, _sz, _sz, _u64p, _u64p, _sz, C.c_void_p]),
+    "rosetta_kv_attention_workspace_bytes": (_sz, [_sz] * 7),
+    "rosetta_verify_drafts": (_ST, [_u64p, _sz, _u64p, _sz, _i32, _u64p, _u64p, _u64p, _u64p, _sz,
+                                    _sz, _sz, _u64p, _u64p, _u64p, _u64p, _sz, C.c_void_p]),
+    "rosetta_verify_drafts_workspace_bytes": (_sz, [_sz, _sz]),
+})
+
 FUNCTIONS = {"inv": 0, "inv_sqrt": 1, "silu": 2, "gelu": 3, "exp": 4}
 SPACINGS = {"uniform": 0, "log": 1}
 FITS = {"linear": 0, "constant": 1}
@@ -754,6 +787,8 @@ def _on_its_stream(call):
         torch = _torch()
         if stream is None:
             first = args[0] if args else kw.get(names[0])
+            if isinstance(first, KVCache):
+                first = first.k
             device = first.get_device() if isinstance(first, _tensor_class()) else -1
             if device < 0 or device == torch._C._cuda_getDevice():
                 return call(*args, **kw)
@@ -937,6 +972,239 @@ def cross_entropy_backward(h, w, targets, lse, gloss, ignore_index: int = -100,
                                                 dim, vocab, ghp, ghs, gwp, gws, sp, sb,
                                                 _stream_of(h, stream)))
     return gh, gw
+
+
+# --------------------------------------------------------------------------
+# the clear side, decoding: an 8-bit cache and drafted tokens (device)
+# --------------------------------------------------------------------------
+
+class KVCache(NamedTuple):
+    """Keys and values in 8 bits: k and v int8 [pages][kv_heads][page][dim] (views
+    with any strides that are multiples of 16, the last dimension contiguous), and
+    their scales float32 [pages][kv_heads][page], contiguous over a page."""
+    k: object
+    v: object
+    k_scale: object
+    v_scale: object
+
+
+def kv_cache(pages: int, kv_heads: int, page: int, dim: int, device="cuda") -> KVCache:
+    """A cache of zeros.  page: a power of two from 16 on; dim: a multiple of 16 up
+    to 256."""
+    torch = _torch()
+    shape = (pages, kv_heads, page, dim)
+    k, v = (torch.zeros(shape, dtype=torch.int8, device=device) for _ in range(2))
+    ks, vs = (torch.zeros(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
+    return KVCache(k, v, ks, vs)
+
+
+def _tensor(t, name: str, dtype, dims: int, device):
+    """A device tensor's (shape, strides), of `dims` dimensions, the last contiguous."""
+    if not isinstance(t, _tensor_class()) or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be a torch tensor" + (f" of {dtype}" if dtype else ""))
+    size, strides = t.shape, t.stride()
+    if len(size) != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, not {tuple(size)}")
+    at = t.get_device()
+    if at < 0 or (device is not None and at != device):
+        _misplaced(t, name, device)
+    if size[-1] > 1 and strides[-1] != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return size, strides
+
+
+def _cache(cache, device=None):
+    """(struct, device) of a cache; strides over one element alone are any."""
+    torch = _torch()
+    if not isinstance(cache, KVCache):
+        raise TypeError("cache must be a KVCache")
+    size, st = _tensor(cache.k, "cache.k", torch.int8, 4, device)
+    on = cache.k.get_device()
+    if _tensor(cache.v, "cache.v", torch.int8, 4, on) != (size, st):
+        raise ValueError("cache.v must have the shape and strides of cache.k")
+    pages, heads, page, dim = size
+    ssize, ss = _tensor(cache.k_scale, "cache.k_scale", torch.float32, 3, on)
+    if ssize != size[:3]:
+        raise ValueError(f"cache.k_scale is {tuple(ssize)}, the call needs {tuple(size[:3])}")
+    if _tensor(cache.v_scale, "cache.v_scale", torch.float32, 3, on) != (ssize, ss):
+        raise ValueError("cache.v_scale must have the shape and strides of cache.k_scale")
+    at_head = st[1] if heads > 1 else 0
+    at_place = st[2] if page > 1 else 0
+    return CacheStruct(
+        cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(),
+        cache.v_scale.data_ptr(), pages, heads, page, dim, st[0] if pages > 1 else 0, at_head,
+        at_place, ss[0] if pages > 1 else 0, ss[1] if heads > 1 else 0), on
+
+
+def _rows(table, starts, lens, rows: int, device):
+    torch = _torch()
+    size, st = _tensor(table, "table", torch.int32, 2, device)
+    batch = size[0]
+    return RowsStruct(table.data_ptr(), st[0] if batch > 1 else size[1], size[1],
+                      _vec(starts, "starts", torch.int32, batch + 1, device),
+                      _vec(lens, "lens", torch.int32, batch, device), batch, rows)
+
+
+def _heads(t, name: str, dtype, shape, device):
+    """(address, row stride, head stride) of [rows][heads][dim]."""
+    size, st = _tensor(t, name, dtype, 3, device)
+    if tuple(size) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(size)}, the call needs {tuple(shape)}")
+    return (t.data_ptr(), st[0] if size[0] > 1 else size[1] * size[2],
+            st[1] if size[1] > 1 else size[2])
+
+
+@_on_its_stream
+def kv_write(k, v, cache, table, starts, lens, stream=None):
+    """Keys and values [rows][kv_heads][dim] (float32, bfloat16 or float16) to the
+    cache in 8 bits, a scale per row and head.  The batch is packed: sequence b has
+    rows starts[b] .. starts[b + 1], the last of its lens[b] positions; position t
+    lies at place t % page of page table[b][t // page] (all int32)."""
+    c, on = _cache(cache)
+    dtype = getattr(k, "dtype", None)
+    rows = k.shape[0] if isinstance(k, _tensor_class()) and k.dim() == 3 else 0
+    shape = (rows, c.kv_heads, c.dim)
+    ka = _heads(k, "k", dtype, shape, on)
+    va = _heads(v, "v", dtype, shape, on)
+    r = _rows(table, starts, lens, rows, on)
+    _check(lib().rosetta_kv_write(*ka, *va, _type(dtype, "k"), c, r, _stream_of(cache.k, stream)))
+
+
+@_on_its_stream
+def kv_read(cache, table, starts, lens, rows: int, dtype, k=None, v=None, stream=None):
+    """(k, v) [rows][kv_heads][dim]: the values that the rows' positions hold.  Rows of
+    no sequence are not written."""
+    c, on = _cache(cache)
+    shape = (rows, c.kv_heads, c.dim)
+    code = _type(dtype, "dtype")
+    r = _rows(table, starts, lens, rows, on)
+    k = cache.k.new_empty(shape, dtype=dtype) if k is None else k
+    v = cache.k.new_empty(shape, dtype=dtype) if v is None else v
+    _check(lib().rosetta_kv_read(c, r, code, *_heads(k, "k", dtype, shape, on),
+                                 *_heads(v, "v", dtype, shape, on), _stream_of(cache.k, stream)))
+    return k, v
+
+
+@_on_its_stream
+def kv_keep(cache, table, starts, lens, path, count, stream=None):
+    """Of each sequence's rows (drafted tokens, say) the accepted ones moved together:
+    row i's position takes what row path[starts[b] + i]'s holds, i < count[b].  Returns
+    the new lens, lens[b] - n + count[b].  path and count as verify_drafts gives them."""
+    torch = _torch()
+    c, on = _cache(cache)
+    rows = path.numel() if isinstance(path, _tensor_class()) else 0
+    pp = _vec(path, "path", torch.int32, rows, on)
+    r = _rows(table, starts, lens, rows, on)
+    cp = _vec(count, "count", torch.int32, r.batch, on)
+    out = lens.new_empty(r.batch, dtype=torch.int32)
+    _check(lib().rosetta_kv_keep(c, r, pp, cp, out.data_ptr(), _stream_of(cache.k, stream)))
+    return out
+
+
+@_on_its_stream
+def tree_masks(parents, starts, max_rows: int, stream=None):
+    """int64 [rows][ceil(max_rows / 64)]: bit j of a row says whether it is its
+    sequence's row j or has it among its ancestors.  parents int32 [rows]: the place of
+    each row's parent among its sequence's rows, -1 for none.  (Zeros for rows of no
+    sequence.)"""
+    torch = _torch()
+    rows = parents.numel() if isinstance(parents, _tensor_class()) else 0
+    on = parents.get_device() if isinstance(parents, _tensor_class()) else -1
+    if max_rows < 1:
+        raise ValueError("max_rows must be at least 1")
+    if on < 0 and isinstance(parents, _tensor_class()):
+        _misplaced(parents, "parents", None)
+    pp = _vec(parents, "parents", torch.int32, rows, on)
+    batch = starts.numel() - 1 if isinstance(starts, _tensor_class()) else 0
+    if batch < 0:
+        raise ValueError("starts holds nothing")
+    sp = _vec(starts, "starts", torch.int32, batch + 1, on)
+    words = -(-max_rows // 64)
+    masks = parents.new_empty((rows, words), dtype=torch.int64)
+    _check(lib().rosetta_tree_masks(pp, sp, batch, rows, words, masks.data_ptr(),
+                                    _stream_of(parents, stream)))
+    return masks
+
+
+@_on_its_stream
+def kv_attention(q, cache, table, starts, lens, masks=None, scale: float = None,
+                 max_rows: int = None, out=None, want_lse: bool = True, workspace=None,
+                 stream=None):
+    """(out, lse) of queries q [rows][heads][dim] (bfloat16 or float16) over the cache,
+    the rows' own entries among it: row i of a sequence sees the positions before its
+    rows, and its rows up to i, or with `masks` (int64 [rows][words], as tree_masks
+    makes them) those whose bit is set.  A row that sees nothing gives zeros and -inf.
+    scale: 1 / sqrt(dim) where not given.  max_rows: the most rows of any sequence (all
+    rows, where not given; fewer leave less to launch).  lse is float32 [rows][heads], or
+    None.  Rows of no sequence, or behind max_rows, are not written."""
+    torch = _torch()
+    c, on = _cache(cache)
+    if not isinstance(q, _tensor_class()):
+        raise TypeError("q must be a torch tensor")
+    dtype = q.dtype
+    code = _type(dtype, "q")
+    rows, heads = q.shape[:2] if q.dim() == 3 else (0, 0)
+    shape = (rows, heads, c.dim)
+    qa = _heads(q, "q", dtype, shape, on)
+    r = _rows(table, starts, lens, rows, on)
+    max_rows = rows if max_rows is None else min(max_rows, rows)
+    if max_rows < 0:
+        raise ValueError("max_rows must not be negative")
+    if scale is None:
+        scale = c.dim ** -0.5
+    mp, words = None, 0
+    if masks is not None:
+        size, _ = _tensor(masks, "masks", torch.int64, 2, on)
+        words = size[1]
+        mp = _vec(masks, "masks", torch.int64, rows * words, on)
+    L = lib()
+    need = L.rosetta_kv_attention_workspace_bytes(heads, c.kv_heads, c.dim, r.batch, rows, max_rows,
+                                                  r.table_len * c.page)
+    wp, wb = None, 0
+    if need:
+        wp, wb, workspace = _scratch(workspace, need, q)
+    out = q.new_empty(shape) if out is None else out
+    lse = q.new_empty((rows, heads), dtype=torch.float32) if want_lse else None
+    _check(L.rosetta_kv_attention(*qa, code, heads, c, r, max_rows, mp, words, scale,
+                                  *_heads(out, "out", dtype, shape, on),
+                                  lse.data_ptr() if want_lse else None, wp, wb,
+                                  _stream_of(q, stream)))
+    return out, lse
+
+
+@_on_its_stream
+def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=None):
+    """(tokens, path, count): drafted tokens verified against the target's probabilities.
+    p, q [rows][vocab] (of one type): the target's after each row, and those that the
+    row's children were drawn from; drafts int64 [rows] the tokens, u float32 [rows]
+    numbers of [0, 1).  A sequence's rows are the nodes of a tree whose node 0 is the
+    last certain token; parents int32 [rows] as for tree_masks (None: each follows the
+    one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
+    how many new tokens there are; path int32 and tokens int64 [rows]: those, from each
+    sequence's first row on, -1 behind."""
+    torch = _torch()
+    pp, ps, rows, vocab = _mat(p, "p")
+    dtype, on = p.dtype, p.get_device()
+    qp, qs = _mat(q, "q", dtype, (rows, vocab), on)[:2]
+    dp = _vec(drafts, "drafts", torch.int64, rows, on)
+    up = _vec(u, "u", torch.float32, rows, on)
+    ap = None if parents is None else _vec(parents, "parents", torch.int32, rows, on)
+    batch = starts.numel() - 1 if isinstance(starts, _tensor_class()) else 0
+    if batch < 0:
+        raise ValueError("starts holds nothing")
+    sp = _vec(starts, "starts", torch.int32, batch + 1, on)
+    L = lib()
+    need = L.rosetta_verify_drafts_workspace_bytes(batch, vocab)
+    wp, wb = None, 0
+    if need:
+        wp, wb, workspace = _scratch(workspace, need, p)
+    tokens = drafts.new_empty(rows)
+    path = starts.new_empty(rows)
+    count = starts.new_empty(batch)
+    _check(L.rosetta_verify_drafts(pp, ps, qp, qs, _type(dtype, "p"), dp, ap, up, sp, batch, rows,
+                                   vocab, tokens.data_ptr(), path.data_ptr(), count.data_ptr(), wp,
+                                   wb, _stream_of(p, stream)))
+    return tokens, path, count
 
 
 # --------------------------------------------------------------------------
