@@ -742,8 +742,8 @@ size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, s
  * places of heads, or keys and values in one buffer, will do too).  A head's `dim`
  * values, and a page's scales of a head, are contiguous.  value = scale * q, as
  * for the clear side's 8-bit rows, a row being one head of one position.
- * dim: a multiple of 16 up to 256; page: a power of two from 16 on (else
- * ROSETTA_ERR_UNSUPPORTED); k and v start on 16 bytes, and their strides are
+ * dim: a multiple of 16 up to 256; page: a power of two from 16 on; table_len *
+ * page at most 2^30 (else ROSETTA_ERR_UNSUPPORTED); k and v start on 16 bytes, and their strides are
  * multiples of 16. */
 typedef struct {
   int8_t *k, *v;
@@ -800,7 +800,8 @@ rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts,
  * `masks` [rows][words] (any bits; rosetta_tree_masks makes a tree's), row j where
  * bit j is set.  A row that sees nothing gives zeros and lse = -infinity.  What a
  * row does not see does not touch it, whatever it holds; a row of q with a NaN or an
- * infinity gives NaN.  q, out [rows][heads][dim] of type `dtype` (ROSETTA_BF16 or
+ * infinity gives NaN, and so does a row that sees a position with a scale that is NaN
+ * or infinite.  q, out [rows][heads][dim] of type `dtype` (ROSETTA_BF16 or
  * ROSETTA_F16; ROSETTA_F32 is ROSETTA_ERR_UNSUPPORTED).  scale >= 0.
  * max_rows: no sequence has more rows (those behind are left as they were; with
  * masks, max_rows <= 64 words).  Scores, statistics and sums are 32-bit; the weights

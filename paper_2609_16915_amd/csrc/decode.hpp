@@ -25,12 +25,15 @@ struct Span {
   int first, n;
   int64_t base;
 };
-__host__ __device__ inline Span span_of(const int *starts, const int *lens, size_t b, size_t rows) {
-  const int64_t s = starts[b], e = starts[b + 1], all = (int64_t)rows;
-  const int64_t first = s < 0 ? 0 : s > all ? all : s;
-  const int64_t last = e < first ? first : e > all ? all : e;
+__host__ __device__ inline Span span_of(int64_t start, int64_t end, int64_t length, size_t rows) {
+  const int64_t all = (int64_t)rows;
+  const int64_t first = start < 0 ? 0 : start > all ? all : start;
+  const int64_t last = end < first ? first : end > all ? all : end;
   const int n = (int)(last - first);
-  return {(int)first, n, (lens ? (int64_t)lens[b] : 0) - n};
+  return {(int)first, n, length - n};
+}
+__host__ __device__ inline Span span_of(const int *starts, const int *lens, size_t b, size_t rows) {
+  return span_of(starts[b], starts[b + 1], lens ? lens[b] : 0, rows);
 }
 
 // Where position t of a sequence lies in the cache: its page, or -1 where there is

@@ -15,7 +15,7 @@ namespace {
 
 // Sizes past these would leave the kernels' index types.
 constexpr size_t MAX_ROWS = (size_t)1 << 30, MAX_HEADS = (size_t)1 << 15, MAX_BATCH = 65535;
-constexpr size_t MAX_TABLE = (size_t)1 << 30, MAX_DIM = 256;
+constexpr size_t MAX_TABLE = (size_t)1 << 30, MAX_DIM = 256;  // (positions; a page's, too)
 constexpr size_t MAX_PLACE = (size_t)1 << 26;  // 16 places stay within 31-bit offsets
 constexpr size_t MAX_VOCAB = (size_t)1 << 30, MAX_WORDS = (size_t)1 << 20;
 
@@ -65,6 +65,8 @@ rosetta_status check_given(const rosetta_kv_cache *c, const rosetta_kv_rows *r, 
     return fail(ROSETTA_ERR_UNSUPPORTED, "%zu rows of %zu sequences, %zu pages each", r->rows,
                 r->batch, r->table_len);
   if (r->table_len < 1) return fail(ROSETTA_ERR_PARAMS, "a table of no pages");
+  if (r->table_len * c->page > MAX_TABLE)
+    return fail(ROSETTA_ERR_UNSUPPORTED, "%zu pages of %zu positions each", r->table_len, c->page);
   Array inner;
   if (c->place_stride % 16 || c->head_stride % 16 || c->page_stride % 16 ||
       c->place_stride > MAX_PLACE ||

@@ -37,6 +37,10 @@ using u32 = uint32_t;
 
 constexpr float NONE = -__builtin_inff();
 
+// (by value: std::min's references kept its operands in scratch memory, and with them
+// all that follows from them in vector registers)
+__device__ inline int least(int a, int b) { return a < b ? a : b; }
+
 // ---- 8 bits to f16 ----
 
 // Pairs (x, y) of bytes, biased by 128, under exponents that make them 1024 + x, + y.
@@ -74,11 +78,36 @@ __device__ inline float across(float a, F f) {
   asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
   return f(a, b);
 }
+// The larger ones, NaN passed over (fmaxf would quiet each operand first).
+__device__ inline float max2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 __device__ inline float row_max(float a) {
-  return across(a, [](float x, float y) { return fmaxf(x, y); });
+  return across(a, [](float x, float y) { return max2(x, y); });
 }
 __device__ inline float row_sum(float a) {
   return across(a, [](float x, float y) { return x + y; });
+}
+// The scales of a position: where that of the value is no number, neither is the score's,
+// and the value counts as 0, so that rows that do not see it are not touched.
+__device__ inline void settle(float &k, float &v) {
+  const bool fine = fabsf(v) < __builtin_inff();
+  k = fine ? k : __builtin_nanf("");
+  v = fine ? v : 0.f;
+}
+
+// The value N lanes on, in a ring of sixteen.
+template <int N>
+__device__ inline float turned(float a) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0x120 + N,
+                                                            0xf, 0xf, false));
 }
 
 // What a launch works on.
@@ -86,14 +115,22 @@ struct Work {
   AttendArgs a;
   int group, parts;  // heads to a head of the cache, parts of a sequence
   int row_blocks;    // workgroups to the rows of a sequence and head
+  int joiners;       // groups of threads to the parts of a row
   float *sums;       // parts > 1: [rows][heads][parts][DIM], (reference, sum) [..][parts]
   float2 *ends;
 };
 
-// One sequence and head of the cache, as its workgroups see it.
+// A word that a whole wave reads, through the scalar cache: what a launch only reads, at
+// an address that all lanes share.
+__device__ inline int shared_word(const int *p) {
+  return *(const __attribute__((address_space(4))) int *)(uintptr_t)p;
+}
+
+// One sequence and head of the cache, as its workgroups see it.  Positions are 32-bit, as
+// lens is (a sequence without any has base = -n).
 struct Seq {
-  Span sp;
-  int64_t length;  // positions that are in the table
+  int first, n, base;
+  int length;  // positions that are in the table
   const int *table;
   const int8_t *k, *v;  // of the head
   const float *ks, *vs;
@@ -101,11 +138,13 @@ struct Seq {
 __device__ inline Seq seq_of(const AttendArgs &a, int b, int head) {
   Seq s;
   const Packed &r = a.packed;
-  s.sp = span_of(r.starts, r.lens, b, r.rows);
-  s.sp.n = s.sp.n < (int)a.max_rows ? s.sp.n : (int)a.max_rows;
+  const int lens = shared_word(r.lens + b);
+  const Span sp = span_of(shared_word(r.starts + b), shared_word(r.starts + b + 1), lens, r.rows);
+  s.first = sp.first;
+  s.n = sp.n < (int)a.max_rows ? sp.n : (int)a.max_rows;
+  s.base = lens > 0 ? lens - sp.n : -sp.n;
   const int64_t capacity = (int64_t)r.table_len << a.cache.page_log;
-  const int64_t length = r.lens[b];
-  s.length = length < 0 ? 0 : length > capacity ? capacity : length;
+  s.length = lens < 0 ? 0 : lens > capacity ? (int)capacity : lens;
   s.table = r.table + b * r.table_stride;
   s.k = a.cache.k + head * a.cache.head_stride;
   s.v = a.cache.v + head * a.cache.head_stride;
@@ -114,26 +153,28 @@ __device__ inline Seq seq_of(const AttendArgs &a, int b, int head) {
   return s;
 }
 
-// Sixteen positions from t on (a multiple of 16), which lie in one page.
+// The page of positions t .. + 15 (t a multiple of 16, so that they lie in one), or what
+// names none.  Asked for ahead of what is read there.
+__device__ inline int entry_at(const Seq &s, const AttendArgs &a, int t) {
+  const u32 at = (u32)t >> a.cache.page_log;
+  return at < a.packed.table_len ? shared_word(s.table + at) : -1;
+}
+
+// Those positions, of the entry's page.
 struct Sixteen {
   const int8_t *k, *v;
   const float *ks, *vs;
-  bool there;  // (where not, page 0 is read and not used)
 };
-__device__ inline Sixteen sixteen_at(const Seq &s, const AttendArgs &a, int64_t t) {
+__device__ inline bool is_page(const AttendArgs &a, int entry) {
+  return (size_t)(u32)entry < a.cache.pages && entry >= 0;
+}
+__device__ inline Sixteen sixteen_at(const Seq &s, const AttendArgs &a, int entry, int t) {
   const Cache &c = a.cache;
-  int64_t pg = page_of(s.table, a.packed.table_len, c.page_log, c.pages, t);
-  Sixteen x;
-  x.there = pg >= 0;
-  pg = pg < 0 ? 0 : pg;
-  const int64_t place = t & (((int64_t)1 << c.page_log) - 1);
-  const int64_t at = pg * c.page_stride + place * c.place_stride;
-  const int64_t sat = pg * c.scale_page_stride + place;
-  x.k = s.k + at;
-  x.v = s.v + at;
-  x.ks = s.ks + sat;
-  x.vs = s.vs + sat;
-  return x;
+  const size_t pg = is_page(a, entry) ? entry : 0;  // (where none, page 0 is read and not used)
+  const size_t place = t & ((1 << c.page_log) - 1);
+  const size_t at = pg * c.page_stride + place * c.place_stride;
+  const size_t sat = pg * c.scale_page_stride + place;
+  return {s.k + at, s.v + at, s.ks + sat, s.vs + sat};
 }
 
 // A row of a workgroup: its query, and where it reads and writes.  rows past the last
@@ -146,7 +187,7 @@ __device__ inline Row row_of(const Seq &s, int r, int group, int kv_head) {
   Row x;
   x.i = r / group;
   x.head = kv_head * group + r % group;
-  x.at = x.i < s.sp.n ? s.sp.first + x.i : -1;
+  x.at = x.i < s.n ? s.first + x.i : -1;
   return x;
 }
 
@@ -201,7 +242,8 @@ struct Rows16 {
         for (int i = 0; i < 8; ++i) h[i] = (_Float16)ldexpf(f[ks][i], up);
         __builtin_memcpy(&q[j][ks], h, 16);
       }
-      factor[j] = ldexpf(a.scale * 1.44269504088896340736f, -up) + odd;
+      // (never 0: what is not seen has a score of -infinity)
+      factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), 0x1p-120f) + odd;
       top[j] = NONE;
       big[j] = 0.f;
       ref[j] = 0.f;
@@ -212,54 +254,59 @@ struct Rows16 {
   }
 
   // Scores s[x][j] (tile x of TILES, four positions of row j) to weights, two tiles to a
-  // fragment.  ks, vs: the scales of the lane's positions.  seen(x, r, j), where MASKED:
+  // fragment.  ks(x), vs(x): the scales of the lane's positions, v_scale a number and
+  // most() the largest.  bits(j), where `masked` (the same in all lanes): bit 16 x + r says
   // whether row j sees position r of tile x.
-  template <bool MASKED, int TILES, class Seen>
-  __device__ void weigh(const v4f (&s)[TILES][NY], const v4f (&ks)[TILES], const v4f (&vs)[TILES],
-                        Seen seen, v4i (&w)[TILES / 2][NY]) {
-    float largest = 0.f;
-    if constexpr (!MASKED) {
+  template <int TILES, class Ks, class Vs, class Most, class Bits>
+  __device__ void weigh(v4f (&s)[TILES][NY], Ks ks, Vs vs, Most most, bool masked, Bits bits,
+                        v4i (&w)[TILES / 2][NY]) {
+    float largest[NY];
 #pragma unroll
-      for (int x = 0; x < TILES; ++x)
+    for (int j = 0; j < NY; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (vs[x][r] < __builtin_inff()) largest = fmaxf(largest, vs[x][r]);
-      largest = row_max(largest);
+      for (int x = 0; x < TILES; ++x) s[x][j] *= ks(x);
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < NY; ++j) {
+        const uint64_t seen = bits(j);
+        float l = 0.f;
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
+          const u32 b = (u32)(seen >> (16 * x)) & 0xf;
+          const v4f v = vs(x);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool there = b & (1u << r);
+            s[x][j][r] = there ? s[x][j][r] : NONE;
+            l = max2(l, there ? v[r] : 0.f);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        largest[j] = row_max(l);
+      }
+    } else {
+      const float l = most();
+#pragma unroll
+      for (int j = 0; j < NY; ++j) largest[j] = l;
     }
     bool grows = false;
     float before[NY];
-    u32 seen_by[NY];
-    float z[NY][TILES][4];
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
       float m = NONE;
-      seen_by[j] = 0;
 #pragma unroll
-      for (int x = 0; x < TILES; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = s[x][j][r] * ks[x][r];
-          if constexpr (MASKED) {
-            const bool there = seen(x, r, j);
-            seen_by[j] |= (u32)there << (4 * x + r);
-            v = there ? v : NONE;
-            if (there && vs[x][r] < __builtin_inff()) largest = fmaxf(largest, vs[x][r]);
-          }
-          z[j][x][r] = v;
-          m = fmaxf(m, v);
-        }
+      for (int x = 0; x < TILES; ++x) {
+        m = max3(m, s[x][j][0], s[x][j][1]);
+        m = max3(m, s[x][j][2], s[x][j][3]);
+      }
       m = row_max(m);
-      if constexpr (MASKED) largest = row_max(largest);
-      before[j] = ref[j];
-      const bool none = top[j] == NONE;
-      grows |= m > top[j] || largest > big[j];
-      top[j] = fmaxf(top[j], m);
-      big[j] = fmaxf(big[j], largest);
+      grows |= m > top[j] || largest[j] > big[j];
+      before[j] = top[j] == NONE ? NONE : ref[j];
+      top[j] = max2(top[j], m);
+      big[j] = max2(big[j], largest[j]);
       int e = __builtin_amdgcn_frexp_expf(big[j]);
       e = e < -80 ? -80 : e > 100 ? 100 : e;
       ref[j] = top[j] == NONE ? 0.f : fmaf(top[j], factor[j], (float)(e - 15));
-      if (none) before[j] = NONE;
-      if constexpr (MASKED) largest = 0.f;
     }
     if (__any(grows)) {
 #pragma unroll
@@ -275,17 +322,12 @@ struct Rows16 {
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
         _Float16 h[4];
+        const v4f v = vs(x);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float p = __builtin_amdgcn_exp2f(fmaf(z[j][x][r], factor[j], -ref[j]));
-          float y = p * vs[x][r];
-          if constexpr (MASKED) {
-            const bool there = seen_by[j] >> (4 * x + r) & 1;
-            p = there ? p : 0.f;
-            y = there ? y : 0.f;
-          }
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[x][j][r], factor[j], -ref[j]));
           sum[j] += p;
-          h[r] = (_Float16)y;
+          h[r] = (_Float16)(p * v[r]);
         }
         __builtin_memcpy((char *)&w[x / 2][j] + 8 * (x % 2), h, 8);
       }
@@ -347,29 +389,48 @@ struct Rows16 {
   }
 };
 
-// Whether a row at place i sees position t, base = its sequence's first row's; masks: of
-// the row, or null.
-__device__ inline bool sees(const Seq &s, const AttendArgs &a, const uint64_t *mask, int i,
-                            int64_t t) {
-  const int64_t j = t - s.sp.base;
-  if (t >= s.length) return false;
-  if (j < 0) return true;
-  if (!a.masks) return j <= i;
-  return j < s.sp.n && j < (int64_t)a.words * 64 && mask && (mask[j >> 6] >> (j & 63) & 1);
+// The first n of 64 bits.
+__device__ inline uint64_t below(int64_t n) {
+  return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
+}
+
+// Which of the 64 positions from t on the row at place i sees (mask: its words, where the
+// call has masks and the row is one).
+__device__ inline uint64_t seen_from(const Seq &s, const AttendArgs &a, const uint64_t *mask, int i,
+                                     int t) {
+  const uint64_t there = below(s.length - t);
+  const int j = t - s.base;  // of bit 0
+  if (!a.masks) return there & below((int64_t)i + 1 - j);
+  uint64_t m = 0;
+  if (mask && j > -64 && j < s.n) {
+    if (j < 0) {
+      m = mask[0] << -j;
+    } else {
+      const size_t word = j >> 6;
+      const int by = j & 63;
+      if (word < a.words) m = mask[word] >> by;
+      if (by && word + 1 < a.words) m |= mask[word + 1] << (64 - by);
+    }
+    m &= below(s.n - j);
+  }
+  return there & (below(-(int64_t)j) | m);
 }
 
 // [from, to) of part `part` of `length` positions, multiples of `unit` but for the end.
-__device__ inline void part_of(int64_t length, int parts, int part, int unit, int64_t &from,
-                               int64_t &to) {
-  const int64_t units = (length + unit - 1) / unit;
-  from = units * part / parts * unit;
-  to = units * (part + 1) / parts * unit;
-  to = to < length ? to : length;
+__device__ inline void part_of(int length, int parts, int part, int unit, int &from, int &to) {
+  const int64_t units = ((int64_t)length + unit - 1) / unit;
+  from = (int)(units * part / parts * unit);
+  const int64_t end = units * (part + 1) / parts * unit;
+  to = end < length ? (int)end : length;
 }
 
 // ---- few rows: the cache goes by once, straight to registers ----
+//
+// The waves take steps of 32 positions in turn.  A step's keys make room for the next
+// one's as soon as the scores are there, its values after the second product: no
+// register waits twice, and the other waves' work covers the rest of the way.
 template <int D, int NY>
-__global__ void __launch_bounds__(256) k_attend_few(Work w) {
+__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const AttendArgs &a = w.a;
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
@@ -383,8 +444,62 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
   const int part = id % (unsigned)w.parts, block = id / (unsigned)w.parts;
   const Seq s = seq_of(a, b, head);
   const int r0 = block * 16 * NY;
-  if (r0 >= s.sp.n * w.group) return;
+  if (r0 >= s.n * w.group) return;
   auto row = [&](int j) { return row_of(s, r0 + 16 * j + m, w.group, head); };
+
+  // positions that some row sees, and that every row sees
+  const int last = least((r0 + 16 * NY - 1) / w.group, s.n - 1);
+  const int end = a.masks ? s.length : least(s.length, s.base + last + 1);
+  const int all = least(s.length, s.base + (a.masks ? 0 : r0 / w.group + 1));
+  int from, to;
+  part_of(end < 0 ? 0 : end, w.parts, part, 32, from, to);
+
+  constexpr int NS = D / 64, VB = D / 16;  // K: 16 bytes of NS chunks, V: VB bytes of a row
+  using vb = std::conditional_t<VB == 4, int, std::conditional_t<VB == 8, v2i, v4i>>;
+  v4i fk[2][NS];
+  vb fv[2][4];
+  v4f fks[2], fvs[2];
+  const u32 dim = (u32)a.cache.dim, stride = (u32)a.cache.place_stride;
+  u32 kat[NS];
+#pragma unroll
+  for (int c = 0; c < NS; ++c) kat[c] = m * stride + (64 * c + 16 * g < dim ? 64 * c + 16 * g : 0);
+  const u32 vat = 4 * g * stride + (VB * m < dim ? VB * m : 0);
+  auto load_keys = [&](const Sixteen (&at)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int c = 0; c < NS; ++c) fk[h][c] = *(const v4i *)(at[h].k + kat[c]);
+    }
+  };
+  auto load_values = [&](const Sixteen (&at)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) fv[h][r] = *(const vb *)(at[h].v + vat + r * stride);
+    }
+  };
+  auto load_scales = [&](const Sixteen (&at)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __builtin_memcpy(&fks[h], at[h].ks + 4 * g, 16);
+      __builtin_memcpy(&fvs[h], at[h].vs + 4 * g, 16);
+    }
+  };
+  constexpr int TURN = 4 * 32;
+  int t = from + 32 * wave;
+  // table entries: of this step, and of the next
+  int now[2], next[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    now[h] = t < to ? entry_at(s, a, t + 16 * h) : -1;
+    next[h] = t + TURN < to ? entry_at(s, a, t + TURN + 16 * h) : -1;
+  }
+  if (t < to) {
+    const Sixteen at[2] = {sixteen_at(s, a, now[0], t), sixteen_at(s, a, now[1], t + 16)};
+    load_keys(at);
+    load_scales(at);
+    load_values(at);
+  }
 
   // product ks of 32 takes bytes 16 g + 8 (ks % 2) .. + 8 of chunk ks / 2 of 64
   Rows16<D, NY> x;
@@ -392,41 +507,15 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
   if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, row, first);
   else x.template load<f16>(a, row, first);
 
-  // positions that some row sees, and that every row sees
-  const int last = std::min((r0 + 16 * NY - 1) / w.group, s.sp.n - 1);
-  int64_t end = a.masks ? s.length : std::min(s.length, s.sp.base + last + 1);
-  const int64_t all = std::min(s.length, s.sp.base + (a.masks ? 0 : r0 / w.group + 1));
-  int64_t from, to;
-  part_of(end < 0 ? 0 : end, w.parts, part, 32, from, to);
-
-  constexpr int NS = D / 64, VB = D / 16;  // K: 16 bytes of NS chunks, V: VB bytes of a row
-  using vb = std::conditional_t<VB == 4, int, std::conditional_t<VB == 8, v2i, v4i>>;
-  struct Step {
-    v4i k[2][NS];
-    vb v[2][4];
-    v4f ks[2], vs[2];
-    bool there;
-  };
-  const int dim = (int)a.cache.dim, stride = (int)a.cache.place_stride;
-  int kat[NS], vat;
+  for (; t < to; t += TURN) {
+    const bool more = t + TURN < to;
+    const Sixteen ahead[2] = {sixteen_at(s, a, next[0], t + TURN),
+                              sixteen_at(s, a, next[1], t + TURN + 16)};
+    int later[2] = {-1, -1};
+    if (t + 2 * TURN < to) {
 #pragma unroll
-  for (int c = 0; c < NS; ++c) kat[c] = m * stride + (64 * c + 16 * g < dim ? 64 * c + 16 * g : 0);
-  vat = 4 * g * stride + (VB * m < dim ? VB * m : 0);
-  auto load = [&](Step &f, int64_t t) {
-    f.there = true;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Sixteen at = sixteen_at(s, a, t + 16 * h);
-      f.there = f.there && at.there;
-#pragma unroll
-      for (int c = 0; c < NS; ++c) f.k[h][c] = *(const v4i *)(at.k + kat[c]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) f.v[h][r] = *(const vb *)(at.v + vat + r * stride);
-      __builtin_memcpy(&f.ks[h], at.ks + 4 * g, 16);
-      __builtin_memcpy(&f.vs[h], at.vs + 4 * g, 16);
+      for (int h = 0; h < 2; ++h) later[h] = entry_at(s, a, t + 2 * TURN + 16 * h);
     }
-  };
-  auto use = [&](const Step &f, int64_t t) {
     v4f sc[2][NY];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -436,8 +525,8 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int c = 0; c < NS; ++c) {
-        const v2i a0 = widen(f.k[h][c].x), a1 = widen(f.k[h][c].y);
-        const v2i b0 = widen(f.k[h][c].z), b1 = widen(f.k[h][c].w);
+        const v2i a0 = widen(fk[h][c].x), a1 = widen(fk[h][c].y);
+        const v2i b0 = widen(fk[h][c].z), b1 = widen(fk[h][c].w);
         const v4i ka = {a0.x, a0.y, a1.x, a1.y}, kb = {b0.x, b0.y, b1.x, b1.y};
 #pragma unroll
         for (int j = 0; j < NY; ++j) {
@@ -445,26 +534,40 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
           sc[h][j] = mac(kb, x.q[j][2 * c + 1], sc[h][j]);
         }
       }
-    v4i p[1][NY];
-    if (t + 32 <= all && f.there) {
-      x.template weigh<false>(sc, f.ks, f.vs, [](int, int, int) { return true; }, p);
-    } else {
-      const bool there[2] = {sixteen_at(s, a, t).there, sixteen_at(s, a, t + 16).there};
-      const uint64_t *mask[NY];
-      int at[NY];
+    if (more) load_keys(ahead);
 #pragma unroll
-      for (int j = 0; j < NY; ++j) {
-        const Row r = row(j);
-        at[j] = r.i;
-        mask[j] = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float k = fks[h][r], v = fvs[h][r];
+        settle(k, v);
+        fks[h][r] = k;
+        fvs[h][r] = v;
       }
-      x.template weigh<true>(sc, f.ks, f.vs, [&](int h, int r, int j) {
-        return there[h] && sees(s, a, mask[j], at[j], t + 16 * h + 4 * g + r);
-      }, p);
-    }
+    v4i p[1][NY];
+    const bool there[2] = {is_page(a, now[0]), is_page(a, now[1])};
+    const uint64_t in = (there[0] ? 0xffffu : 0u) | (there[1] ? 0xffff0000u : 0u);
+    x.template weigh<2>(
+        sc, [&](int h) { return fks[h]; }, [&](int h) { return fvs[h]; },
+        [&] {
+          float v = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) v = max3(v, fvs[h][r], fvs[h][r + 1]);
+          return row_max(v);
+        },
+        !(t + 32 <= all && there[0] && there[1]),
+        [&](int j) {
+          const Row r = row(j);
+          const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
+          return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
+        },
+        p);
+    if (more) load_scales(ahead);
     auto bytes = [&](int h, int r, int word) {
-      if constexpr (VB == 4) return (u32)f.v[h][r];
-      else return (u32)f.v[h][r][word];
+      if constexpr (VB == 4) return (u32)fv[h][r];
+      else return (u32)fv[h][r][word];
     };
 #pragma unroll
     for (int word = 0; word < VB / 4; ++word) {
@@ -482,18 +585,12 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
       turn(std::integral_constant<int, 2>{});
       turn(std::integral_constant<int, 3>{});
     }
-  };
-  // the waves take steps of 32 positions in turn, the next one's loads under way
-  constexpr int TURN = 4 * 32;
-  Step f, n;
-  int64_t t = from + 32 * wave;
-  if (t < to) load(f, t);
-  for (; t < to; t += 2 * TURN) {
-    if (t + TURN < to) load(n, t + TURN);
-    use(f, t);
-    if (t + TURN >= to) break;
-    if (t + 2 * TURN < to) load(f, t + 2 * TURN);
-    use(n, t + TURN);
+    if (more) load_values(ahead);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      now[h] = next[h];
+      next[h] = later[h];
+    }
   }
 
   // The waves' sums together, in order: waves 2 and 3 to 0 and 1, 1 to 0.
@@ -541,39 +638,283 @@ __global__ void __launch_bounds__(256) k_attend_few(Work w) {
   }
 }
 
-// ---- parts of a sequence joined: one thread to four outputs of a row ----
+// ---- many rows: tiles of the cache widened once, in LDS, for all of a workgroup's rows ----
+//
+// A tile is 64 positions.  Each of the four waves brings in sixteen of them and writes
+// them to LDS as the fragments that the products take, so that every read there is 16
+// bytes a lane, in lane order.  One tile is used while the next is written and the one
+// after is on its way.
+template <int D, int NY>
+struct Many {
+  static constexpr int KS = D / 32, NX = D / 16, NS = D / 64, VB = D / 16;
+  static constexpr int TILE = 64;
+  static constexpr int KEYS = 4 * KS * 1024, VALUES = 2 * NX * 1024;
+  static constexpr int STAGE = KEYS + VALUES + 2 * TILE * 4 + 32;  // and scales, what is there, largest
+  static constexpr int LDS = 2 * STAGE;
+  static constexpr int ROWS = 4 * 16 * NY;
+};
+
+template <int D, int NY>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
+  using M = Many<D, NY>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const AttendArgs &a = w.a;
+  const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int kv_heads = (int)a.cache.kv_heads;
+  // the blocks of one head's part are neighbours on one XCD, those with most to see first
+  const unsigned id = xcd_block(blockIdx.x, gridDim.x);
+  const int block = w.row_blocks - 1 - id % (unsigned)w.row_blocks;
+  unsigned rest = id / (unsigned)w.row_blocks;
+  const int head = rest % kv_heads;
+  rest /= kv_heads;
+  const int part = rest % (unsigned)w.parts, b = rest / (unsigned)w.parts;
+  const Seq s = seq_of(a, b, head);
+  const int r0 = block * M::ROWS;
+  if (r0 >= s.n * w.group) return;
+  const int rw = r0 + 16 * NY * wave;
+  auto row = [&](int j) { return row_of(s, rw + 16 * j + m, w.group, head); };
+
+  Rows16<D, NY> x;
+  auto first = [&](int ks) { return 32 * ks + 8 * g; };
+  if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, row, first);
+  else x.template load<f16>(a, row, first);
+
+  // what some row of the workgroup sees, of this wave sees, and all of this wave's see
+  const int n1 = s.n - 1;
+  const int last = least((r0 + M::ROWS - 1) / w.group, n1);
+  const int mine = least((rw + 16 * NY - 1) / w.group, n1);
+  const int end = a.masks ? s.length : least(s.length, s.base + last + 1);
+  int some = a.masks ? s.length : least(s.length, s.base + mine + 1);
+  const int all = least(s.length, s.base + (a.masks ? 0 : rw / w.group + 1));
+  if (rw >= s.n * w.group) some = 0;
+  int from, to;
+  part_of(end < 0 ? 0 : end, w.parts, part, M::TILE, from, to);
+
+  using vb = std::conditional_t<M::VB == 4, int, std::conditional_t<M::VB == 8, v2i, v4i>>;
+  struct Sub {
+    v4i k[M::NS];
+    vb v[4];
+    float ks, vs;
+    bool there;
+  } sub;
+  const u32 dim = (u32)a.cache.dim, stride = (u32)a.cache.place_stride;
+  u32 kat[M::NS];
+#pragma unroll
+  for (int c = 0; c < M::NS; ++c)
+    kat[c] = m * stride + (64 * c + 16 * g < dim ? 64 * c + 16 * g : 0);
+  const u32 vat = 4 * g * stride + (M::VB * m < dim ? M::VB * m : 0);
+  // (the table's entry for the tile after the one to be loaded is asked for with it)
+  int entry = from < to ? entry_at(s, a, from + 16 * wave) : -1;
+  auto load = [&](int t) {
+    const Sixteen at = sixteen_at(s, a, entry, t + 16 * wave);
+    sub.there = is_page(a, entry);
+    entry = t + M::TILE < to ? entry_at(s, a, t + M::TILE + 16 * wave) : -1;
+#pragma unroll
+    for (int c = 0; c < M::NS; ++c) sub.k[c] = *(const v4i *)(at.k + kat[c]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sub.v[r] = *(const vb *)(at.v + vat + r * stride);
+    sub.ks = at.ks[m];
+    sub.vs = at.vs[m];
+  };
+  auto write = [&](char *stage) {
+#pragma unroll
+    for (int c = 0; c < M::NS; ++c) {
+      char *to = stage + (((wave * M::KS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
+      const v2i a0 = widen(sub.k[c].x), a1 = widen(sub.k[c].y);
+      const v2i b0 = widen(sub.k[c].z), b1 = widen(sub.k[c].w);
+      *(v4i *)to = v4i{a0.x, a0.y, a1.x, a1.y};
+      *(v4i *)(to + 256) = v4i{b0.x, b0.y, b1.x, b1.y};
+    }
+    auto word = [&](int r, int i) {
+      if constexpr (M::VB == 4) return (u32)sub.v[r];
+      else return (u32)sub.v[r][i];
+    };
+    char *to = stage + M::KEYS + wave / 2 * M::NX * 1024 + lane * 16 + wave % 2 * 8;
+#pragma unroll
+    for (int i = 0; i < M::VB / 4; ++i) {
+      auto turn = [&](auto byte) {
+        constexpr int I = decltype(byte)::value;
+        *(v2i *)(to + (4 * i + I) * 1024) = v2i{(int)widen_two<I>(word(0, i), word(1, i)),
+                                               (int)widen_two<I>(word(2, i), word(3, i))};
+      };
+      turn(std::integral_constant<int, 0>{});
+      turn(std::integral_constant<int, 1>{});
+      turn(std::integral_constant<int, 2>{});
+      turn(std::integral_constant<int, 3>{});
+    }
+    float *scales = (float *)(stage + M::KEYS + M::VALUES);
+    settle(sub.ks, sub.vs);
+    if (lane < 16) scales[16 * wave + m] = sub.ks;
+    if (lane < 16) scales[M::TILE + 16 * wave + m] = sub.vs;
+    // the largest v_scale of the sixteen
+    float most = sub.vs;
+    most = max2(most, turned<8>(most));
+    most = max2(most, turned<4>(most));
+    most = max2(most, turned<2>(most));
+    most = max2(most, turned<1>(most));
+    if (lane == 0) {
+      ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
+      scales[2 * M::TILE + 4 + wave] = most;
+    }
+  };
+  auto use = [&](const char *stage, int t) {
+    const v4i *keys = (const v4i *)stage + lane;
+    const v4i *values = (const v4i *)(stage + M::KEYS) + lane;
+    const float *scales = (const float *)(stage + M::KEYS + M::VALUES);
+    auto ks = [&](int h) { return *(const v4f *)(scales + 16 * h + 4 * g); };
+    auto vs = [&](int h) { return *(const v4f *)(scales + M::TILE + 16 * h + 4 * g); };
+    v4f sc[4][NY];
+    // the next fragments on their way while the present ones are multiplied (and no more:
+    // all of them at once do not fit the registers)
+    v4i kf[2][M::KS];
+#pragma unroll
+    for (int c = 0; c < M::KS; ++c) kf[0][c] = keys[c * 64];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+#pragma unroll
+      for (int j = 0; j < NY; ++j) sc[h][j] = v4f{0, 0, 0, 0};
+      if (h < 3) {
+#pragma unroll
+        for (int c = 0; c < M::KS; ++c) kf[(h + 1) % 2][c] = keys[((h + 1) * M::KS + c) * 64];
+      }
+#pragma unroll
+      for (int c = 0; c < M::KS; ++c)
+#pragma unroll
+        for (int j = 0; j < NY; ++j) sc[h][j] = mac(kf[h % 2][c], x.q[j][c], sc[h][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const int *there = (const int *)(scales + 2 * M::TILE);
+    const int here = __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3]);
+    v4i p[2][NY];
+    x.template weigh<4>(
+        sc, ks, vs,
+        [&] {
+          const v4f most = *(const v4f *)(scales + 2 * M::TILE + 4);
+          return max3(max2(most[0], most[1]), most[2], most[3]);
+        },
+        !(t + M::TILE <= all && here),
+        [&](int j) {
+          uint64_t in = 0;
+#pragma unroll
+          for (int h = 0; h < 4; ++h) in |= (uint64_t)(there[h] ? 0xffff : 0) << (16 * h);
+          const Row r = row(j);
+          const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
+          return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
+        },
+        p);
+    constexpr int G = 4, GROUPS = 2 * M::NX / G;
+    v4i vf[2][G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) vf[0][i] = values[i * 64];
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) {
+      if (n + 1 < GROUPS) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) vf[(n + 1) % 2][i] = values[((n + 1) * G + i) * 64];
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const int at = (n * G + i) % M::NX, u = n * G / M::NX;
+#pragma unroll
+        for (int j = 0; j < NY; ++j) x.o[at][j] = mac(vf[n % 2][i], p[u][j], x.o[at][j]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (from < to) {
+    load(from);
+    write(lds);
+    if (from + M::TILE < to) load(from + M::TILE);
+  }
+  int at = 0;
+  auto next = [&](int t) {
+    __syncthreads();  // this tile is written, and the one before it no longer read
+    if (t + M::TILE < to) {
+      write(lds + (at ^ 1) * M::STAGE);
+      if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
+    }
+  };
+  int t = from;
+  for (; t < least(some, to); t += M::TILE, at ^= 1) {
+    next(t);
+    use(lds + at * M::STAGE, t);
+  }
+  for (; t < to; t += M::TILE, at ^= 1) next(t);  // (what only other waves see)
+#pragma unroll
+  for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
+}
+
+// ---- parts of a sequence joined ----
+//
+// D / 4 threads of four outputs to a row, and `w.joiners` such groups, a power of two, to
+// its parts: bound by latency, so that a thread's parts are read ahead of each other.
+// 128 parts of 32 rows: 86 us with one group.
 template <int D>
 __global__ void __launch_bounds__(256) k_attend_join(Work w) {
   const AttendArgs &a = w.a;
-  constexpr int LANES = D / 4, ROWS = 256 / LANES;
-  const Span sp = span_of(a.packed.starts, a.packed.lens, blockIdx.y, a.packed.rows);
-  const int n = sp.n < (int)a.max_rows ? sp.n : (int)a.max_rows;
-  const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (r >= n * (int64_t)a.heads) return;
-  const int lane = threadIdx.x % LANES;
-  const size_t row = sp.first * a.heads + r;
-  const float2 *ends = w.ends + row * w.parts;
-  const v4f *sums = (const v4f *)(w.sums + row * w.parts * D) + lane;
-  float ref = NONE;
-  bool any = false;
-  for (int p = 0; p < w.parts; ++p) {
-    any |= ends[p].x != NONE;
-    ref = fmaxf(ref, ends[p].x);
-  }
-  float total = 0.f;
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+  __shared__ v4f sums[GROUPS][LANES];
+  __shared__ float2 ends[GROUPS];
+  const Seq s = seq_of(a, blockIdx.y, 0);
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int sub = group % w.joiners;
+  const int64_t r = (int64_t)blockIdx.x * (GROUPS / w.joiners) + group / w.joiners;
+  const bool mine = r < s.n * (int64_t)a.heads;
+  const size_t row = s.first * a.heads + r;
+  const float2 *from = w.ends + row * w.parts;
+  const v4f *parts = (const v4f *)(w.sums + row * w.parts * D) + lane;
+  // the parts sub, sub + joiners, ...
+  constexpr int AHEAD = 4;
+  float ref = NONE, total = 0.f;
   v4f o = {0, 0, 0, 0};
-  for (int p = 0; p < w.parts; ++p) {
-    const float2 e = ends[p];
-    if (e.x == NONE) continue;
-    const float f = __builtin_amdgcn_exp2f(e.x - ref);
-    total += e.y * f;
-    o += sums[(size_t)p * LANES] * f;
+  for (int p0 = sub; mine && p0 < w.parts; p0 += AHEAD * w.joiners) {
+    float2 e[AHEAD];
+    v4f v[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int p = least(p0 + i * w.joiners, w.parts - 1);
+      e[i] = from[p];
+      v[i] = parts[(size_t)p * LANES];
+    }
+    const float before = ref;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (p0 + i * w.joiners >= w.parts) e[i].x = NONE;
+      ref = fmaxf(ref, e[i].x);
+    }
+    if (ref == NONE) continue;
+    const float by = __builtin_amdgcn_exp2f(before - ref);
+    total *= by;
+    o *= by;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (e[i].x == NONE) continue;  // (its outputs were not written)
+      const float f = __builtin_amdgcn_exp2f(e[i].x - ref);
+      total += e[i].y * f;
+      o += v[i] * f;
+    }
   }
-  const float inv = any ? 1.f / total : 0.f;
-  if (a.lse && lane == 0) a.lse[row] = any ? (ref + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : NONE;
+  sums[group][lane] = o;
+  if (lane == 0) ends[group] = float2{ref, total};
+  __syncthreads();
+  if (sub || !mine) return;
+  float all = NONE;
+  for (int i = 0; i < w.joiners; ++i) all = fmaxf(all, ends[group + i].x);
+  const bool none = all == NONE;
+  total = 0.f;
+  o = v4f{0, 0, 0, 0};
+  for (int i = 0; i < w.joiners && !none; ++i) {
+    const float f = __builtin_amdgcn_exp2f(ends[group + i].x - all);
+    total += ends[group + i].y * f;
+    o += sums[group + i][lane] * f;
+  }
+  const float inv = none ? 0.f : 1.f / total;
+  if (a.lse && lane == 0)
+    a.lse[row] = none ? NONE : (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
   if (lane * 4 >= (int)a.cache.dim) return;
   Row at;
-  at.at = sp.first + (int)(r / (int64_t)a.heads);
+  at.at = s.first + (int)(r / (int64_t)a.heads);
   at.head = (int)(r % (int64_t)a.heads);
   const float f[8] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   Rows16<D, 1>::put8(a, at, lane * 4, f, 4);
@@ -585,6 +926,7 @@ namespace {
 
 struct Plan {
   int d, ny, parts, row_blocks;
+  bool many;
 };
 
 Plan plan_of(size_t heads, size_t kv_heads, size_t dim, size_t batch, size_t max_rows,
@@ -592,10 +934,14 @@ Plan plan_of(size_t heads, size_t kv_heads, size_t dim, size_t batch, size_t max
   Plan p;
   p.d = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
   const size_t group = heads / kv_heads, rows = max_rows * group;
-  p.ny = rows <= 16 || p.d == 256 ? 1 : 2;  // (two groups of 256 do not fit the registers)
-  p.row_blocks = (int)((rows + 16 * p.ny - 1) / (16 * p.ny));
+  p.many = rows > 32;
+  // (two groups of 256 do not fit the registers beside what is on its way)
+  p.ny = p.d == 256 || rows <= 16 ? 1 : 2;
+  const size_t each = 16 * p.ny * (p.many ? 4 : 1);
+  p.row_blocks = (int)((rows + each - 1) / each);
   const size_t blocks = batch * kv_heads * p.row_blocks;
-  size_t parts = blocks ? (1024 + blocks - 1) / blocks : 1;
+  const size_t wanted = p.many ? 512 : 1024;
+  size_t parts = blocks ? (wanted + blocks - 1) / blocks : 1;
   parts = std::min(parts, (positions + 127) / 128);
   p.parts = (int)std::max<size_t>(1, std::min<size_t>(parts, 128));
   return p;
@@ -619,13 +965,16 @@ size_t kv_attention_workspace(size_t heads, size_t kv_heads, size_t dim, size_t 
 hipError_t launch_kv_attention(const AttendArgs &a, hipStream_t st) {
   const size_t positions = a.packed.table_len << a.cache.page_log;
   const Plan p = plan_of(a.heads, a.cache.kv_heads, a.cache.dim, a.packed.batch, a.max_rows, positions);
-  Work w{a, (int)(a.heads / a.cache.kv_heads), p.parts, p.row_blocks, nullptr, nullptr};
+  Work w{a, (int)(a.heads / a.cache.kv_heads), p.parts, p.row_blocks, 1, nullptr, nullptr};
   if (p.parts > 1) {
     w.sums = (float *)a.workspace;
     w.ends = (float2 *)(w.sums + a.packed.rows * a.heads * p.parts * p.d);
   }
   const size_t blocks = a.packed.batch * a.cache.kv_heads * p.parts * p.row_blocks;
-  const size_t joins = (a.max_rows * a.heads * p.d / 4 + 255) / 256;
+  // (a few parts to a group of threads)
+  const int groups = 1024 / p.d;
+  while (w.joiners < groups && w.joiners * 4 < p.parts) w.joiners *= 2;
+  const size_t each = groups / w.joiners, joins = (a.max_rows * a.heads + each - 1) / each;
   if (!grid_fits(blocks, 256) || (p.parts > 1 && (a.packed.batch > 65535 || !grid_fits(joins * a.packed.batch, 256))))
     return hipErrorInvalidConfiguration;
   return by_dim(p.d, [&](auto d) {
@@ -639,7 +988,14 @@ hipError_t launch_kv_attention(const AttendArgs &a, hipStream_t st) {
       hipLaunchKernelGGL((k_attend_few<D, NY>), dim3((unsigned)blocks), dim3(256), LDS, st, w);
       e = hipGetLastError();
     };
-    if (p.ny == 1) few(std::integral_constant<int, 1>{});
+    if (p.many) {
+      constexpr int NY = D == 256 ? 1 : 2;
+      using M = Many<D, NY>;
+      e = allow_lds(k_attend_many<D, NY>, M::LDS);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((k_attend_many<D, NY>), dim3((unsigned)blocks), dim3(256), M::LDS, st, w);
+      e = hipGetLastError();
+    } else if (p.ny == 1) few(std::integral_constant<int, 1>{});
     else if constexpr (D < 256) few(std::integral_constant<int, 2>{});
     if (e != hipSuccess || p.parts == 1) return e;
     hipLaunchKernelGGL(k_attend_join<D>, dim3((unsigned)joins, (unsigned)a.packed.batch), dim3(256), 0,

@@ -63,7 +63,8 @@ COMMON = [
     (dict(dim=272), UNSUPPORTED), (dict(page=8), UNSUPPORTED), (dict(page=48), UNSUPPORTED),
     (dict(page=0), UNSUPPORTED), (dict(pages=1 << 31), UNSUPPORTED),
     (dict(batch=65536), UNSUPPORTED), (dict(rows=1 << 30), UNSUPPORTED),
-    (dict(table_len=0), PARAMS), (dict(table_stride=2), PARAMS),
+    (dict(table_len=0), PARAMS),
+    (dict(table_len=(1 << 26) + 1, table_stride=1 << 27), UNSUPPORTED), (dict(table_stride=2), PARAMS),
     (dict(place_stride=56), PARAMS), (dict(place_stride=48), PARAMS),
     (dict(head_stride=1008), PARAMS), (dict(page_stride=2032), PARAMS),
     (dict(head_stride=1032), PARAMS), (dict(page_stride=2056), PARAMS),
