@@ -253,23 +253,32 @@ struct Rows16 {
     }
   }
 
-  // Scores s[x][j] (tile x of TILES, four positions of row j) to weights, two tiles to a
-  // fragment.  ks(x), vs(x): the scales of the lane's positions, v_scale a number and
-  // most() the largest.  bits(j), where `masked` (the same in all lanes): bit 16 x + r says
-  // whether row j sees position r of tile x.
-  template <int TILES, class Ks, class Vs, class Most, class Bits>
-  __device__ void weigh(v4f (&s)[TILES][NY], Ks ks, Vs vs, Most most, bool masked, Bits bits,
-                        v4i (&w)[TILES / 2][NY]) {
+  // Scores s[x][j] (tile x of TILES, four positions of row j): times their keys' scales,
+  // and the largest so far.
+  template <int TILES>
+  __device__ static void scaled(v4f (&s)[TILES][NY], int x, const v4f &ks, float (&m)[NY]) {
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      s[x][j] *= ks;
+      m[j] = max3(m[j], s[x][j][0], s[x][j][1]);
+      m[j] = max3(m[j], s[x][j][2], s[x][j][3]);
+    }
+  }
+
+  // The references for the scores s, m their largest: what was added up so far goes over to
+  // them.  vs(x): the values' scales of the lane's positions, most() the largest of all.
+  // bits(j), where `masked` (the same in all lanes): bit 16 x + r says whether row j sees
+  // position r of tile x; what it does not see becomes -infinity.
+  template <int TILES, class Vs, class Most, class Bits>
+  __device__ void refer(v4f (&s)[TILES][NY], float (&m)[NY], Vs vs, Most most, bool masked,
+                        Bits bits) {
     float largest[NY];
-#pragma unroll
-    for (int j = 0; j < NY; ++j)
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) s[x][j] *= ks(x);
     if (masked) {
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
         const uint64_t seen = bits(j);
         float l = 0.f;
+        m[j] = NONE;
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
           const u32 b = (u32)(seen >> (16 * x)) & 0xf;
@@ -279,6 +288,7 @@ struct Rows16 {
             const bool there = b & (1u << r);
             s[x][j][r] = there ? s[x][j][r] : NONE;
             l = max2(l, there ? v[r] : 0.f);
+            m[j] = max2(m[j], s[x][j][r]);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -293,16 +303,10 @@ struct Rows16 {
     float before[NY];
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
-      float m = NONE;
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        m = max3(m, s[x][j][0], s[x][j][1]);
-        m = max3(m, s[x][j][2], s[x][j][3]);
-      }
-      m = row_max(m);
-      grows |= m > top[j] || largest[j] > big[j];
+      const float most_here = row_max(m[j]);
+      grows |= most_here > top[j] || largest[j] > big[j];
       before[j] = top[j] == NONE ? NONE : ref[j];
-      top[j] = max2(top[j], m);
+      top[j] = max2(top[j], most_here);
       big[j] = max2(big[j], largest[j]);
       int e = __builtin_amdgcn_frexp_expf(big[j]);
       e = e < -80 ? -80 : e > 100 ? 100 : e;
@@ -317,21 +321,18 @@ struct Rows16 {
         for (int i = 0; i < NX; ++i) o[i][j] *= by;
       }
     }
+  }
+
+  // The weights of row j in a tile, to half `half` of a fragment.
+  __device__ void weigh(const v4f &s, const v4f &vs, int j, int half, v4i &w) {
+    _Float16 h[4];
 #pragma unroll
-    for (int j = 0; j < NY; ++j) {
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        _Float16 h[4];
-        const v4f v = vs(x);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[x][j][r], factor[j], -ref[j]));
-          sum[j] += p;
-          h[r] = (_Float16)(p * v[r]);
-        }
-        __builtin_memcpy((char *)&w[x / 2][j] + 8 * (x % 2), h, 8);
-      }
+    for (int r = 0; r < 4; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[r], factor[j], -ref[j]));
+      sum[j] += p;
+      h[r] = (_Float16)(p * vs[r]);
     }
+    __builtin_memcpy((char *)&w + 8 * half, h, 8);
   }
 
   // The end of group j: a part's sums, or the row itself.  A lane's outputs are DIM / 4
@@ -547,8 +548,13 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     v4i p[1][NY];
     const bool there[2] = {is_page(a, now[0]), is_page(a, now[1])};
     const uint64_t in = (there[0] ? 0xffffu : 0u) | (there[1] ? 0xffff0000u : 0u);
-    x.template weigh<2>(
-        sc, [&](int h) { return fks[h]; }, [&](int h) { return fvs[h]; },
+    float largest[NY];
+#pragma unroll
+    for (int j = 0; j < NY; ++j) largest[j] = NONE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) x.template scaled<2>(sc, h, fks[h], largest);
+    x.template refer<2>(
+        sc, largest, [&](int h) { return fvs[h]; },
         [&] {
           float v = 0.f;
 #pragma unroll
@@ -562,8 +568,11 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
           const Row r = row(j);
           const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
           return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
-        },
-        p);
+        });
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < NY; ++j) x.weigh(sc[h][j], fvs[h], j, h, p[0][j]);
     if (more) load_scales(ahead);
     auto bytes = [&](int h, int r, int word) {
       if constexpr (VB == 4) return (u32)fv[h][r];
@@ -635,6 +644,16 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
   if (wave == 0) {
 #pragma unroll
     for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
+  }
+}
+
+// MACS matrix instructions with VALUS vector instructions spread between them.
+template <int MACS, int VALUS>
+__device__ inline void interleave() {
+#pragma unroll
+  for (int i = 0; i < MACS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, (VALUS + MACS - 1) / MACS, 0);
   }
 }
 
@@ -758,15 +777,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
       scales[2 * M::TILE + 4 + wave] = most;
     }
   };
-  auto use = [&](const char *stage, int t) {
+  auto use = [&](const char *stage, int t, char *next) {
     const v4i *keys = (const v4i *)stage + lane;
     const v4i *values = (const v4i *)(stage + M::KEYS) + lane;
     const float *scales = (const float *)(stage + M::KEYS + M::VALUES);
     auto ks = [&](int h) { return *(const v4f *)(scales + 16 * h + 4 * g); };
     auto vs = [&](int h) { return *(const v4f *)(scales + M::TILE + 16 * h + 4 * g); };
     v4f sc[4][NY];
-    // the next fragments on their way while the present ones are multiplied (and no more:
-    // all of them at once do not fit the registers)
+    float largest[NY];
+#pragma unroll
+    for (int j = 0; j < NY; ++j) largest[j] = NONE;
+    // The next fragments are on their way while the present ones are multiplied (and no
+    // more: all of them at once do not fit the registers), and what the scores go through
+    // is spread between the products that follow, here and below: a wave's vector and
+    // matrix instructions then run side by side.
     v4i kf[2][M::KS];
 #pragma unroll
     for (int c = 0; c < M::KS; ++c) kf[0][c] = keys[c * 64];
@@ -782,13 +806,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
       for (int c = 0; c < M::KS; ++c)
 #pragma unroll
         for (int j = 0; j < NY; ++j) sc[h][j] = mac(kf[h % 2][c], x.q[j][c], sc[h][j]);
+      if (h > 0) {
+        x.template scaled<4>(sc, h - 1, ks(h - 1), largest);
+        interleave<M::KS * NY, 8 * NY>();
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
+    x.template scaled<4>(sc, 3, ks(3), largest);
     const int *there = (const int *)(scales + 2 * M::TILE);
     const int here = __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3]);
-    v4i p[2][NY];
-    x.template weigh<4>(
-        sc, ks, vs,
+    x.template refer<4>(
+        sc, largest, vs,
         [&] {
           const v4f most = *(const v4f *)(scales + 2 * M::TILE + 4);
           return max3(max2(most[0], most[1]), most[2], most[3]);
@@ -801,15 +829,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
           const Row r = row(j);
           const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
           return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
-        },
-        p);
-    constexpr int G = 4, GROUPS = 2 * M::NX / G;
+        });
+    v4i p[2][NY];
+    constexpr int G = 4, EACH = M::NX / G;  // groups of products with the values, per half
     v4i vf[2][G];
 #pragma unroll
     for (int i = 0; i < G; ++i) vf[0][i] = values[i * 64];
 #pragma unroll
-    for (int n = 0; n < GROUPS; ++n) {
-      if (n + 1 < GROUPS) {
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < NY; ++j) x.weigh(sc[h][j], vs(h), j, h, p[0][j]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < 2 * EACH; ++n) {
+      if (n + 1 < 2 * EACH) {
 #pragma unroll
         for (int i = 0; i < G; ++i) vf[(n + 1) % 2][i] = values[((n + 1) * G + i) * 64];
       }
@@ -819,8 +852,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
 #pragma unroll
         for (int j = 0; j < NY; ++j) x.o[at][j] = mac(vf[n % 2][i], p[u][j], x.o[at][j]);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      // beside the first half's products the second half's weights, a share to a group
+      // (beside the second half's, the next tile)
+      if (n < EACH) {
+#pragma unroll
+        for (int k = n * 2 * NY / EACH; k < (n + 1) * 2 * NY / EACH; ++k)
+          x.weigh(sc[2 + k / NY][k % NY], vs(2 + k / NY), k % NY, k / NY, p[1][k % NY]);
+        interleave<G * NY, 2 * NY / EACH * 18>();
+      }
+      if (n + 1 < 2 * EACH) __builtin_amdgcn_sched_barrier(0);
     }
+    write(next);  // (behind the last tile what was there before, which nobody reads)
   };
   if (from < to) {
     load(from);
@@ -828,19 +870,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
     if (from + M::TILE < to) load(from + M::TILE);
   }
   int at = 0;
-  auto next = [&](int t) {
-    __syncthreads();  // this tile is written, and the one before it no longer read
-    if (t + M::TILE < to) {
-      write(lds + (at ^ 1) * M::STAGE);
-      if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
-    }
-  };
   int t = from;
   for (; t < least(some, to); t += M::TILE, at ^= 1) {
-    next(t);
-    use(lds + at * M::STAGE, t);
+    __syncthreads();  // this tile is written, and the one before it no longer read
+    use(lds + at * M::STAGE, t, lds + (at ^ 1) * M::STAGE);
+    if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
   }
-  for (; t < to; t += M::TILE, at ^= 1) next(t);  // (what only other waves see)
+  for (; t < to; t += M::TILE, at ^= 1) {  // (what only other waves see)
+    __syncthreads();
+    if (t + M::TILE < to) write(lds + (at ^ 1) * M::STAGE);
+    if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
+  }
 #pragma unroll
   for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
 }
