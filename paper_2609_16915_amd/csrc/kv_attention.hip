@@ -205,29 +205,34 @@ struct Rows16 {
   v4f o[NX][NY];
 
   // q's values k .. + 7 of a lane come from its row's first(ks) on.  `at` gives the Row
-  // of group j.
+  // of group j, of which row `some` of the call is one for sure.  All of it is asked for
+  // before any is used (under conditions of their own the loads went one after the other).
   template <class T, class At, class First>
-  __device__ void load(const AttendArgs &a, At at, First first) {
+  __device__ void load(const AttendArgs &a, int some, At at, First first) {
+    v4i raw[NY][KS];
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
       const Row r = at(j);
+      const T *from = (const T *)a.q.p + (r.at >= 0 ? r.at : some) * a.q.row + r.head * a.q.head;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int d = first(ks);
+        __builtin_memcpy(&raw[j][ks], from + (d < (int)a.cache.dim ? d : 0), 16);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      const bool mine = at(j).at >= 0;
       float f[KS][8];
       float m = 0.f, odd = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int d = first(ks);
-        struct __attribute__((packed, aligned(1))) {
-          T v[8];
-        } x;
-        if (r.at >= 0 && d < (int)a.cache.dim) {
-          __builtin_memcpy(&x, (const T *)a.q.p + r.at * a.q.row + r.head * a.q.head + d, sizeof x);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x.v[i] = (T)0.f;
-        }
+        const bool in = mine && first(ks) < (int)a.cache.dim;
+        T x[8];
+        __builtin_memcpy(x, &raw[j][ks], 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          f[ks][i] = (float)x.v[i];
+          f[ks][i] = in ? (float)x[i] : 0.f;
           m = fmaxf(m, fabsf(f[ks][i]));
           odd += f[ks][i] * 0.f;
         }
@@ -505,8 +510,8 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
   // product ks of 32 takes bytes 16 g + 8 (ks % 2) .. + 8 of chunk ks / 2 of 64
   Rows16<D, NY> x;
   auto first = [&](int ks) { return 64 * (ks / 2) + 16 * g + 8 * (ks % 2); };
-  if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, row, first);
-  else x.template load<f16>(a, row, first);
+  if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
+  else x.template load<f16>(a, s.first, row, first);
 
   for (; t < to; t += TURN) {
     const bool more = t + TURN < to;
@@ -674,7 +679,7 @@ struct Many {
 };
 
 template <int D, int NY>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
+__global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend_many(Work w) {
   using M = Many<D, NY>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const AttendArgs &a = w.a;
@@ -696,8 +701,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
 
   Rows16<D, NY> x;
   auto first = [&](int ks) { return 32 * ks + 8 * g; };
-  if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, row, first);
-  else x.template load<f16>(a, row, first);
+  if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
+  else x.template load<f16>(a, s.first, row, first);
 
   // what some row of the workgroup sees, of this wave sees, and all of this wave's see
   const int n1 = s.n - 1;
@@ -736,9 +741,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
     sub.ks = at.ks[m];
     sub.vs = at.vs[m];
   };
-  auto write = [&](char *stage) {
+  // in PIECES: what a piece does runs beside products
+  constexpr int PIECES = M::NX / 4;
+  auto write_piece = [&](char *stage, int piece) {
 #pragma unroll
-    for (int c = 0; c < M::NS; ++c) {
+    for (int c = piece * M::NS / PIECES; c < (piece + 1) * M::NS / PIECES; ++c) {
       char *to = stage + (((wave * M::KS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
       const v2i a0 = widen(sub.k[c].x), a1 = widen(sub.k[c].y);
       const v2i b0 = widen(sub.k[c].z), b1 = widen(sub.k[c].w);
@@ -750,32 +757,34 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
       else return (u32)sub.v[r][i];
     };
     char *to = stage + M::KEYS + wave / 2 * M::NX * 1024 + lane * 16 + wave % 2 * 8;
-#pragma unroll
-    for (int i = 0; i < M::VB / 4; ++i) {
-      auto turn = [&](auto byte) {
-        constexpr int I = decltype(byte)::value;
-        *(v2i *)(to + (4 * i + I) * 1024) = v2i{(int)widen_two<I>(word(0, i), word(1, i)),
-                                               (int)widen_two<I>(word(2, i), word(3, i))};
-      };
-      turn(std::integral_constant<int, 0>{});
-      turn(std::integral_constant<int, 1>{});
-      turn(std::integral_constant<int, 2>{});
-      turn(std::integral_constant<int, 3>{});
-    }
+    auto turn = [&](auto byte) {
+      constexpr int I = decltype(byte)::value;
+      *(v2i *)(to + (4 * piece + I) * 1024) =
+          v2i{(int)widen_two<I>(word(0, piece), word(1, piece)),
+              (int)widen_two<I>(word(2, piece), word(3, piece))};
+    };
+    turn(std::integral_constant<int, 0>{});
+    turn(std::integral_constant<int, 1>{});
+    turn(std::integral_constant<int, 2>{});
+    turn(std::integral_constant<int, 3>{});
+    if (piece) return;
     float *scales = (float *)(stage + M::KEYS + M::VALUES);
     settle(sub.ks, sub.vs);
-    if (lane < 16) scales[16 * wave + m] = sub.ks;
-    if (lane < 16) scales[M::TILE + 16 * wave + m] = sub.vs;
     // the largest v_scale of the sixteen
     float most = sub.vs;
     most = max2(most, turned<8>(most));
     most = max2(most, turned<4>(most));
     most = max2(most, turned<2>(most));
     most = max2(most, turned<1>(most));
-    if (lane == 0) {
-      ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
-      scales[2 * M::TILE + 4 + wave] = most;
-    }
+    // (the lanes of a place write the same)
+    scales[16 * wave + m] = sub.ks;
+    scales[M::TILE + 16 * wave + m] = sub.vs;
+    ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
+    scales[2 * M::TILE + 4 + wave] = most;
+  };
+  auto write = [&](char *stage) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) write_piece(stage, i);
   };
   auto use = [&](const char *stage, int t, char *next) {
     const v4i *keys = (const v4i *)stage + lane;
@@ -859,10 +868,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) k_attend_many(Work w) {
         for (int k = n * 2 * NY / EACH; k < (n + 1) * 2 * NY / EACH; ++k)
           x.weigh(sc[2 + k / NY][k % NY], vs(2 + k / NY), k % NY, k / NY, p[1][k % NY]);
         interleave<G * NY, 2 * NY / EACH * 18>();
+      } else {  // (behind the last tile what was there before, which nobody reads)
+        write_piece(next, n - EACH);
+        interleave<G * NY, 44>();
       }
-      if (n + 1 < 2 * EACH) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    write(next);  // (behind the last tile what was there before, which nobody reads)
   };
   if (from < to) {
     load(from);
