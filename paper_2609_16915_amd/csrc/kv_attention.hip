@@ -985,14 +985,25 @@ Plan plan_of(size_t heads, size_t kv_heads, size_t dim, size_t batch, size_t max
   Plan p;
   p.d = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
   const size_t group = heads / kv_heads, rows = max_rows * group;
-  p.many = rows > 32;
+  // Tiles widened once for all rows against ones that each wave widens for itself, without
+  // a barrier and in smaller pieces (microseconds, the first against the second):
+  // rows of 256 59 : 91 (512 rows over 4096 positions); of 128 17 : 25 (4 x 1024 rows over
+  // 256), 215 : 331 (16384 over 4096), 30 : 26 (4 x 64 over 4096); of 64 33 : 42 (2 x 8192
+  // over 1024, 512 workgroups), 138 : 98 (4096 over 4096, 384 workgroups).
+  const size_t large = batch * kv_heads * ((rows + 127) / 128);
+  p.many = p.d == 256 ? rows > 32 : rows > 128 && (p.d == 128 || large >= 512);
   // (two groups of 256 do not fit the registers beside what is on its way)
   p.ny = p.d == 256 || rows <= 16 ? 1 : 2;
   const size_t each = 16 * p.ny * (p.many ? 4 : 1);
   p.row_blocks = (int)((rows + each - 1) / each);
+  // Parts until there is a workgroup to a CU, two where all rows go by in one: sums that
+  // are joined cost their way to memory and back (five prompts of 777, 420 workgroups: 37
+  // us in two parts, 30 in one).  One group of rows is cut in two at least, so that long
+  // sequences end sooner (64 of 2048 to 8192 positions: 147 us in one, 133 in two).
   const size_t blocks = batch * kv_heads * p.row_blocks;
-  const size_t wanted = p.many ? 512 : 1024;
-  size_t parts = blocks ? (wanted + blocks - 1) / blocks : 1;
+  const size_t wanted = p.many ? 256 : 512;
+  size_t parts = (wanted + blocks - 1) / blocks;
+  if (!p.many && p.row_blocks == 1 && blocks < 1024) parts = std::max<size_t>(parts, 2);
   parts = std::min(parts, (positions + 127) / 128);
   p.parts = (int)std::max<size_t>(1, std::min<size_t>(parts, 128));
   return p;
