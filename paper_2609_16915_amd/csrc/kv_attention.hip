@@ -95,10 +95,10 @@ __device__ inline float row_max(float a) {
 __device__ inline float row_sum(float a) {
   return across(a, [](float x, float y) { return x + y; });
 }
-// The scales of a position: where that of the value is no number, neither is the score's,
+// The scales of a position: where one of them is no number, or infinite, the score is none,
 // and the value counts as 0, so that rows that do not see it are not touched.
 __device__ inline void settle(float &k, float &v) {
-  const bool fine = fabsf(v) < __builtin_inff();
+  const bool fine = fabsf(v) < __builtin_inff() && fabsf(k) < __builtin_inff();
   k = fine ? k : __builtin_nanf("");
   v = fine ? v : 0.f;
 }
