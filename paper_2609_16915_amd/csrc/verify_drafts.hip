@@ -29,6 +29,7 @@ constexpr int PIECES = 64;   // of a row, at most: a lane each
 constexpr int PIECE = 2048;  // values of a piece, at least
 constexpr int NODES = 1024;  // of a sequence that take part
 constexpr int TEAM = 1024;   // threads of the last kernel
+constexpr int ROUNDS = 3;    // launches of many workgroups before it, at most
 
 struct Job {
   VerifyArgs a;
@@ -111,32 +112,35 @@ struct Walk {
   }
 };
 
-// This thread's share, of `threads`, of the sum over values [lo, hi) of a row.
-template <class T>
+// This thread's share, of `threads`, of the sum over values [lo, hi) of a row, N groups of
+// four of either row asked for at a time.
+template <int N, class T>
 __device__ double share(const T *p, const T *q, double c, size_t lo, size_t hi, int thread,
                         int threads) {
   struct __attribute__((packed, aligned(1))) Four {
     T v[4];
   };
-  double s0 = 0, s1 = 0;
-  size_t v = lo + 4 * thread;
-  for (; v + 4 + 4 * threads <= hi; v += 8 * threads) {
-    Four x, y, x1, y1;
-    __builtin_memcpy(&x, p + v, sizeof x);
-    __builtin_memcpy(&y, q + v, sizeof y);
-    __builtin_memcpy(&x1, p + v + 4 * threads, sizeof x);
-    __builtin_memcpy(&y1, q + v + 4 * threads, sizeof y);
+  double s[2] = {0, 0};
+  const int fours = (int)((hi - lo) / 4);
+  for (int i0 = thread; i0 < fours; i0 += N * threads) {
+    Four x[N], y[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s0 += left_of((double)(float)x.v[i], (double)(float)y.v[i], c);
-      s1 += left_of((double)(float)x1.v[i], (double)(float)y1.v[i], c);
+    for (int n = 0; n < N; ++n) {
+      const int i = i0 + n * threads < fours ? i0 + n * threads : i0;
+      __builtin_memcpy(&x[n], p + lo + 4 * (size_t)i, sizeof x[n]);
+      __builtin_memcpy(&y[n], q + lo + 4 * (size_t)i, sizeof y[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (i0 + n * threads >= fours) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s[n % 2] += left_of((double)(float)x[n].v[i], (double)(float)y[n].v[i], c);
     }
   }
-  for (; v < hi; v += 4 * threads)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (v + i < hi) s0 += left_of((double)(float)p[v + i], (double)(float)q[v + i], c);
-  return s0 + s1;
+  for (size_t v = lo + 4 * (size_t)fours + thread; v < hi; v += threads)
+    s[0] += left_of((double)(float)p[v], (double)(float)q[v], c);
+  return s[0] + s[1];
 }
 
 // One round: every workgroup walks as far as the sums so far go and makes its piece of
@@ -149,11 +153,18 @@ __global__ void __launch_bounds__(256) k_verify_round(Job j, int round) {
   const VerifyArgs &a = j.a;
   const int b = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x % 64;
   if (threadIdx.x < 64) {
+    double sums[ROUNDS];  // of the rounds before (what a walk does not ask for is not read)
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+      sums[i] = i < round && lane < j.pieces ? j.sums[((size_t)i * a.batch + b) * j.pieces + lane] : 0.;
     Walk<T> w(a, b);
     bool more = w.n > 0 && w.go([](int, int, int64_t) {});
     int k = 0;
-    for (; more && k < round; ++k) {
-      w.z = wave_sum(lane < j.pieces ? j.sums[((size_t)k * a.batch + b) * j.pieces + lane] : 0.);
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      if (!more || i >= round) continue;
+      k = i + 1;
+      w.z = wave_sum(sums[i]);
       more = w.go([](int, int, int64_t) {});
     }
     if (lane == 0) {
@@ -166,7 +177,7 @@ __global__ void __launch_bounds__(256) k_verify_round(Job j, int round) {
   __syncthreads();
   if (node < 0) return;
   const size_t lo = piece * j.piece, hi = lo + j.piece < a.vocab ? lo + j.piece : a.vocab;
-  double s = share((const T *)a.p + (size_t)node * a.p_stride,
+  double s = share<2>((const T *)a.p + (size_t)node * a.p_stride,
                    (const T *)a.q + (size_t)node * a.q_stride, at, lo, hi, threadIdx.x, 256);
   s = wave_sum(s);
   if (lane == 0) shared[threadIdx.x / 64] = s;
@@ -242,7 +253,7 @@ __global__ void __launch_bounds__(TEAM) k_verify_end(Job j) {
     } else {
       for (int i = wave; i < j.pieces; i += WAVES) {
         const size_t lo = i * j.piece, hi = lo + j.piece < a.vocab ? lo + j.piece : a.vocab;
-        const double s = wave_sum(share(p, q, at, lo, hi, lane, 64));
+        const double s = wave_sum(share<8>(p, q, at, lo, hi, lane, 64));
         if (lane == 0) pieces[i] = s;
       }
     }
@@ -328,17 +339,22 @@ __global__ void __launch_bounds__(TEAM) k_verify_end(Job j) {
 int pieces_of(size_t vocab) {
   return (int)std::min<size_t>(PIECES, (vocab + PIECE - 1) / PIECE);
 }
-constexpr int ROUNDS = 3;
-int rounds_of(bool tree, size_t vocab) { return pieces_of(vocab) < 4 ? 0 : tree ? ROUNDS : 1; }
+// Launches before the last: none where a row is but a few pieces; one for chains, which
+// want one sum; for trees as many as the slowest sequence is likely to want (16 trees of 32
+// over 128000 words: 51 us with one, 45 with two, 39 with three, 40 with four; one tree 20,
+// 20, 22 and 25).
+int rounds_of(bool tree, size_t batch, size_t vocab) {
+  return pieces_of(vocab) < 4 ? 0 : !tree ? 1 : batch < 8 ? 2 : ROUNDS;
+}
 
 }  // namespace
 
 size_t verify_drafts_workspace(size_t batch, size_t vocab) {
-  return rounds_of(true, vocab) * batch * pieces_of(vocab) * sizeof(double);
+  return rounds_of(true, batch, vocab) * batch * pieces_of(vocab) * sizeof(double);
 }
 
 hipError_t launch_verify_drafts(const VerifyArgs &a, hipStream_t st) {
-  Job j{a, pieces_of(a.vocab), rounds_of(a.parents != nullptr, a.vocab), 0, (double *)a.workspace};
+  Job j{a, pieces_of(a.vocab), rounds_of(a.parents != nullptr, a.batch, a.vocab), 0, (double *)a.workspace};
   j.piece = ((a.vocab + j.pieces - 1) / j.pieces + 3) / 4 * 4;
   j.pieces = (int)((a.vocab + j.piece - 1) / j.piece);
   if (a.batch > 65535 || !grid_fits(a.batch, TEAM)) return hipErrorInvalidConfiguration;
