@@ -89,6 +89,12 @@ __device__ inline float max3(float a, float b, float c) {
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
 }
+__device__ inline u32 max3(u32 a, u32 b, u32 c) {
+  u32 r;
+  asm("v_max3_u32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ inline u32 bits_of(float a) { return __builtin_bit_cast(u32, a); }
 __device__ inline float row_max(float a) {
   return across(a, [](float x, float y) { return max2(x, y); });
 }
@@ -200,7 +206,7 @@ struct Rows16 {
   v4i q[NY][KS];
   float factor[NY];   // of a score, in powers of two
   float top[NY];      // the largest score before the factor
-  float big[NY];      // the largest v_scale
+  float big[NY];      // the largest v_scale, whatever its sign
   float ref[NY], sum[NY];
   v4f o[NX][NY];
 
@@ -292,7 +298,7 @@ struct Rows16 {
           for (int r = 0; r < 4; ++r) {
             const bool there = b & (1u << r);
             s[x][j][r] = there ? s[x][j][r] : NONE;
-            l = max2(l, there ? v[r] : 0.f);
+            l = max2(l, there ? fabsf(v[r]) : 0.f);
             m[j] = max2(m[j], s[x][j][r]);
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -305,22 +311,22 @@ struct Rows16 {
       for (int j = 0; j < NY; ++j) largest[j] = l;
     }
     bool grows = false;
-    float before[NY];
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
-      const float most_here = row_max(m[j]);
-      grows |= most_here > top[j] || largest[j] > big[j];
-      before[j] = top[j] == NONE ? NONE : ref[j];
-      top[j] = max2(top[j], most_here);
-      big[j] = max2(big[j], largest[j]);
-      int e = __builtin_amdgcn_frexp_expf(big[j]);
-      e = e < -80 ? -80 : e > 100 ? 100 : e;
-      ref[j] = top[j] == NONE ? 0.f : fmaf(top[j], factor[j], (float)(e - 15));
+      m[j] = row_max(m[j]);
+      grows |= m[j] > top[j] || largest[j] > big[j];
     }
     if (__any(grows)) {
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
-        const float by = before[j] == NONE ? 0.f : __builtin_amdgcn_exp2f(before[j] - ref[j]);
+        const float before = ref[j];
+        const bool none = top[j] == NONE;
+        top[j] = max2(top[j], m[j]);
+        big[j] = max2(big[j], largest[j]);
+        int e = __builtin_amdgcn_frexp_expf(big[j]);
+        e = e < -80 ? -80 : e > 100 ? 100 : e;
+        ref[j] = top[j] == NONE ? 0.f : fmaf(top[j], factor[j], (float)(e - 15));
+        const float by = none ? 0.f : __builtin_amdgcn_exp2f(before - ref[j]);
         sum[j] *= by;
 #pragma unroll
         for (int i = 0; i < NX; ++i) o[i][j] *= by;
@@ -541,15 +547,30 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
         }
       }
     if (more) load_keys(ahead);
+    // The largest of the scales, as bits: of numbers that are positive and finite, of
+    // which all are as a rule.
+    u32 tops[2] = {0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float k = fks[h][r], v = fvs[h][r];
-        settle(k, v);
-        fks[h][r] = k;
-        fvs[h][r] = v;
+      for (int r = 0; r < 4; r += 2) {
+        tops[0] = max3(tops[0], bits_of(fks[h][r]), bits_of(fks[h][r + 1]));
+        tops[1] = max3(tops[1], bits_of(fvs[h][r]), bits_of(fvs[h][r + 1]));
       }
+    float most = __builtin_bit_cast(float, tops[1]);
+    if (__any(tops[0] >= 0x7f800000u || tops[1] >= 0x7f800000u)) {
+      most = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float k = fks[h][r], v = fvs[h][r];
+          settle(k, v);
+          fks[h][r] = k;
+          fvs[h][r] = v;
+          most = max2(most, fabsf(v));
+        }
+    }
     v4i p[1][NY];
     const bool there[2] = {is_page(a, now[0]), is_page(a, now[1])};
     const uint64_t in = (there[0] ? 0xffffu : 0u) | (there[1] ? 0xffff0000u : 0u);
@@ -560,14 +581,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     for (int h = 0; h < 2; ++h) x.template scaled<2>(sc, h, fks[h], largest);
     x.template refer<2>(
         sc, largest, [&](int h) { return fvs[h]; },
-        [&] {
-          float v = 0.f;
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; r += 2) v = max3(v, fvs[h][r], fvs[h][r + 1]);
-          return row_max(v);
-        },
+        [&] { return row_max(most); },
         !(t + 32 <= all && there[0] && there[1]),
         [&](int j) {
           const Row r = row(j);
@@ -771,7 +785,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     float *scales = (float *)(stage + M::KEYS + M::VALUES);
     settle(sub.ks, sub.vs);
     // the largest v_scale of the sixteen
-    float most = sub.vs;
+    float most = fabsf(sub.vs);
     most = max2(most, turned<8>(most));
     most = max2(most, turned<4>(most));
     most = max2(most, turned<2>(most));

@@ -1000,7 +1000,7 @@ def kv_cache(pages: int, kv_heads: int, page: int, dim: int, device="cuda") -> K
 
 def _tensor(t, name: str, dtype, dims: int, device):
     """A device tensor's (shape, strides), of `dims` dimensions, the last contiguous."""
-    if not isinstance(t, _tensor_class()) or (dtype is not None and t.dtype != dtype):
+    if not isinstance(t, _tensor_class()) or (dtype is not None and t.dtype is not dtype):
         raise TypeError(f"{name} must be a torch tensor" + (f" of {dtype}" if dtype else ""))
     size, strides = t.shape, t.stride()
     if len(size) != dims:
@@ -1008,32 +1008,34 @@ def _tensor(t, name: str, dtype, dims: int, device):
     at = t.get_device()
     if at < 0 or (device is not None and at != device):
         _misplaced(t, name, device)
-    if size[-1] > 1 and strides[-1] != 1:
+    if strides[-1] != 1 and size[-1] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
     return size, strides
 
 
-def _cache(cache, device=None):
+def _cache(cache):
     """(struct, device) of a cache; strides over one element alone are any."""
-    torch = _torch()
     if not isinstance(cache, KVCache):
         raise TypeError("cache must be a KVCache")
-    size, st = _tensor(cache.k, "cache.k", torch.int8, 4, device)
-    on = cache.k.get_device()
-    if _tensor(cache.v, "cache.v", torch.int8, 4, on) != (size, st):
+    torch = _torch()
+    k, v, ks, vs = cache
+    size, st = _tensor(k, "cache.k", torch.int8, 4, None)
+    ssize, ss = _tensor(ks, "cache.k_scale", torch.float32, 3, k.get_device())
+    on = k.get_device()
+    if _tensor(v, "cache.v", torch.int8, 4, on) != (size, st):
         raise ValueError("cache.v must have the shape and strides of cache.k")
-    pages, heads, page, dim = size
-    ssize, ss = _tensor(cache.k_scale, "cache.k_scale", torch.float32, 3, on)
+    if _tensor(vs, "cache.v_scale", torch.float32, 3, on) != (ssize, ss):
+        raise ValueError("cache.v_scale must have the shape and strides of cache.k_scale")
     if ssize != size[:3]:
         raise ValueError(f"cache.k_scale is {tuple(ssize)}, the call needs {tuple(size[:3])}")
-    if _tensor(cache.v_scale, "cache.v_scale", torch.float32, 3, on) != (ssize, ss):
-        raise ValueError("cache.v_scale must have the shape and strides of cache.k_scale")
-    at_head = st[1] if heads > 1 else 0
-    at_place = st[2] if page > 1 else 0
-    return CacheStruct(
-        cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(),
-        cache.v_scale.data_ptr(), pages, heads, page, dim, st[0] if pages > 1 else 0, at_head,
-        at_place, ss[0] if pages > 1 else 0, ss[1] if heads > 1 else 0), on
+    pages, heads, page, dim = size
+    if pages > 1 and heads > 1 and page > 1:
+        return CacheStruct(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads,
+                           page, dim, st[0], st[1], st[2], ss[0], ss[1]), on
+    return CacheStruct(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page,
+                       dim, st[0] if pages > 1 else 0, st[1] if heads > 1 else 0,
+                       st[2] if page > 1 else 0, ss[0] if pages > 1 else 0,
+                       ss[1] if heads > 1 else 0), on
 
 
 def _rows(table, starts, lens, rows: int, device):
