@@ -448,12 +448,19 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int kv_heads = (int)a.cache.kv_heads;
+  // Several groups of rows read the same part of the cache: one right after the other, so
+  // that they find it in the caches (trees of 25 in seven groups 28 us, 35 with the
+  // sequences in between; 32 all on one XCD, which then gets the long sequences).  With one
+  // group the sequences go by in turn (64 of 2048 to 8192 positions 133 us, 141 with their
+  // parts next to each other).
   unsigned id = blockIdx.x;
+  const unsigned batch = (unsigned)a.packed.batch, parts = (unsigned)w.parts;
   const int head = id % kv_heads;
   id /= kv_heads;
-  const int b = id % (unsigned)a.packed.batch;
-  id /= (unsigned)a.packed.batch;
-  const int part = id % (unsigned)w.parts, block = id / (unsigned)w.parts;
+  const int block = id % (unsigned)w.row_blocks;
+  id /= (unsigned)w.row_blocks;
+  const int b = w.row_blocks > 1 ? id / parts : id % batch;
+  const int part = w.row_blocks > 1 ? id % parts : id / batch;
   const Seq s = seq_of(a, b, head);
   const int r0 = block * 16 * NY;
   if (r0 >= s.n * w.group) return;
