@@ -707,12 +707,15 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int kv_heads = (int)a.cache.kv_heads;
-  // the blocks of one head's part are neighbours on one XCD, those with most to see first
-  const unsigned id = xcd_block(blockIdx.x, gridDim.x);
-  const int block = w.row_blocks - 1 - id % (unsigned)w.row_blocks;
-  unsigned rest = id / (unsigned)w.row_blocks;
+  // Heads in turn: with eight of them, or a divisor, an XCD has the same ones throughout, and
+  // some of every sequence; the blocks with most to see first.  (Runs of blocks to an XCD
+  // give it whole sequences, the long or the short ones: four of 512 to 2048 positions 134
+  // us in turn, 210 so; one of 4096 with two heads of 256, 329 and 541.)
+  unsigned rest = blockIdx.x;
   const int head = rest % kv_heads;
   rest /= kv_heads;
+  const int block = w.row_blocks - 1 - rest % (unsigned)w.row_blocks;
+  rest /= (unsigned)w.row_blocks;
   const int part = rest % (unsigned)w.parts, b = rest / (unsigned)w.parts;
   const Seq s = seq_of(a, b, head);
   const int r0 = block * M::ROWS;
