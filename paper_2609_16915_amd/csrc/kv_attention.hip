@@ -359,7 +359,8 @@ struct Rows16 {
     const size_t row = r.at * a.heads + r.head;
     if (w.parts > 1) {
       const size_t at = row * w.parts + part;
-      if (g == 0) w.ends[at] = float2{none ? NONE : ref[j], total};
+      // (a reference that is no number would be passed over in the join: the sum says it)
+      if (g == 0) w.ends[at] = float2{none ? NONE : ref[j] == ref[j] ? ref[j] : 0.f, total};
       if (none) return;
       float *to = w.sums + at * D + d0;
 #pragma unroll
@@ -1011,24 +1012,27 @@ Plan plan_of(size_t heads, size_t kv_heads, size_t dim, size_t batch, size_t max
   const size_t group = heads / kv_heads, rows = max_rows * group;
   // Tiles widened once for all rows against ones that each wave widens for itself, without
   // a barrier and in smaller pieces (microseconds, the first against the second):
-  // rows of 256 59 : 91 (512 rows over 4096 positions); of 128 17 : 25 (4 x 1024 rows over
-  // 256), 215 : 331 (16384 over 4096), 30 : 26 (4 x 64 over 4096); of 64 33 : 42 (2 x 8192
-  // over 1024, 512 workgroups), 138 : 98 (4096 over 4096, 384 workgroups).
+  // rows of 256 58 : 93 (512 rows over 4096 positions, four sequences); of 128 17 : 26
+  // (four of 1024 over 256), 213 : 323 (16384 over 4096), 31 : 26 (four of 64 over 4096);
+  // of 64 141 : 202 (32768 over 4096), 42 : 43 (two of 8192 over 1024, 512 workgroups of
+  // the first), 110 : 93 (12 heads of 4096 over 4096, 384 of them).
   const size_t large = batch * kv_heads * ((rows + 127) / 128);
   p.many = p.d == 256 ? rows > 32 : rows > 128 && (p.d == 128 || large >= 512);
   // (two groups of 256 do not fit the registers beside what is on its way)
   p.ny = p.d == 256 || rows <= 16 ? 1 : 2;
   const size_t each = 16 * p.ny * (p.many ? 4 : 1);
   p.row_blocks = (int)((rows + each - 1) / each);
-  // Parts until there is a workgroup to a CU, two where all rows go by in one: sums that
-  // are joined cost their way to memory and back (five prompts of 777, 420 workgroups: 37
-  // us in two parts, 30 in one).  One group of rows is cut in two at least, so that long
-  // sequences end sooner (64 of 2048 to 8192 positions: 147 us in one, 133 in two).
+  // Parts until the CUs have the workgroups that they hold of the tiles' kernel, long ones,
+  // or two of the other: sums that are joined cost their way to memory and back (four
+  // sequences of 1024 rows over 256 positions: 34 us in two parts, 17 in one; 1024 rows
+  // over 4096: 48 us in eight, 54 in four).  One group of rows is cut in two at least, so
+  // that long sequences end sooner (64 of 2048 to 8192 positions: 147 us in one, 133 in two).
   const size_t blocks = batch * kv_heads * p.row_blocks;
-  const size_t wanted = p.many ? 256 : 512;
+  const size_t wanted = p.d == 256 ? 256 : 512;
+  const size_t least_part = !p.many ? 128 : p.d == 256 ? 256 : 512;
   size_t parts = (wanted + blocks - 1) / blocks;
   if (!p.many && p.row_blocks == 1 && blocks < 1024) parts = std::max<size_t>(parts, 2);
-  parts = std::min(parts, (positions + 127) / 128);
+  parts = std::min(parts, (positions + least_part - 1) / least_part);
   p.parts = (int)std::max<size_t>(1, std::min<size_t>(parts, 128));
   return p;
 }
@@ -1044,11 +1048,13 @@ hipError_t by_dim(int d, F f) {
 
 size_t kv_attention_workspace(size_t heads, size_t kv_heads, size_t dim, size_t batch, size_t rows,
                               size_t max_rows, size_t positions) {
-  const Plan p = plan_of(heads, kv_heads, dim, batch, max_rows, positions);
+  const Plan p = plan_of(heads, kv_heads, dim, batch, std::min(max_rows, rows), positions);
   return p.parts > 1 ? rows * heads * p.parts * (p.d * sizeof(float) + sizeof(float2)) : 0;
 }
 
-hipError_t launch_kv_attention(const AttendArgs &a, hipStream_t st) {
+hipError_t launch_kv_attention(const AttendArgs &given, hipStream_t st) {
+  AttendArgs a = given;
+  a.max_rows = std::min(a.max_rows, a.packed.rows);
   const size_t positions = a.packed.table_len << a.cache.page_log;
   const Plan p = plan_of(a.heads, a.cache.kv_heads, a.cache.dim, a.packed.batch, a.max_rows, positions);
   Work w{a, (int)(a.heads / a.cache.kv_heads), p.parts, p.row_blocks, 1, nullptr, nullptr};
