@@ -1020,11 +1020,15 @@ def _cache(cache):
     torch = _torch()
     k, v, ks, vs = cache
     size, st = _tensor(k, "cache.k", torch.int8, 4, None)
-    ssize, ss = _tensor(ks, "cache.k_scale", torch.float32, 3, k.get_device())
     on = k.get_device()
-    if _tensor(v, "cache.v", torch.int8, 4, on) != (size, st):
+    ssize, ss = _tensor(ks, "cache.k_scale", torch.float32, 3, on)
+    if not (isinstance(v, _tensor_class()) and v.dtype is torch.int8 and v.get_device() == on and
+            v.shape == size and v.stride() == st):
+        _tensor(v, "cache.v", torch.int8, 4, on)
         raise ValueError("cache.v must have the shape and strides of cache.k")
-    if _tensor(vs, "cache.v_scale", torch.float32, 3, on) != (ssize, ss):
+    if not (isinstance(vs, _tensor_class()) and vs.dtype is torch.float32 and
+            vs.get_device() == on and vs.shape == ssize and vs.stride() == ss):
+        _tensor(vs, "cache.v_scale", torch.float32, 3, on)
         raise ValueError("cache.v_scale must have the shape and strides of cache.k_scale")
     if ssize != size[:3]:
         raise ValueError(f"cache.k_scale is {tuple(ssize)}, the call needs {tuple(size[:3])}")
@@ -1056,6 +1060,14 @@ def _heads(t, name: str, dtype, shape, device):
             st[1] if size[1] > 1 else size[2])
 
 
+def _made_heads(out, name: str, dtype, shape, like):
+    """`out` checked, or a new tensor: (tensor, address, row stride, head stride)."""
+    if out is None:
+        out = like.new_empty(shape, dtype=dtype)
+        return out, out.data_ptr(), shape[1] * shape[2], shape[2]
+    return out, *_heads(out, name, dtype, shape, like.get_device())
+
+
 @_on_its_stream
 def kv_write(k, v, cache, table, starts, lens, stream=None):
     """Keys and values [rows][kv_heads][dim] (float32, bfloat16 or float16) to the
@@ -1080,10 +1092,9 @@ def kv_read(cache, table, starts, lens, rows: int, dtype, k=None, v=None, stream
     shape = (rows, c.kv_heads, c.dim)
     code = _type(dtype, "dtype")
     r = _rows(table, starts, lens, rows, on)
-    k = cache.k.new_empty(shape, dtype=dtype) if k is None else k
-    v = cache.k.new_empty(shape, dtype=dtype) if v is None else v
-    _check(lib().rosetta_kv_read(c, r, code, *_heads(k, "k", dtype, shape, on),
-                                 *_heads(v, "v", dtype, shape, on), _stream_of(cache.k, stream)))
+    k, kp, ks, kh = _made_heads(k, "k", dtype, shape, cache.k)
+    v, vp, vs, vh = _made_heads(v, "v", dtype, shape, cache.k)
+    _check(lib().rosetta_kv_read(c, r, code, kp, ks, kh, vp, vs, vh, _stream_of(cache.k, stream)))
     return k, v
 
 
@@ -1165,10 +1176,9 @@ def kv_attention(q, cache, table, starts, lens, masks=None, scale: float = None,
     wp, wb = None, 0
     if need:
         wp, wb, workspace = _scratch(workspace, need, q)
-    out = q.new_empty(shape) if out is None else out
+    out, op, os_, oh = _made_heads(out, "out", dtype, shape, q)
     lse = q.new_empty((rows, heads), dtype=torch.float32) if want_lse else None
-    _check(L.rosetta_kv_attention(*qa, code, heads, c, r, max_rows, mp, words, scale,
-                                  *_heads(out, "out", dtype, shape, on),
+    _check(L.rosetta_kv_attention(*qa, code, heads, c, r, max_rows, mp, words, scale, op, os_, oh,
                                   lse.data_ptr() if want_lse else None, wp, wb,
                                   _stream_of(q, stream)))
     return out, lse

@@ -273,3 +273,172 @@ def test_rows_and_positions_stay_inside(tmp_path):
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0, out.stdout
     assert out.stdout.startswith("5184 spans")
+
+
+# ------------------------------------------------- streams and devices, stood in for
+
+CALLS = ["kv_write", "kv_read", "kv_keep", "tree_masks", "kv_attention", "verify_drafts"]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_stream_is_entered_however_it_is_passed(monkeypatch, name):
+    """What a call allocates comes from the memory of the stream that it runs on."""
+    import inspect
+
+    class Entered(Exception):
+        pass
+
+    stream = object()
+
+    def enter(s):
+        assert s is stream
+        raise Entered
+
+    monkeypatch.setattr(torch.cuda, "stream", enter)
+    call = getattr(R, name)
+    at = list(inspect.signature(call).parameters).index("stream")
+    args = [torch.zeros(4, 64)] * at
+    with pytest.raises(Entered):
+        call(*args[:2], stream=stream)
+    with pytest.raises(Entered):
+        call(*args, stream)
+    with pytest.raises(TypeError, match="stream"):
+        call(*args, stream, stream=stream)
+
+
+class OnDevice(torch.Tensor):
+    """A tensor that says it lies on a ROCm device."""
+    @staticmethod
+    def __new__(cls, t, index):
+        f = torch.Tensor._make_subclass(cls, t)
+        f.at = index
+        return f
+
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: torch.device("cuda", self.at))
+
+    def get_device(self):
+        return getattr(self, "at", 0)
+
+    def new_empty(self, *args, **kw):
+        return OnDevice(torch.empty(*args, **kw), self.at)
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    """Two devices, 0 the current one, and a library that notes where it is called."""
+    class Machine:
+        current = 0
+
+        def __init__(self):
+            self.calls = []
+
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return lambda *a: 64
+            return lambda *a: self.calls.append((name, self.current, a[-1])) or 0
+
+    m = Machine()
+
+    class On:
+        def __init__(self, index):
+            self.index = index if isinstance(index, int) else index.index
+
+        def __enter__(self):
+            self.before, m.current = m.current, self.index
+
+        def __exit__(self, *a):
+            m.current = self.before
+
+    monkeypatch.setattr(R, "lib", lambda: m)
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: m.current, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    return m
+
+
+def made(on, cache_on=None):
+    """The arguments of every call, on device `on` (the cache on another, if given)."""
+    t = lambda x: OnDevice(x, on)  # noqa: E731
+    c = lambda x: OnDevice(x, on if cache_on is None else cache_on)  # noqa: E731
+    cache = R.KVCache(c(torch.zeros((2, 1, 16, 64), dtype=torch.int8)),
+                      c(torch.zeros((2, 1, 16, 64), dtype=torch.int8)),
+                      c(torch.zeros((2, 1, 16))), c(torch.zeros((2, 1, 16))))
+    i = lambda *v: t(torch.tensor(v, dtype=torch.int32))  # noqa: E731
+    table, starts, lens = t(torch.zeros((1, 2), dtype=torch.int32)), i(0, 3), i(5)
+    x = t(torch.zeros((3, 1, 64), dtype=torch.bfloat16))
+    p = t(torch.zeros((3, 9)))
+    return {"kv_write": (x, x, cache, table, starts, lens),
+            "kv_read": (cache, table, starts, lens, 3, torch.bfloat16),
+            "kv_keep": (cache, table, starts, lens, i(0, 1, -1), i(2)),
+            "tree_masks": (i(-1, 0, 1), starts, 3),
+            "kv_attention": (x, cache, table, starts, lens),
+            "verify_drafts": (p, p, t(torch.zeros(3).long()), t(torch.zeros(3)), starts)}
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("on", [0, 1])
+def test_a_call_runs_on_its_tensors_device(machine, name, on):
+    getattr(R, name)(*made(on)[name])
+    assert machine.calls == [("rosetta_" + name, on, 100 + on)] and machine.current == 0
+
+
+@pytest.mark.parametrize("name", ["kv_write", "kv_read", "kv_keep", "kv_attention"])
+def test_a_cache_of_another_device_is_refused(machine, name):
+    with pytest.raises(ValueError, match="device"):
+        getattr(R, name)(*made(0, cache_on=1)[name])
+    assert not machine.calls
+
+
+@pytest.mark.parametrize("name", ["kv_write", "kv_attention", "verify_drafts"])
+def test_a_stream_of_another_device_is_refused(machine, monkeypatch, name):
+    class Stream:
+        device_index, cuda_stream = 1, 7
+
+    class Entered:
+        def __init__(self, s):
+            pass
+
+        def __enter__(self):
+            pass
+
+        def __exit__(self, *a):
+            pass
+
+    monkeypatch.setattr(torch.cuda, "stream", Entered)
+    with pytest.raises(ValueError, match="stream"):
+        getattr(R, name)(*made(0)[name], stream=Stream())
+    assert not machine.calls
+
+
+def test_wrong_sizes_and_types(machine):
+    m = made(0)
+    x, _, cache, table, starts, lens = m["kv_write"]
+    wide = OnDevice(torch.zeros((3, 2, 64), dtype=torch.bfloat16), 0)
+    f32 = OnDevice(torch.zeros((3, 1, 64)), 0)
+    ints64 = OnDevice(torch.zeros(2).long(), 0)
+    for error, call in (
+            (ValueError, lambda: R.kv_write(wide, wide, cache, table, starts, lens)),
+            (TypeError, lambda: R.kv_write(x, f32, cache, table, starts, lens)),
+            (TypeError, lambda: R.kv_write(x, x, cache, table, ints64, lens)),
+            (TypeError, lambda: R.kv_write(x, x, cache, table.long(), starts, lens)),
+            (ValueError, lambda: R.kv_write(x, x, cache, table, lens, lens)),
+            (ValueError, lambda: R.kv_write(x, x, cache, table[0], starts, lens)),
+            (ValueError, lambda: R.kv_write(x.transpose(0, 2), x, cache, table, starts, lens)),
+            (ValueError, lambda: R.kv_attention(x, cache, table, starts, lens, out=wide)),
+            (TypeError, lambda: R.kv_attention(x, cache, table, starts, lens, out=f32)),
+            (TypeError, lambda: R.kv_attention(x, cache, table, starts, lens, masks=starts)),
+            (ValueError, lambda: R.kv_attention(x, cache, table, starts, lens, max_rows=-1)),
+            (TypeError, lambda: R.kv_attention(x.int(), cache, table, starts, lens)),
+            (TypeError, lambda: R.kv_read(cache, table, starts, lens, 3, torch.int8)),
+            (ValueError, lambda: R.kv_write(x, x, cache._replace(v=cache.v[:1]), table, starts, lens)),
+            (TypeError, lambda: R.kv_write(x, x, cache._replace(v=f32), table, starts, lens)),
+            (ValueError, lambda: R.kv_write(x, x, cache._replace(
+                k_scale=cache.k_scale[:, :, :8], v_scale=cache.v_scale[:, :, :8]), table, starts, lens)),
+            (TypeError, lambda: R.verify_drafts(*m["verify_drafts"][:2], starts,
+                                                *m["verify_drafts"][3:])),
+            (ValueError, lambda: R.verify_drafts(*m["verify_drafts"],
+                                                 workspace=OnDevice(torch.zeros(3), 0)))):
+        with pytest.raises(error):
+            call()
+    assert not machine.calls
