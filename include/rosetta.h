@@ -743,8 +743,8 @@ size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, s
  * values, and a page's scales of a head, are contiguous.  value = scale * q, as
  * for the clear side's 8-bit rows, a row being one head of one position.
  * dim: a multiple of 16 up to 256; page: a power of two from 16 on; table_len *
- * page at most 2^30 (else ROSETTA_ERR_UNSUPPORTED); k and v start on 16 bytes, and their strides are
- * multiples of 16. */
+ * page at most 2^30 (else ROSETTA_ERR_UNSUPPORTED); k and v start on 16 bytes, and
+ * their strides are multiples of 16. */
 typedef struct {
   int8_t *k, *v;
   float *k_scale, *v_scale;
@@ -828,9 +828,10 @@ size_t rosetta_kv_attention_workspace_bytes(size_t heads, size_t kv_heads, size_
  *   u[i] z q[x] < p[x] - c q[x],
  * and the walk goes on from it; otherwise c grows by z, and z becomes the sum of
  * r = max(p - c q, 0).  At the end one more token is drawn from the last r (of p
- * itself where no child was rejected, or r is zero throughout): the first whose running sum is past
- * u[0] times the whole, or -1 where p is zero throughout.  With children drawn from
- * q independently of each other, the tokens are distributed as the target's.
+ * itself where no child was rejected, or r is zero throughout): the first whose
+ * running sum is past u[0] times the whole, or -1 where p is zero throughout.  With
+ * children drawn from q independently of each other, the tokens are distributed as
+ * the target's.
  * Sums are in 64 bits; NaN counts as nothing left.  Nodes whose token is outside
  * [0, vocab), and those behind a sequence's 1024th, take no part.
  *   count[b]: the nodes kept, node 0 among them, and as many new tokens (0 for a

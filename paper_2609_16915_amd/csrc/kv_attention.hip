@@ -17,7 +17,7 @@
 // the byte permutations that widen them.  A row of q is held in f16 on a power of two
 // that brings its largest value to 2^13: bf16 has fewer bits than f16, so only what is
 // below 2^-27 of the largest loses any.  The weights of the second product, exp(s - m)
-// v_scale, are rounded to f16 (2^-12 of themselves, beside outputs of 2^-9 in bf16);
+// v_scale, are rounded to f16 (by 2^-11 of themselves at most; a bf16 output by 2^-8);
 // their reference takes in the largest v_scale met, so that they are at most 2^15.
 // The sum of the weights is that of the unrounded exponentials.
 #include <algorithm>

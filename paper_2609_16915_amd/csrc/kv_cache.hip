@@ -253,25 +253,27 @@ __global__ void __launch_bounds__(256) k_kv_keep(Cache c, Packed r, const int *p
   }
 }
 
-// One thread a node and word: up through the parents, which lie before their children.
+// One thread a node: up through the parents, which lie before their children, so that
+// its words are done one after the other, the last first.
 __global__ void __launch_bounds__(256) k_tree_masks(const int *parents, const int *starts,
                                                     size_t batch, size_t rows, int words,
                                                     uint64_t *masks) {
   __shared__ int lds[SEARCH];
   const Search search(starts, batch, lds);
-  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= rows * words) return;
-  const int row = (int)(id / words), word = (int)(id % words);
-  const int b = search.of(row);
-  const Span sp = span_of(starts, nullptr, b, rows);
-  uint64_t m = 0;
-  const bool one = row >= sp.first && row < sp.first + sp.n;  // (of a sequence)
-  for (int i = one ? row - sp.first : -1; i >= 64 * word;) {
-    if (i < 64 * word + 64) m |= (uint64_t)1 << (i - 64 * word);
-    const int up = parents[sp.first + i];
-    i = up < i ? up : -1;
+  const size_t row = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (row >= rows) return;
+  const Span sp = span_of(starts, nullptr, search.of((int)row), rows);
+  const int place = (int)row - sp.first;
+  int i = place < sp.n ? place : -1;  // (no sequence's: below 0 already, or behind its rows)
+  for (int word = words - 1; word >= 0; --word) {
+    uint64_t m = 0;
+    while (i >= 64 * word) {
+      if (i < 64 * word + 64) m |= (uint64_t)1 << (i - 64 * word);
+      const int up = parents[sp.first + i];
+      i = up < i ? up : -1;
+    }
+    masks[row * words + word] = m;
   }
-  masks[id] = m;
 }
 
 template <class F>
@@ -354,7 +356,7 @@ hipError_t launch_kv_keep(const Cache &c, const Packed &r, const int *path, cons
 hipError_t launch_tree_masks(const int *parents, const int *starts, size_t batch, size_t rows,
                              size_t words, uint64_t *masks, hipStream_t st) {
   dim3 grid;
-  const hipError_t e = grid_of((rows * words + 255) / 256, 1, grid);
+  const hipError_t e = grid_of((rows + 255) / 256, 1, grid);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_tree_masks, grid, dim3(256), 0, st, parents, starts, batch, rows,
                      (int)words, masks);

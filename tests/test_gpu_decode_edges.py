@@ -172,6 +172,19 @@ def test_many_sequences():
     assert masks[:, 0].tolist() == [(1 << j + 1) - 1 for n, _ in sizes for j in range(n)]
 
 
+@pytest.mark.parametrize("most", [1, 65, 3000])
+def test_masks_of_deep_trees(most):
+    """Chains of many words, and of fewer words than rows; a row behind them."""
+    parents, follows = [], []
+    for n in (3000, 1, 700):
+        parents += list(range(-1, n - 1))
+        follows += [(1 << i + 1) - 1 for i in range(n)]
+    starts = ints([0, 3000, 3001, 3001, 3701]).cuda()
+    words = -(-most // 64)
+    got = R.tree_masks(ints(parents + [0]).cuda(), starts, most).cpu()
+    assert torch.equal(got, words_of([m % (1 << 64 * words) for m in follows + [0]], words))
+
+
 def test_heads_of_one_group():
     b = Batch([(1, 300), (3, 77)], 1, 128, 32, seed=80)
     (q, qc), = packed(b.rows, [128], 128, BF16, 81)
