@@ -184,7 +184,7 @@ rosetta_status rosetta_kv_keep(const rosetta_kv_cache *cache, const rosetta_kv_r
 
 rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts, size_t batch,
                                   size_t rows, size_t words, uint64_t *masks, void *stream) {
-  if (batch > MAX_BATCH || rows >= MAX_ROWS || words > MAX_WORDS)
+  if (batch > MAX_BATCH || rows >= MAX_ROWS || words > MAX_WORDS || rows * words >= (size_t)1 << 32)
     return fail(ROSETTA_ERR_UNSUPPORTED, "%zu rows of %zu sequences, %zu words each", rows, batch,
                 words);
   if (words < 1) return fail(ROSETTA_ERR_PARAMS, "masks of no words");
