@@ -822,7 +822,8 @@ size_t rosetta_kv_attention_workspace_bytes(size_t heads, size_t kv_heads, size_
  * is the last certain token, parents as for rosetta_tree_masks (NULL: each node's is
  * the one before).  p [rows][vocab]: the target's probabilities after each node, q
  * those that the node's children drafts[] were drawn from (both of type `dtype`;
- * rows of q without children are not read to any effect), u [rows] numbers of [0, 1).
+ * rows of q whose node has no children, or none that takes part, are not read), u
+ * [rows] numbers of [0, 1).
  * From node 0 on the children of the node reached are tried in order: with c = 0 and
  * z = 1 at first, child i with token x is accepted if
  *   u[i] z q[x] < p[x] - c q[x],

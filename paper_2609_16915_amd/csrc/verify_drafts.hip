@@ -9,7 +9,8 @@
 // taking q off r_k / z_k is taking z_k q off r_k.  A child with token x and random
 // number u is accepted where u q(x) <= r_k(x) / z_k, strictly: u z_k q(x) < p(x) - c_k
 // q(x).  Where no child is, the last token is drawn from r_k.  So a rejection costs one
-// pass over two rows, and nothing but c is kept of it.
+// pass over two rows, and nothing but c is kept of it.  r_0 is p itself: the drafter has
+// no distribution at a leaf, so that q is not read where c is 0.
 //
 // All in 64 bits: a draw lies next to one of the vocabulary's borders, and in 32 bits
 // one draw in a hundred or so would depend on the order of the sum.
@@ -45,9 +46,13 @@ __device__ inline double wave_sum(double x) {
   return x;
 }
 
-__device__ inline double left_of(double p, double q, double c) {
-  const double r = p - c * q;
-  return r > 0 ? r : 0;  // (NaN: nothing)
+// (p - c q)+, and p+ without q.  (NaN: nothing)
+__device__ inline double above_0(double r) { return r > 0 ? r : 0; }
+template <class T>
+__device__ inline double left_at(const T *p, const T *q, double c, size_t v) {
+  double r = (double)(float)p[v];
+  if (c != 0) r -= c * (double)(float)q[v];
+  return above_0(r);
 }
 
 // A wave's walk through one sequence's tree.  Lanes hold 64 nodes at a time.
@@ -113,10 +118,10 @@ struct Walk {
 };
 
 // This thread's share, of `threads`, of the sum over values [lo, hi) of a row, N groups of
-// four of either row asked for at a time.
-template <int N, class T>
-__device__ double share(const T *p, const T *q, double c, size_t lo, size_t hi, int thread,
-                        int threads) {
+// four of either row asked for at a time.  Q: whether q is taken off.
+template <int N, bool Q, class T>
+__device__ double share_of(const T *p, const T *q, double c, size_t lo, size_t hi, int thread,
+                           int threads) {
   struct __attribute__((packed, aligned(1))) Four {
     T v[4];
   };
@@ -128,19 +133,29 @@ __device__ double share(const T *p, const T *q, double c, size_t lo, size_t hi, 
     for (int n = 0; n < N; ++n) {
       const int i = i0 + n * threads < fours ? i0 + n * threads : i0;
       __builtin_memcpy(&x[n], p + lo + 4 * (size_t)i, sizeof x[n]);
-      __builtin_memcpy(&y[n], q + lo + 4 * (size_t)i, sizeof y[n]);
+      if constexpr (Q) __builtin_memcpy(&y[n], q + lo + 4 * (size_t)i, sizeof y[n]);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       if (i0 + n * threads >= fours) break;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s[n % 2] += left_of((double)(float)x[n].v[i], (double)(float)y[n].v[i], c);
+      for (int i = 0; i < 4; ++i) {
+        double r = (double)(float)x[n].v[i];
+        if constexpr (Q) r -= c * (double)(float)y[n].v[i];
+        s[n % 2] += above_0(r);
+      }
     }
   }
   for (size_t v = lo + 4 * (size_t)fours + thread; v < hi; v += threads)
-    s[0] += left_of((double)(float)p[v], (double)(float)q[v], c);
+    s[0] += left_at(p, q, Q ? c : 0., v);
   return s[0] + s[1];
+}
+// (c is the same in all of them)
+template <int N, class T>
+__device__ double share(const T *p, const T *q, double c, size_t lo, size_t hi, int thread,
+                        int threads) {
+  return c != 0 ? share_of<N, true>(p, q, c, lo, hi, thread, threads)
+                : share_of<N, false>(p, q, c, lo, hi, thread, threads);
 }
 
 // One round: every workgroup walks as far as the sums so far go and makes its piece of
@@ -288,7 +303,7 @@ __global__ void __launch_bounds__(TEAM) k_verify_end(Job j) {
     const size_t v0 = std::min(lo + threadIdx.x * each, hi), v1 = std::min(v0 + each, hi);
     double mine = 0;
     for (size_t v = v0; v < v1; ++v)
-      mine += left_of((double)(float)p[v], (double)(float)q[v], at);
+      mine += left_at(p, q, at, v);
     double upto = mine;  // inclusive over the wave, then with the waves before
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -304,7 +319,7 @@ __global__ void __launch_bounds__(TEAM) k_verify_end(Job j) {
     auto some = [&](double run) {  // the first value past the aim, or the last with weight
       int v_last = -1;
       for (size_t v = v0; v < v1; ++v) {
-        const double r = left_of((double)(float)p[v], (double)(float)q[v], at);
+        const double r = left_at(p, q, at, v);
         if (!(r > 0)) continue;
         v_last = (int)v;
         run += r;

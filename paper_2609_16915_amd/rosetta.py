@@ -1188,8 +1188,8 @@ def kv_attention(q, cache, table, starts, lens, masks=None, scale: float = None,
 def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=None):
     """(tokens, path, count): drafted tokens verified against the target's probabilities.
     p, q [rows][vocab] (of one type): the target's after each row, and those that the
-    row's children were drawn from; drafts int64 [rows] the tokens, u float32 [rows]
-    numbers of [0, 1).  A sequence's rows are the nodes of a tree whose node 0 is the
+    row's children were drawn from (anything, where it has none); drafts int64 [rows] the
+    tokens, u float32 [rows] numbers of [0, 1).  A sequence's rows are the nodes of a tree whose node 0 is the
     last certain token; parents int32 [rows] as for tree_masks (None: each follows the
     one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
     how many new tokens there are; path int32 and tokens int64 [rows]: those, from each
