@@ -6,6 +6,11 @@ int64 read as raw 64-bit words), passed by data_ptr() together with the
 current HIP stream; host helpers take and return numpy arrays.  There is no
 fallback: if the library is not built, or a call fails, an exception is
 raised.
+
+A call given a `stream` is put on that stream and waits for nothing on any
+other: what it reads must be ready there (made on it, or before its
+wait_stream(); torch.ones() beside the call is on the current stream, and is
+not), and must stay until it has run.
 """
 from __future__ import annotations
 
