@@ -253,8 +253,9 @@ struct Rows16 {
         for (int i = 0; i < 8; ++i) h[i] = (_Float16)ldexpf(f[ks][i], up);
         __builtin_memcpy(&q[j][ks], h, 16);
       }
-      // (never 0: what is not seen has a score of -infinity)
-      factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), 0x1p-120f) + odd;
+      // (never 0: what is not seen has a score of -infinity; but of so little that no other
+      // score, 2^128 at most, comes to anything by it)
+      factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), 0x1p-149f) + odd;
       top[j] = NONE;
       big[j] = 0.f;
       ref[j] = 0.f;

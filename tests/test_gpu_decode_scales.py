@@ -1,0 +1,129 @@
+"""Attention over caches whose scales are of any size: past 2^100, far apart from each
+other, and keys whose scales make up for tiny queries.
+
+Bounds: a score as in attend64 (test_gpu_decode).  The products p_t v_scale[t] become
+weights of f16, the largest of a row's between 2^-2 and 2^15, so that a weight is off by
+2^-11 of itself or, where it is small, by 2^-25, which is at most 2^-23 of the largest."""
+import math
+
+import pytest
+
+from paper_2609_16915_amd import rosetta as R
+
+from gpu_helpers import require_gpu
+from test_gpu_decode import (BF16, D, E, F16, F32, U, Batch, ancestors, gen, packed,
+                             seen_fast, tree, within, words_of)
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def attend64(b, q, masks, scale):
+    """(out, lse, bound of out, bound of lse)."""
+    rows, heads, dim = q.shape
+    group = heads // b.heads
+    zero = torch.zeros((), dtype=D)
+    out, lse = torch.zeros((rows, heads, dim), dtype=D), torch.full((rows, heads), -math.inf, dtype=D)
+    bo, bl = torch.zeros_like(out), torch.zeros((rows, heads), dtype=D)
+    for i, (n, length) in enumerate(b.sizes):
+        k, there = b.values(i, 0, length)
+        v, _ = b.values(i, 1, length)
+        finite = torch.isfinite(k).all(2) & torch.isfinite(v).all(2)
+        k, v = (torch.where(finite[..., None], t, zero) for t in (k, v))
+        vs = torch.stack([b.scale[1][b.place(i, t)[0], :, b.place(i, t)[1]].abs().to(D)
+                          if there[t] else torch.zeros(b.heads, dtype=D) for t in range(length)], 1)
+        seen = seen_fast(b, i, masks) & there[None]
+        at = slice(b.starts[i], b.starts[i] + n)
+        for h in range(heads):
+            x, g = q[at, h].to(D), h // group
+            sees = seen & finite[g][None] if masks is not None else seen
+            s = (x @ k[g].t() * scale).masked_fill(~sees, -math.inf)
+            z = torch.logsumexp(s, 1)
+            p = torch.where(sees, torch.exp(s - z.nan_to_num(0, 0, 0)[:, None]), zero)
+            lse[at, h] = z
+            out[at, h] = p @ v[g]
+            mags = (x.abs() @ k[g].abs().t() * scale).masked_fill(~sees, 0).amax(1)
+            es = ((dim + 9) * E * mags + 8 * E)[:, None]
+            largest = (p * torch.where(finite[g], vs[g], zero)[None]).amax(1)
+            few = sees.sum(1) * 2.0 ** -23 * largest * 128
+            bo[at, h] = p @ v[g].abs() * (U[F16] + 2 * es + (length + 64) * E) + few[:, None]
+            # (reference and logarithm of the sum: up to 128 each beside the result)
+            bl[at, h] = es[:, 0] + (length + 64) * E + 4 * E * (160 + z.abs().nan_to_num(0, 0, 0))
+    bo = bo + U[q.dtype] * (out.abs() + bo) + (2.0 ** -25 if q.dtype == F16 else 0)
+    return out, lse, bo, bl
+
+
+def check(b, q, masks=None, scale=None):
+    qc = q.cuda()
+    out, lse = R.kv_attention(qc, *b.cuda(), scale=scale, max_rows=max(n for n, _ in b.sizes),
+                              masks=None if masks is None else masks.cuda())
+    o, z, bo, bl = attend64(b, q, masks, b.dim ** -0.5 if scale is None else scale)
+    within(lse, z, bl)
+    within(out, o, bo)
+    return out, lse
+
+
+# (sizes, heads, heads of the cache, dim): a kernel each, with and without parts
+CALLS = {
+    "one row": ([(1, 700)], 4, 1, 64),
+    "one row, parts": ([(1, 3000)], 4, 1, 128),
+    "rows": ([(20, 500), (3, 260)], 4, 2, 128),
+    "rows of 80": ([(9, 300)], 6, 2, 80),
+    "rows of 256": ([(7, 400)], 4, 1, 256),
+    "tiles of 128": ([(140, 900), (33, 33)], 2, 1, 128),
+    "tiles of 96": ([(140, 300)], 2, 1, 96),
+    "tiles of 256": ([(40, 500), (70, 71)], 2, 1, 256),
+    "tiles of 64": ([(130 + i, 130 + 3 * i) for i in range(16)], 16, 16, 64),
+}
+
+
+def call(name, seed, page=16):
+    sizes, heads, kv, dim = CALLS[name]
+    if name == "tiles of 64":  # (the kernel of tiles is taken from 512 workgroups on)
+        assert len(sizes) * kv * -(-max(n for n, _ in sizes) * heads // kv // 128) >= 512
+    b = Batch(sizes, kv, dim, page, seed=seed)
+    q = torch.randn((b.rows, heads, dim), generator=gen(seed + 1))
+    return b, q
+
+
+def at_places(b, f):
+    """f(i, t, page, place) for every position of every sequence."""
+    for i, (_, length) in enumerate(b.sizes):
+        for t in range(length):
+            pg, at = b.place(i, t)
+            f(i, t, pg, at)
+
+
+def masks_of(b):
+    import random
+    rng = random.Random(5)
+    most = max(n for n, _ in b.sizes)
+    return words_of([r for n, _ in b.sizes for r in ancestors(tree(rng, n))], -(-most // 64))
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_tiny_queries(name):
+    """Scores of some tens from queries of 2^-123, scales of keys of 2^93 and a scale of 2^28."""
+    b, q = call(name, 115)
+    b.scale[0] *= 2.0 ** 99
+    check(b, (q * 2.0 ** -123).to(BF16), scale=2.0 ** 24)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_tiny_scales_of_keys_and_huge_queries(name):
+    b, q = call(name, 106)
+    b.scale[0] *= 2.0 ** -112
+    check(b, (q * 2.0 ** 112).to(BF16))
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("power", [97])
+def test_no_scale_gives_the_mean_whatever_the_keys_are(name, power):
+    b, q = call(name, 107)
+    b.scale[0] *= 2.0 ** power
+    check(b, q.to(BF16), scale=0.0)
