@@ -806,7 +806,8 @@ rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts,
  * max_rows: no sequence has more rows (those behind are left as they were; with
  * masks, max_rows <= 64 words).  Scores, statistics and sums are 32-bit; the weights
  * of the values are rounded to f16 with 2^15 for the largest possible (scales of
- * values from 2^-80 to 2^100 keep their precision).  workspace:
+ * values from 2^-80 to 2^100 keep their precision).  Scales of keys may be of any
+ * size (beside some of 2^100 and more, rows of q below 2^100).  workspace:
  * rosetta_kv_attention_workspace_bytes bytes (0 where parts of a sequence need no
  * joining), positions being table_len * page. */
 rosetta_status rosetta_kv_attention(const void *q, size_t q_row_stride, size_t q_head_stride,

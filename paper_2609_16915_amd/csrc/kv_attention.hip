@@ -37,6 +37,17 @@ using u32 = uint32_t;
 
 constexpr float NONE = -__builtin_inff();
 
+// Products <q, K> go up to 2^28 (q up to 2^13, K to 2^7, 256 of them), so that a key's
+// scale of FAR or more could take them past what 32 bits hold.  A wave that meets one takes
+// all of them 2^-28 times as large from there on, and what its scores are multiplied with
+// 2^28 times: nothing is lost, and a cache without any pays a comparison (prompt of 8192
+// 684 us -> 690, trees of 25 30.0 -> 30.3).
+constexpr float FAR = 0x1p100f, NEARER_K = 0x1p-28f;
+
+// What a score is multiplied with, at least: not 0, since what is not seen has a score of
+// -infinity, and so little that no other score, 2^128 at most, comes to anything by it.
+constexpr float LEAST = 0x1p-149f;
+
 // (by value: std::min's references kept its operands in scratch memory, and with them
 // all that follows from them in vector registers)
 __device__ inline int least(int a, int b) { return a < b ? a : b; }
@@ -209,6 +220,7 @@ struct Rows16 {
   float big[NY];      // the largest v_scale, whatever its sign
   float ref[NY], sum[NY];
   v4f o[NX][NY];
+  bool far_k = false;  // keys' scales count as NEARER_K of what they are (the same in all lanes)
 
   // q's values k .. + 7 of a lane come from its row's first(ks) on.  `at` gives the Row
   // of group j, of which row `some` of the call is one for sure.  All of it is asked for
@@ -245,7 +257,9 @@ struct Rows16 {
       }
       m = row_max(m);
       odd = row_sum(odd);  // NaN where the row holds NaN or an infinity
-      const int up = m > 0.f ? 13 - __builtin_amdgcn_frexp_expf(m) : 0;
+      // (no more than 2^120, which brings bf16's smallest to f16's normal numbers, and keeps
+      // the factor one)
+      const int up = m > 0.f ? least(13 - __builtin_amdgcn_frexp_expf(m), 120) : 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         _Float16 h[8];
@@ -253,15 +267,22 @@ struct Rows16 {
         for (int i = 0; i < 8; ++i) h[i] = (_Float16)ldexpf(f[ks][i], up);
         __builtin_memcpy(&q[j][ks], h, 16);
       }
-      // (never 0: what is not seen has a score of -infinity; but of so little that no other
-      // score, 2^128 at most, comes to anything by it)
-      factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), 0x1p-149f) + odd;
+      factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), LEAST) + odd;
       top[j] = NONE;
       big[j] = 0.f;
       ref[j] = 0.f;
       sum[j] = 0.f;
 #pragma unroll
       for (int i = 0; i < NX; ++i) o[i][j] = v4f{0, 0, 0, 0};
+    }
+  }
+
+  __device__ void nearer_keys() {
+    far_k = true;
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      top[j] *= NEARER_K;
+      factor[j] = factor[j] > LEAST ? factor[j] * (1 / NEARER_K) : factor[j];
     }
   }
 
@@ -557,7 +578,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
       }
     if (more) load_keys(ahead);
     // The largest of the scales, as bits: of numbers that are positive and finite, of
-    // which all are as a rule.
+    // which all are as a rule, and below FAR.
     u32 tops[2] = {0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -567,8 +588,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
         tops[1] = max3(tops[1], bits_of(fvs[h][r]), bits_of(fvs[h][r + 1]));
       }
     float most = __builtin_bit_cast(float, tops[1]);
-    if (__any(tops[0] >= 0x7f800000u || tops[1] >= 0x7f800000u)) {
+    if (x.far_k || __any(tops[0] >= bits_of(FAR) || tops[1] >= 0x7f800000u)) {
       most = 0.f;
+      bool far = false;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -578,7 +600,22 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
           fks[h][r] = k;
           fvs[h][r] = v;
           most = max2(most, fabsf(v));
+          far |= fabsf(k) >= FAR;
         }
+      if (!x.far_k && __any(far)) {  // (one that is there?)
+        const int room = s.length - t - 4 * g;
+        far = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            far |= fabsf(fks[h][r]) >= FAR && is_page(a, now[h]) && 16 * h + r < room;
+        if (__any(far)) x.nearer_keys();
+      }
+      if (x.far_k) {
+        fks[0] *= NEARER_K;
+        fks[1] *= NEARER_K;
+      }
     }
     v4i p[1][NY];
     const bool there[2] = {is_page(a, now[0]), is_page(a, now[1])};
@@ -693,10 +730,13 @@ __device__ inline void interleave() {
 // after is on its way.
 template <int D, int NY>
 struct Many {
-  static constexpr int KS = D / 32, NX = D / 16, NS = D / 64, VB = D / 16;
+  static constexpr int STEPS = D / 32, NX = D / 16, NS = D / 64, VB = D / 16;
   static constexpr int TILE = 64;
-  static constexpr int KEYS = 4 * KS * 1024, VALUES = 2 * NX * 1024;
-  static constexpr int STAGE = KEYS + VALUES + 2 * TILE * 4 + 32;  // and scales, what is there, largest
+  static constexpr int KEYS = 4 * STEPS * 1024, VALUES = 2 * NX * 1024;
+  // behind them the scales (keys', values', keys' NEARER_K times), of each wave's sixteen what
+  // is there (and bit 1: a key's scale is FAR or more), and the largest scale of values
+  static constexpr int KS = 0, VS = TILE, NEAR_KS = 2 * TILE, THERE = 3 * TILE, MOST = THERE + 4;
+  static constexpr int STAGE = KEYS + VALUES + (MOST + 4) * 4;
   static constexpr int LDS = 2 * STAGE;
   static constexpr int ROWS = 4 * 16 * NY;
 };
@@ -747,6 +787,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     vb v[4];
     float ks, vs;
     bool there;
+    int room;  // positions from its first on that are in the table
   } sub;
   const u32 dim = (u32)a.cache.dim, stride = (u32)a.cache.place_stride;
   u32 kat[M::NS];
@@ -759,6 +800,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   auto load = [&](int t) {
     const Sixteen at = sixteen_at(s, a, entry, t + 16 * wave);
     sub.there = is_page(a, entry);
+    sub.room = s.length - (t + 16 * wave);
     entry = t + M::TILE < to ? entry_at(s, a, t + M::TILE + 16 * wave) : -1;
 #pragma unroll
     for (int c = 0; c < M::NS; ++c) sub.k[c] = *(const v4i *)(at.k + kat[c]);
@@ -772,7 +814,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   auto write_piece = [&](char *stage, int piece) {
 #pragma unroll
     for (int c = piece * M::NS / PIECES; c < (piece + 1) * M::NS / PIECES; ++c) {
-      char *to = stage + (((wave * M::KS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
+      char *to = stage + (((wave * M::STEPS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
       const v2i a0 = widen(sub.k[c].x), a1 = widen(sub.k[c].y);
       const v2i b0 = widen(sub.k[c].z), b1 = widen(sub.k[c].w);
       *(v4i *)to = v4i{a0.x, a0.y, a1.x, a1.y};
@@ -803,10 +845,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     most = max2(most, turned<2>(most));
     most = max2(most, turned<1>(most));
     // (the lanes of a place write the same)
-    scales[16 * wave + m] = sub.ks;
-    scales[M::TILE + 16 * wave + m] = sub.vs;
-    ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
-    scales[2 * M::TILE + 4 + wave] = most;
+    scales[M::KS + 16 * wave + m] = sub.ks;
+    scales[M::VS + 16 * wave + m] = sub.vs;
+    scales[M::NEAR_KS + 16 * wave + m] = sub.ks * NEARER_K;
+    const bool far = __ballot(fabsf(sub.ks) >= FAR) & below(sub.room) & 0xffff;
+    ((int *)scales)[M::THERE + wave] = sub.there ? far ? 3 : 1 : 0;
+    scales[M::MOST + wave] = most;
   };
   auto write = [&](char *stage) {
 #pragma unroll
@@ -816,8 +860,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     const v4i *keys = (const v4i *)stage + lane;
     const v4i *values = (const v4i *)(stage + M::KEYS) + lane;
     const float *scales = (const float *)(stage + M::KEYS + M::VALUES);
-    auto ks = [&](int h) { return *(const v4f *)(scales + 16 * h + 4 * g); };
-    auto vs = [&](int h) { return *(const v4f *)(scales + M::TILE + 16 * h + 4 * g); };
+    const v4i there = *(const v4i *)(scales + M::THERE);
+    const int flags = __builtin_amdgcn_readfirstlane((there[0] | there[1] | there[2] | there[3]) & 2) |
+                      __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3] & 1);
+    if (!x.far_k && (flags & 2)) x.nearer_keys();
+    const float *key_scales = scales + (x.far_k ? M::NEAR_KS : M::KS) + 4 * g;
+    auto ks = [&](int h) { return *(const v4f *)(key_scales + 16 * h); };
+    auto vs = [&](int h) { return *(const v4f *)(scales + M::VS + 16 * h + 4 * g); };
     v4f sc[4][NY];
     float largest[NY];
 #pragma unroll
@@ -827,20 +876,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     // is spread between the products that follow, here and below: a wave's vector and
     // matrix instructions then run side by side.  The wave at its products goes first
     // where two want to issue (16384 rows of 128 over 4096 positions: 204 us -> 198).
-    v4i kf[2][M::KS];
+    v4i kf[2][M::STEPS];
     if constexpr (D < 256) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int c = 0; c < M::KS; ++c) kf[0][c] = keys[c * 64];
+    for (int c = 0; c < M::STEPS; ++c) kf[0][c] = keys[c * 64];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
 #pragma unroll
       for (int j = 0; j < NY; ++j) sc[h][j] = v4f{0, 0, 0, 0};
       if (h < 3) {
 #pragma unroll
-        for (int c = 0; c < M::KS; ++c) kf[(h + 1) % 2][c] = keys[((h + 1) * M::KS + c) * 64];
+        for (int c = 0; c < M::STEPS; ++c) kf[(h + 1) % 2][c] = keys[((h + 1) * M::STEPS + c) * 64];
       }
 #pragma unroll
-      for (int c = 0; c < M::KS; ++c)
+      for (int c = 0; c < M::STEPS; ++c)
 #pragma unroll
         for (int j = 0; j < NY; ++j) sc[h][j] = mac(kf[h % 2][c], x.q[j][c], sc[h][j]);
       if (h > 0) {
@@ -850,19 +899,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     }
     if constexpr (D < 256) __builtin_amdgcn_s_setprio(0);
     x.template scaled<4>(sc, 3, ks(3), largest);
-    const int *there = (const int *)(scales + 2 * M::TILE);
-    const int here = __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3]);
     x.template refer<4>(
         sc, largest, vs,
         [&] {
-          const v4f most = *(const v4f *)(scales + 2 * M::TILE + 4);
+          const v4f most = *(const v4f *)(scales + M::MOST);
           return max3(max2(most[0], most[1]), most[2], most[3]);
         },
-        !(t + M::TILE <= all && here),
+        !(t + M::TILE <= all && (flags & 1)),
         [&](int j) {
           uint64_t in = 0;
 #pragma unroll
-          for (int h = 0; h < 4; ++h) in |= (uint64_t)(there[h] ? 0xffff : 0) << (16 * h);
+          for (int h = 0; h < 4; ++h) in |= (uint64_t)(there[h] & 1 ? 0xffff : 0) << (16 * h);
           const Row r = row(j);
           const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
           return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);

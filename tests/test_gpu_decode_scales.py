@@ -107,11 +107,35 @@ def masks_of(b):
 
 
 @pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("power", [105, 125])
+def test_huge_scales_of_keys_and_tiny_queries(name, masked, power):
+    """Scores of some tens from queries of 2^-power and keys of 2^power, beside keys of
+    ordinary size, whose scores are 0."""
+    b, q = call(name, 104)
+    b.scale[0] *= torch.where(torch.rand(b.scale[0].shape, generator=gen(105)) < 0.3, 2.0 ** power, 1.0)
+    check(b, (q * 2.0 ** -power).to(BF16), masks_of(b) if masked else None, scale=4.0 * b.dim ** -0.5)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
 def test_tiny_queries(name):
     """Scores of some tens from queries of 2^-123, scales of keys of 2^93 and a scale of 2^28."""
     b, q = call(name, 115)
     b.scale[0] *= 2.0 ** 99
     check(b, (q * 2.0 ** -123).to(BF16), scale=2.0 ** 24)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_unseen_keys_of_every_size_beside_huge_queries(name):
+    b, q = call(name, 116)
+    b.scale[0] *= 2.0 ** -112
+    used = set()
+    at_places(b, lambda i, t, pg, at: used.add((pg, at)))
+    for pg in range(b.pages):
+        for at in range(b.page):
+            if (pg, at) not in used:
+                b.scale[0][pg, :, at] = [2.0 ** 120, -(2.0 ** 126), 0.0][(pg + at) % 3]
+    check(b, (q * 2.0 ** 112).to(BF16))
 
 
 @pytest.mark.parametrize("name", list(CALLS))
@@ -122,7 +146,7 @@ def test_tiny_scales_of_keys_and_huge_queries(name):
 
 
 @pytest.mark.parametrize("name", list(CALLS))
-@pytest.mark.parametrize("power", [97])
+@pytest.mark.parametrize("power", [97, 125])
 def test_no_scale_gives_the_mean_whatever_the_keys_are(name, power):
     b, q = call(name, 107)
     b.scale[0] *= 2.0 ** power
