@@ -37,13 +37,6 @@ using u32 = uint32_t;
 
 constexpr float NONE = -__builtin_inff();
 
-// Products <q, K> go up to 2^28 (q up to 2^13, K to 2^7, 256 of them), so that a key's
-// scale of FAR or more could take them past what 32 bits hold.  A wave that meets one takes
-// all of them 2^-28 times as large from there on, and what its scores are multiplied with
-// 2^28 times: nothing is lost, and a cache without any pays a comparison (prompt of 8192
-// 684 us -> 690, trees of 25 30.0 -> 30.3).
-constexpr float FAR = 0x1p100f, NEARER_K = 0x1p-28f;
-
 // What a score is multiplied with, at least: not 0, since what is not seen has a score of
 // -infinity, and so little that no other score, 2^128 at most, comes to anything by it.
 constexpr float LEAST = 0x1p-149f;
@@ -112,10 +105,23 @@ __device__ inline float row_max(float a) {
 __device__ inline float row_sum(float a) {
   return across(a, [](float x, float y) { return x + y; });
 }
-// The scales of a position: where one of them is no number, or infinite, the score is none,
-// and the value counts as 0, so that rows that do not see it are not touched.
-__device__ inline void settle(float &k, float &v) {
-  const bool fine = fabsf(v) < __builtin_inff() && fabsf(k) < __builtin_inff();
+// ---- scales of any size ----
+//
+// The first pass over the cache takes for granted, but looks, what holds for scales as caches
+// have them:
+//  - no key's scale is FAR.  Products <q, K> go up to 2^28 (q to 2^13, K to 2^7, 256 of them),
+//    and times 2^100 past what 32 bits hold.
+//  - no value's is.  A row's exponentials are at most 2^15 over the largest scale of its values,
+//    and too many would be below what 32 bits hold for their sum.
+// Where one does not hold, the pass is made again, with scales 2^-28 as large (and 2^28 times
+// as much to each score) if some are FAR, and a row's reference that of its largest product of
+// exponential and scale.  Such rows take more than twice as long.
+constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
+
+// The scales of a position: where one of them is no number, or infinite, or it is not there,
+// the score is none, and the value counts as 0, so that rows that do not see it are not touched.
+__device__ inline void settle(float &k, float &v, bool there) {
+  const bool fine = there && fabsf(v) < __builtin_inff() && fabsf(k) < __builtin_inff();
   k = fine ? k : __builtin_nanf("");
   v = fine ? v : 0.f;
 }
@@ -136,6 +142,15 @@ struct Work {
   float *sums;       // parts > 1: [rows][heads][parts][DIM], (reference, sum) [..][parts]
   float2 *ends;
 };
+
+// The launch's arguments where they lie, for a function that is called: an address that the
+// compiler knows to be the same in all lanes.
+__device__ inline const Work *alike(const Work *w) {
+  const uint64_t p = (uintptr_t)w;
+  const u32 lo = __builtin_amdgcn_readfirstlane((u32)p);
+  const u32 hi = __builtin_amdgcn_readfirstlane((u32)(p >> 32));
+  return (const Work *)(const __attribute__((address_space(4))) Work *)(((uint64_t)hi << 32) | lo);
+}
 
 // A word that a whole wave reads, through the scalar cache: what a launch only reads, at
 // an address that all lanes share.
@@ -220,7 +235,6 @@ struct Rows16 {
   float big[NY];      // the largest v_scale, whatever its sign
   float ref[NY], sum[NY];
   v4f o[NX][NY];
-  bool far_k = false;  // keys' scales count as NEARER_K of what they are (the same in all lanes)
 
   // q's values k .. + 7 of a lane come from its row's first(ks) on.  `at` gives the Row
   // of group j, of which row `some` of the call is one for sure.  All of it is asked for
@@ -268,6 +282,12 @@ struct Rows16 {
         __builtin_memcpy(&q[j][ks], h, 16);
       }
       factor[j] = fmaxf(ldexpf(a.scale * 1.44269504088896340736f, -up), LEAST) + odd;
+    }
+    clear();
+  }
+  __device__ void clear() {
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
       top[j] = NONE;
       big[j] = 0.f;
       ref[j] = 0.f;
@@ -276,13 +296,25 @@ struct Rows16 {
       for (int i = 0; i < NX; ++i) o[i][j] = v4f{0, 0, 0, 0};
     }
   }
-
-  __device__ void nearer_keys() {
-    far_k = true;
+  // Whether the scales that the rows saw ask for the other pass: 2 if some
+  // are FAR (keys' or the values'), else 1.
+  __device__ int asks(bool far) const {
+#pragma unroll
+    for (int j = 0; j < NY; ++j) far |= big[j] >= FAR;
+    return __any(far) ? 2 : 0;
+  }
+  // Before and after a pass with scales NEARER times as large: scores as they are; sums that
+  // are as much smaller as the outputs.
+  __device__ void nearer() {
+#pragma unroll
+    for (int j = 0; j < NY; ++j)
+      factor[j] = factor[j] > LEAST ? factor[j] * (1 / NEARER) : factor[j];
+  }
+  __device__ void as_they_are() {
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
-      top[j] *= NEARER_K;
-      factor[j] = factor[j] > LEAST ? factor[j] * (1 / NEARER_K) : factor[j];
+      ref[j] += 28;
+      sum[j] *= NEARER;
     }
   }
 
@@ -353,6 +385,40 @@ struct Rows16 {
 #pragma unroll
         for (int i = 0; i < NX; ++i) o[i][j] *= by;
       }
+    }
+  }
+
+  // The same in the other pass: the reference is that of the largest product, and such that no
+  // exponential is past 2^95.
+  template <int TILES, class Vs, class Bits>
+  __device__ void refer_odd(v4f (&s)[TILES][NY], Vs vs, bool masked, Bits bits) {
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      const uint64_t seen = masked ? bits(j) : ~(uint64_t)0;
+      float m = NONE, lift = NONE;
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        const u32 b = (u32)(seen >> (16 * x)) & 0xf;
+        const v4f v = vs(x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[x][j][r] = b & (1u << r) ? s[x][j][r] : NONE;
+          m = max2(m, s[x][j][r]);
+          lift = max2(lift, fmaf(s[x][j][r], factor[j], __builtin_amdgcn_logf(fabsf(v[r]))));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      m = row_max(m);
+      lift = row_max(lift) - 15;
+      const float before = ref[j];
+      const bool none = top[j] == NONE;
+      top[j] = max2(top[j], m);
+      ref[j] = max3(fmaf(top[j], factor[j], -95.f), lift, none ? NONE : before);
+      if (top[j] == NONE) ref[j] = 0.f;
+      const float by = none ? 0.f : __builtin_amdgcn_exp2f(before - ref[j]);
+      sum[j] *= by;
+#pragma unroll
+      for (int i = 0; i < NX; ++i) o[i][j] *= by;
     }
   }
 
@@ -464,9 +530,11 @@ __device__ inline void part_of(int length, int parts, int part, int unit, int &f
 // The waves take steps of 32 positions in turn.  A step's keys make room for the next
 // one's as soon as the scores are there, its values after the second product: no
 // register waits twice, and the other waves' work covers the rest of the way.
-template <int D, int NY>
-__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+//
+// ODD: the other pass, with scales that are `far` or not.  Returns whether the scales met ask for
+// it (2: some are FAR; the same in all threads); then nothing is stored.
+template <int D, int NY, bool ODD>
+__device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   const AttendArgs &a = w.a;
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -486,7 +554,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
   const int part = w.row_blocks > 1 ? id % parts : id / batch;
   const Seq s = seq_of(a, b, head);
   const int r0 = block * 16 * NY;
-  if (r0 >= s.n * w.group) return;
+  if (r0 >= s.n * w.group) return 0;
   auto row = [&](int j) { return row_of(s, r0 + 16 * j + m, w.group, head); };
 
   // positions that some row sees, and that every row sees
@@ -528,6 +596,32 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     }
   };
   constexpr int TURN = 4 * 32;
+  // product ks of 32 takes bytes 16 g + 8 (ks % 2) .. + 8 of chunk ks / 2 of 64
+  Rows16<D, NY> x;
+  auto first = [&](int ks) { return 64 * (ks / 2) + 16 * g + 8 * (ks % 2); };
+  // behind the waves' sums: whether a wave met a key's scale that is FAR, and what that comes to
+  constexpr int EACH = 64 * (4 * Rows16<D, NY>::NX * NY + 4 * NY);
+  int *asked = (int *)lds + 2 * EACH;
+  // The scales of a step settled: the largest of the values', and whether one of the keys' is FAR.
+  auto settle_step = [&](const int (&entries)[2], int t, float &most) {
+    const int room = s.length - t - 4 * g;
+    bool far = false;
+    most = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool page = is_page(a, entries[h]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float k = fks[h][r], v = fvs[h][r];
+        settle(k, v, page && 16 * h + r < room);
+        fks[h][r] = k;
+        fvs[h][r] = v;
+        most = max2(most, fabsf(v));
+        far |= fabsf(k) >= FAR;
+      }
+    }
+    return __any(far);
+  };
   int t = from + 32 * wave;
   // table entries: of this step, and of the next
   int now[2], next[2];
@@ -543,11 +637,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     load_values(at);
   }
 
-  // product ks of 32 takes bytes 16 g + 8 (ks % 2) .. + 8 of chunk ks / 2 of 64
-  Rows16<D, NY> x;
-  auto first = [&](int ks) { return 64 * (ks / 2) + 16 * g + 8 * (ks % 2); };
   if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
   else x.template load<f16>(a, s.first, row, first);
+  if (ODD && far) x.nearer();
 
   for (; t < to; t += TURN) {
     const bool more = t + TURN < to;
@@ -578,7 +670,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
       }
     if (more) load_keys(ahead);
     // The largest of the scales, as bits: of numbers that are positive and finite, of
-    // which all are as a rule, and below FAR.
+    // which all are as a rule.
     u32 tops[2] = {0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -588,33 +680,16 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
         tops[1] = max3(tops[1], bits_of(fvs[h][r]), bits_of(fvs[h][r + 1]));
       }
     float most = __builtin_bit_cast(float, tops[1]);
-    if (x.far_k || __any(tops[0] >= bits_of(FAR) || tops[1] >= 0x7f800000u)) {
-      most = 0.f;
-      bool far = false;
+    if (ODD || __any(tops[0] >= bits_of(FAR) || tops[1] >= bits_of(FAR))) {
+      const bool now_far = settle_step(now, t, most);
+      if constexpr (ODD) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float k = fks[h][r], v = fvs[h][r];
-          settle(k, v);
-          fks[h][r] = k;
-          fvs[h][r] = v;
-          most = max2(most, fabsf(v));
-          far |= fabsf(k) >= FAR;
+        for (int h = 0; h < 2; ++h) {
+          fks[h] *= far ? NEARER : 1.f;
+          fvs[h] *= far ? NEARER : 1.f;
         }
-      if (!x.far_k && __any(far)) {  // (one that is there?)
-        const int room = s.length - t - 4 * g;
-        far = false;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            far |= fabsf(fks[h][r]) >= FAR && is_page(a, now[h]) && 16 * h + r < room;
-        if (__any(far)) x.nearer_keys();
-      }
-      if (x.far_k) {
-        fks[0] *= NEARER_K;
-        fks[1] *= NEARER_K;
+      } else {
+        far |= now_far;
       }
     }
     v4i p[1][NY];
@@ -625,15 +700,17 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     for (int j = 0; j < NY; ++j) largest[j] = NONE;
 #pragma unroll
     for (int h = 0; h < 2; ++h) x.template scaled<2>(sc, h, fks[h], largest);
-    x.template refer<2>(
-        sc, largest, [&](int h) { return fvs[h]; },
-        [&] { return row_max(most); },
-        !(t + 32 <= all && there[0] && there[1]),
-        [&](int j) {
-          const Row r = row(j);
-          const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
-          return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
-        });
+    const bool masked = !(t + 32 <= all && there[0] && there[1]);
+    auto vs = [&](int h) { return fvs[h]; };
+    auto bits = [&](int j) {
+      const Row r = row(j);
+      const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
+      return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
+    };
+    if constexpr (ODD) x.template refer_odd<2>(sc, vs, masked, bits);
+    else
+      x.template refer<2>(
+          sc, largest, vs, [&] { return row_max(most); }, masked, bits);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -666,21 +743,23 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
       next[h] = later[h];
     }
   }
+  if (ODD && far) x.as_they_are();
 
   // The waves' sums together, in order: waves 2 and 3 to 0 and 1, 1 to 0.
-  constexpr int EACH = 64 * (4 * Rows16<D, NY>::NX * NY + 3 * NY);
   float *mine = (float *)lds;
+  if (!ODD) asked[wave] = far;
 #pragma unroll
   for (int half = 2; half >= 1; half /= 2) {
     if (wave >= half && wave < 2 * half) {
       float *to = mine + (wave - half) * EACH + lane;
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
-        to[(3 * j) * 64] = x.top[j];
-        to[(3 * j + 1) * 64] = x.ref[j];
-        to[(3 * j + 2) * 64] = x.sum[j];
+        to[(4 * j) * 64] = x.top[j];
+        to[(4 * j + 1) * 64] = x.ref[j];
+        to[(4 * j + 2) * 64] = x.sum[j];
+        to[(4 * j + 3) * 64] = x.big[j];
       }
-      v4f *of = (v4f *)(mine + (wave - half) * EACH + 3 * NY * 64) + lane;
+      v4f *of = (v4f *)(mine + (wave - half) * EACH + 4 * NY * 64) + lane;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -689,27 +768,60 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend_few(Work w) {
     __syncthreads();
     if (wave < half) {
       const float *of = mine + wave * EACH + lane;
-      const v4f *o = (const v4f *)(mine + wave * EACH + 3 * NY * 64) + lane;
+      const v4f *o = (const v4f *)(mine + wave * EACH + 4 * NY * 64) + lane;
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
-        const float top = of[(3 * j) * 64], ref = of[(3 * j + 1) * 64];
+        const float top = of[(4 * j) * 64], ref = of[(4 * j + 1) * 64], big = of[(4 * j + 3) * 64];
         const bool here = x.top[j] != NONE, there = top != NONE;
         const float both = !here ? ref : !there ? x.ref[j] : fmaxf(ref, x.ref[j]);
-        const float fa = here ? __builtin_amdgcn_exp2f(x.ref[j] - both) : 0.f;
-        const float fb = there ? __builtin_amdgcn_exp2f(ref - both) : 0.f;
+        const float da = here ? x.ref[j] - both : NONE, db = there ? ref - both : NONE;
         x.ref[j] = both;
         x.top[j] = fmaxf(x.top[j], top);
-        x.sum[j] = x.sum[j] * fa + of[(3 * j + 2) * 64] * fb;
+        const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+        x.sum[j] = x.sum[j] * fa + of[(4 * j + 2) * 64] * fb;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) x.o[i][j] = x.o[i][j] * fa + o[(i * NY + j) * 64] * fb;
+        x.big[j] = fmaxf(x.big[j], big);
       }
     }
     __syncthreads();
   }
+  int again = 0;
   if (wave == 0) {
+    if constexpr (!ODD) {
+      const v4i keys = *(const v4i *)asked;
+      again = x.asks(keys[0] | keys[1] | keys[2] | keys[3]);
+      asked[8] = again;
+    }
+    if (!again) {
 #pragma unroll
-    for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
+      for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
+    }
   }
+  if constexpr (!ODD) {
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(asked[8]);
+  }
+  return again;
+}
+
+// (A function of its own: beside the first pass its registers cost that 10 %, on heads of 64.
+// The scratch memory that the compiler reports is what it saves of the kernel's.)
+template <int D, int NY>
+__device__ __attribute__((noinline)) void
+attend_few_odd(const Work *w, __attribute__((address_space(3))) char *lds, bool far) {
+  attend_few<D, NY, true>(*alike(w), (char *)lds, far);
+}
+
+// (waves to a SIMD as the first pass has them by itself: the function would take more registers)
+template <int D, int NY>
+__global__ void __launch_bounds__(256, (D == 64 ? 3 : D == 128 ? 2 : 1) + (D <= 128 && NY == 1))
+    k_attend_few(Work w) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int again = attend_few<D, NY, false>(w, lds, false);
+  if (again)
+    attend_few_odd<D, NY>((const Work *)(const void *)__builtin_amdgcn_kernarg_segment_ptr(),
+                          (__attribute__((address_space(3))) char *)lds, again >= 2);
 }
 
 // MACS matrix instructions with VALUS vector instructions spread between them.
@@ -730,21 +842,18 @@ __device__ inline void interleave() {
 // after is on its way.
 template <int D, int NY>
 struct Many {
-  static constexpr int STEPS = D / 32, NX = D / 16, NS = D / 64, VB = D / 16;
+  static constexpr int KS = D / 32, NX = D / 16, NS = D / 64, VB = D / 16;
   static constexpr int TILE = 64;
-  static constexpr int KEYS = 4 * STEPS * 1024, VALUES = 2 * NX * 1024;
-  // behind them the scales (keys', values', keys' NEARER_K times), of each wave's sixteen what
-  // is there (and bit 1: a key's scale is FAR or more), and the largest scale of values
-  static constexpr int KS = 0, VS = TILE, NEAR_KS = 2 * TILE, THERE = 3 * TILE, MOST = THERE + 4;
-  static constexpr int STAGE = KEYS + VALUES + (MOST + 4) * 4;
-  static constexpr int LDS = 2 * STAGE;
+  static constexpr int KEYS = 4 * KS * 1024, VALUES = 2 * NX * 1024;
+  static constexpr int STAGE = KEYS + VALUES + 2 * TILE * 4 + 32;  // and scales, what is there, largest
+  static constexpr int LDS = 2 * STAGE;  // (and 32 bytes for what the waves ask for)
   static constexpr int ROWS = 4 * 16 * NY;
 };
 
-template <int D, int NY>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend_many(Work w) {
+// (ODD and what it returns as for attend_few)
+template <int D, int NY, bool ODD>
+__device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales_far) {
   using M = Many<D, NY>;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
   const AttendArgs &a = w.a;
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -761,7 +870,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   const int part = rest % (unsigned)w.parts, b = rest / (unsigned)w.parts;
   const Seq s = seq_of(a, b, head);
   const int r0 = block * M::ROWS;
-  if (r0 >= s.n * w.group) return;
+  if (r0 >= s.n * w.group) return 0;
   const int rw = r0 + 16 * NY * wave;
   auto row = [&](int j) { return row_of(s, rw + 16 * j + m, w.group, head); };
 
@@ -769,13 +878,15 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   auto first = [&](int ks) { return 32 * ks + 8 * g; };
   if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
   else x.template load<f16>(a, s.first, row, first);
+  uint64_t far = scales_far;
+  if (ODD && far) x.nearer();
 
   // what some row of the workgroup sees, of this wave sees, and all of this wave's see
   const int n1 = s.n - 1;
   const int last = least((r0 + M::ROWS - 1) / w.group, n1);
-  const int mine = least((rw + 16 * NY - 1) / w.group, n1);
+  const int mine_last = least((rw + 16 * NY - 1) / w.group, n1);
   const int end = a.masks ? s.length : least(s.length, s.base + last + 1);
-  int some = a.masks ? s.length : least(s.length, s.base + mine + 1);
+  int some = a.masks ? s.length : least(s.length, s.base + mine_last + 1);
   const int all = least(s.length, s.base + (a.masks ? 0 : rw / w.group + 1));
   if (rw >= s.n * w.group) some = 0;
   int from, to;
@@ -787,7 +898,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     vb v[4];
     float ks, vs;
     bool there;
-    int room;  // positions from its first on that are in the table
+    int room;  // positions that are there, from its first on
   } sub;
   const u32 dim = (u32)a.cache.dim, stride = (u32)a.cache.place_stride;
   u32 kat[M::NS];
@@ -800,7 +911,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   auto load = [&](int t) {
     const Sixteen at = sixteen_at(s, a, entry, t + 16 * wave);
     sub.there = is_page(a, entry);
-    sub.room = s.length - (t + 16 * wave);
+    sub.room = sub.there ? s.length - (t + 16 * wave) : 0;
     entry = t + M::TILE < to ? entry_at(s, a, t + M::TILE + 16 * wave) : -1;
 #pragma unroll
     for (int c = 0; c < M::NS; ++c) sub.k[c] = *(const v4i *)(at.k + kat[c]);
@@ -814,7 +925,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
   auto write_piece = [&](char *stage, int piece) {
 #pragma unroll
     for (int c = piece * M::NS / PIECES; c < (piece + 1) * M::NS / PIECES; ++c) {
-      char *to = stage + (((wave * M::STEPS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
+      char *to = stage + (((wave * M::KS + 2 * c + g / 2) * 64 + g % 2 * 32 + m) * 16);
       const v2i a0 = widen(sub.k[c].x), a1 = widen(sub.k[c].y);
       const v2i b0 = widen(sub.k[c].z), b1 = widen(sub.k[c].w);
       *(v4i *)to = v4i{a0.x, a0.y, a1.x, a1.y};
@@ -837,7 +948,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     turn(std::integral_constant<int, 3>{});
     if (piece) return;
     float *scales = (float *)(stage + M::KEYS + M::VALUES);
-    settle(sub.ks, sub.vs);
+    settle(sub.ks, sub.vs, m < sub.room);
+    if constexpr (ODD) {
+      sub.ks *= far ? NEARER : 1.f;
+      sub.vs *= far ? NEARER : 1.f;
+    } else {
+      far |= __ballot(fabsf(sub.ks) >= FAR);
+    }
     // the largest v_scale of the sixteen
     float most = fabsf(sub.vs);
     most = max2(most, turned<8>(most));
@@ -845,13 +962,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     most = max2(most, turned<2>(most));
     most = max2(most, turned<1>(most));
     // (the lanes of a place write the same)
-    scales[M::KS + 16 * wave + m] = sub.ks;
-    scales[M::VS + 16 * wave + m] = sub.vs;
-    scales[M::NEAR_KS + 16 * wave + m] = sub.ks * NEARER_K;
-    const bool far = __ballot(fabsf(sub.ks) >= FAR) & below(sub.room) & 0xffff;
-    ((int *)scales)[M::THERE + wave] = sub.there ? far ? 3 : 1 : 0;
-    scales[M::MOST + wave] = most;
+    scales[16 * wave + m] = sub.ks;
+    scales[M::TILE + 16 * wave + m] = sub.vs;
+    ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
+    scales[2 * M::TILE + 4 + wave] = most;
   };
+  int *asked = (int *)(lds + M::LDS);  // what the waves ask for
   auto write = [&](char *stage) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) write_piece(stage, i);
@@ -860,13 +976,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     const v4i *keys = (const v4i *)stage + lane;
     const v4i *values = (const v4i *)(stage + M::KEYS) + lane;
     const float *scales = (const float *)(stage + M::KEYS + M::VALUES);
-    const v4i there = *(const v4i *)(scales + M::THERE);
-    const int flags = __builtin_amdgcn_readfirstlane((there[0] | there[1] | there[2] | there[3]) & 2) |
-                      __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3] & 1);
-    if (!x.far_k && (flags & 2)) x.nearer_keys();
-    const float *key_scales = scales + (x.far_k ? M::NEAR_KS : M::KS) + 4 * g;
-    auto ks = [&](int h) { return *(const v4f *)(key_scales + 16 * h); };
-    auto vs = [&](int h) { return *(const v4f *)(scales + M::VS + 16 * h + 4 * g); };
+    auto ks = [&](int h) { return *(const v4f *)(scales + 16 * h + 4 * g); };
+    auto vs = [&](int h) { return *(const v4f *)(scales + M::TILE + 16 * h + 4 * g); };
     v4f sc[4][NY];
     float largest[NY];
 #pragma unroll
@@ -876,20 +987,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     // is spread between the products that follow, here and below: a wave's vector and
     // matrix instructions then run side by side.  The wave at its products goes first
     // where two want to issue (16384 rows of 128 over 4096 positions: 204 us -> 198).
-    v4i kf[2][M::STEPS];
+    v4i kf[2][M::KS];
     if constexpr (D < 256) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int c = 0; c < M::STEPS; ++c) kf[0][c] = keys[c * 64];
+    for (int c = 0; c < M::KS; ++c) kf[0][c] = keys[c * 64];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
 #pragma unroll
       for (int j = 0; j < NY; ++j) sc[h][j] = v4f{0, 0, 0, 0};
       if (h < 3) {
 #pragma unroll
-        for (int c = 0; c < M::STEPS; ++c) kf[(h + 1) % 2][c] = keys[((h + 1) * M::STEPS + c) * 64];
+        for (int c = 0; c < M::KS; ++c) kf[(h + 1) % 2][c] = keys[((h + 1) * M::KS + c) * 64];
       }
 #pragma unroll
-      for (int c = 0; c < M::STEPS; ++c)
+      for (int c = 0; c < M::KS; ++c)
 #pragma unroll
         for (int j = 0; j < NY; ++j) sc[h][j] = mac(kf[h % 2][c], x.q[j][c], sc[h][j]);
       if (h > 0) {
@@ -899,21 +1010,28 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     }
     if constexpr (D < 256) __builtin_amdgcn_s_setprio(0);
     x.template scaled<4>(sc, 3, ks(3), largest);
-    x.template refer<4>(
-        sc, largest, vs,
-        [&] {
-          const v4f most = *(const v4f *)(scales + M::MOST);
-          return max3(max2(most[0], most[1]), most[2], most[3]);
-        },
-        !(t + M::TILE <= all && (flags & 1)),
-        [&](int j) {
-          uint64_t in = 0;
+    const int *there = (const int *)(scales + 2 * M::TILE);
+    const int here = __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3]);
+    const bool masked = !(t + M::TILE <= all && here);
+    auto bits = [&](int j) {
+      uint64_t in = 0;
 #pragma unroll
-          for (int h = 0; h < 4; ++h) in |= (uint64_t)(there[h] & 1 ? 0xffff : 0) << (16 * h);
-          const Row r = row(j);
-          const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
-          return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
-        });
+      for (int h = 0; h < 4; ++h) in |= (uint64_t)(there[h] ? 0xffff : 0) << (16 * h);
+      const Row r = row(j);
+      const uint64_t *mask = a.masks && r.at >= 0 ? a.masks + r.at * a.words : nullptr;
+      return (seen_from(s, a, mask, r.i, t) & in) >> (4 * g);
+    };
+    if constexpr (ODD) {
+      x.template refer_odd<4>(sc, vs, masked, bits);
+    } else {
+      x.template refer<4>(
+          sc, largest, vs,
+          [&] {
+            const v4f most = *(const v4f *)(scales + 2 * M::TILE + 4);
+            return max3(max2(most[0], most[1]), most[2], most[3]);
+          },
+          masked, bits);
+    }
     v4i p[2][NY];
     constexpr int G = 4, EACH = M::NX / G;  // groups of products with the values, per half
     v4i vf[2][G];
@@ -968,8 +1086,34 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend
     if (t + M::TILE < to) write(lds + (at ^ 1) * M::STAGE);
     if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
   }
+  if constexpr (ODD) {
+    if (far) x.as_they_are();
+  } else {
+    // (what one wave asks for, all do: they write each other's tiles)
+    asked[wave] = x.asks(far);
+    __syncthreads();
+    const v4i all = *(const v4i *)asked;
+    const int again = __builtin_amdgcn_readfirstlane(all[0] | all[1] | all[2] | all[3]);
+    if (again) return again;
+  }
 #pragma unroll
   for (int j = 0; j < NY; ++j) x.store(w, row(j), j, part);
+  return 0;
+}
+
+template <int D, int NY>
+__device__ __attribute__((noinline)) void
+attend_many_odd(const Work *w, __attribute__((address_space(3))) char *lds, bool far) {
+  attend_many<D, NY, true>(*alike(w), (char *)lds, far);
+}
+
+template <int D, int NY>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend_many(Work w) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int again = attend_many<D, NY, false>(w, lds, false);
+  if (again)
+    attend_many_odd<D, NY>((const Work *)(const void *)__builtin_amdgcn_kernarg_segment_ptr(),
+                           (__attribute__((address_space(3))) char *)lds, again >= 2);
 }
 
 // ---- parts of a sequence joined ----
@@ -1125,7 +1269,7 @@ hipError_t launch_kv_attention(const AttendArgs &given, hipStream_t st) {
     hipError_t e = hipSuccess;
     auto few = [&](auto ny) {
       constexpr int NY = decltype(ny)::value;
-      constexpr size_t LDS = 2 * 64 * (4 * (D / 16) * NY + 3 * NY) * sizeof(float);
+      constexpr size_t LDS = 2 * 64 * (4 * (D / 16) * NY + 4 * NY) * sizeof(float) + 48;
       e = allow_lds(k_attend_few<D, NY>, LDS);
       if (e != hipSuccess) return;
       hipLaunchKernelGGL((k_attend_few<D, NY>), dim3((unsigned)blocks), dim3(256), LDS, st, w);
@@ -1134,9 +1278,9 @@ hipError_t launch_kv_attention(const AttendArgs &given, hipStream_t st) {
     if (p.many) {
       constexpr int NY = D == 256 ? 1 : 2;
       using M = Many<D, NY>;
-      e = allow_lds(k_attend_many<D, NY>, M::LDS);
+      e = allow_lds(k_attend_many<D, NY>, M::LDS + 32);
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((k_attend_many<D, NY>), dim3((unsigned)blocks), dim3(256), M::LDS, st, w);
+      hipLaunchKernelGGL((k_attend_many<D, NY>), dim3((unsigned)blocks), dim3(256), M::LDS + 32, st, w);
       e = hipGetLastError();
     } else if (p.ny == 1) few(std::integral_constant<int, 1>{});
     else if constexpr (D < 256) few(std::integral_constant<int, 2>{});

@@ -106,6 +106,17 @@ def masks_of(b):
     return words_of([r for n, _ in b.sizes for r in ancestors(tree(rng, n))], -(-most // 64))
 
 
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("low,high", [(100, 121), (99, 101)])
+def test_scales_of_values_past_2_to_the_100(name, masked, low, high):
+    b, q = call(name, 101)
+    g = gen(102)
+    size = torch.randint(low, high, b.scale[1].shape, generator=g).float()
+    b.scale[1] = torch.exp2(size) * (1 + torch.rand(size.shape, generator=g)) / 2
+    check(b, q.to(BF16), masks_of(b) if masked else None)
+
+
 @pytest.mark.parametrize("name", list(CALLS))
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("power", [105, 125])
@@ -151,3 +162,26 @@ def test_no_scale_gives_the_mean_whatever_the_keys_are(name, power):
     b, q = call(name, 107)
     b.scale[0] *= 2.0 ** power
     check(b, q.to(BF16), scale=0.0)
+
+
+def test_what_is_written_may_be_as_large_as_its_type():
+    """Keys and values of a bfloat16's largest, written, read and attended."""
+    b = Batch([(5, 200), (200, 200)], 2, 128, 16, seed=111)
+    top = torch.finfo(BF16).max
+    (v, vc), (k, kc) = packed(b.rows, [2, 2], 128, F32, 112)
+    v = (v.clamp(-3, 3) / 3 * top).to(BF16)
+    k = k.to(BF16)
+    where = b.cuda()
+    R.kv_write(k.cuda(), v.cuda(), *where)
+    got = R.kv_read(*where, b.rows, F32)[1].cpu()
+    # half a step, and three roundings to 32 bits: the scale, the quotient, the product
+    most = v.to(D).abs().amax(2, keepdim=True)
+    assert ((got.to(D) - v.to(D)).abs() <= most * (1 / 254 + 4 * E)).all()
+    b.q8 = [t.cpu() for t in where[0][:2]]
+    b.scale = [t.cpu() for t in where[0][2:]]
+    q = torch.randn((b.rows, 4, 128), generator=gen(113)).to(BF16)
+    out, lse = R.kv_attention(q.cuda(), *where)
+    o, z, bo, bl = attend64(b, q, None, 128 ** -0.5)
+    within(lse, z, bl)
+    within(out, o, bo)
+    assert torch.isfinite(out).all()
