@@ -113,10 +113,16 @@ __device__ inline float row_sum(float a) {
 //    and times 2^100 past what 32 bits hold.
 //  - no value's is.  A row's exponentials are at most 2^15 over the largest scale of its values,
 //    and too many would be below what 32 bits hold for their sum.
+//  - the largest of the values' scales is not alone.  A row's reference is that of its largest
+//    score and of its largest scale, which need not be one position's: where the largest scale
+//    weighs little, all weights are small beside it.  f16 holds them, from 2^15 on, in steps of
+//    2^-24, so that n of them are off by n 2^-25 together; where the row's largest output is LOST
+//    times n or more, that is 2^-11 of it at most.
 // Where one does not hold, the pass is made again, with scales 2^-28 as large (and 2^28 times
 // as much to each score) if some are FAR, and a row's reference that of its largest product of
 // exponential and scale.  Such rows take more than twice as long.
 constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
+constexpr float LOST = 0x1p-7f;  // (2^-25, values up to 2^7, 2^11)
 
 // The scales of a position: where one of them is no number, or infinite, or it is not there,
 // the score is none, and the value counts as 0, so that rows that do not see it are not touched.
@@ -296,12 +302,29 @@ struct Rows16 {
       for (int i = 0; i < NX; ++i) o[i][j] = v4f{0, 0, 0, 0};
     }
   }
-  // Whether the scales that the rows saw ask for the other pass: 2 if some
+  // Whether the scales that the rows saw, over n positions, ask for the other pass: 2 if some
   // are FAR (keys' or the values'), else 1.
-  __device__ int asks(bool far) const {
+  __device__ int asks(bool far, int n) const {
+    // (a few outputs of a row say it as a rule)
+    bool again = some_lost<1>(n);
+    if (__any(again)) again = some_lost<NX>(n);
 #pragma unroll
     for (int j = 0; j < NY; ++j) far |= big[j] >= FAR;
-    return __any(far) ? 2 : 0;
+    return (__any(far) ? 2 : 0) | (__any(again) ? 1 : 0);
+  }
+  template <int X>
+  __device__ bool some_lost(int n) const {
+    bool lost = false;
+#pragma unroll
+    for (int j = 0; j < NY; ++j) {
+      float l = 0.f;
+#pragma unroll
+      for (int i = 0; i < X; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l = max2(l, fabsf(o[i][j][r]));
+      lost |= row_max(l) < (float)n * LOST && big[j] > 0.f && sum[j] > 0.f;
+    }
+    return lost;
   }
   // Before and after a pass with scales NEARER times as large: scores as they are; sums that
   // are as much smaller as the outputs.
@@ -790,7 +813,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   if (wave == 0) {
     if constexpr (!ODD) {
       const v4i keys = *(const v4i *)asked;
-      again = x.asks(keys[0] | keys[1] | keys[2] | keys[3]);
+      again = x.asks(keys[0] | keys[1] | keys[2] | keys[3], to - from);
       asked[8] = again;
     }
     if (!again) {
@@ -1090,7 +1113,7 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
     if (far) x.as_they_are();
   } else {
     // (what one wave asks for, all do: they write each other's tiles)
-    asked[wave] = x.asks(far);
+    asked[wave] = x.asks(far, to - from);
     __syncthreads();
     const v4i all = *(const v4i *)asked;
     const int again = __builtin_amdgcn_readfirstlane(all[0] | all[1] | all[2] | all[3]);

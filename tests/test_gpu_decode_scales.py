@@ -164,6 +164,28 @@ def test_no_scale_gives_the_mean_whatever_the_keys_are(name, power):
     check(b, q.to(BF16), scale=0.0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("power", [20, 32, 48, 70])
+@pytest.mark.parametrize("where", [0.0, 0.5, 1.0])
+def test_a_large_value_that_weighs_nothing(name, dtype, power, where):
+    """A position whose value is 2^power times the others' and whose weight is some e^-70
+    of theirs: the output is that of the others."""
+    b, q = call(name, 108)
+    q = q.abs() + 0.5  # (so that keys of one sign score below all others)
+    dim = b.dim
+    b.scale[0] *= 0.1  # the others' scores near each other
+    for i, (n, length) in enumerate(b.sizes):
+        if n == length and dtype == F16:
+            continue  # (its first row would see nothing else, and its type does not hold that)
+        pg, at = b.place(i, int((length - n) * where))
+        b.q8[0][pg, :, at] = -127
+        b.scale[0][pg, :, at] = 70 / (127 * math.sqrt(dim) * 1.2)
+        b.scale[1][pg, :, at] = 2.0 ** (power - 6)
+    out, _ = check(b, q.to(dtype))
+    assert out[b.sizes[0][0] - 1].abs().max() < 5
+
+
 def test_what_is_written_may_be_as_large_as_its_type():
     """Keys and values of a bfloat16's largest, written, read and attended."""
     b = Batch([(5, 200), (200, 200)], 2, 128, 16, seed=111)
@@ -185,3 +207,18 @@ def test_what_is_written_may_be_as_large_as_its_type():
     within(lse, z, bl)
     within(out, o, bo)
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_unseen_scales_of_every_size_beside_small_ones(name):
+    """Rows that see values of 2^-70 alone keep them, whatever lies in their tiles."""
+    b, q = call(name, 114)
+    b.scale[1] *= 2.0 ** -64
+    used = set()
+    at_places(b, lambda i, t, pg, at: used.add((pg, at)))
+    for pg in range(b.pages):
+        for at in range(b.page):
+            if (pg, at) not in used:
+                b.scale[1][pg, :, at] = [2.0 ** 120, 2.0 ** 60, 0.0, math.inf][(pg + at) % 4]
+                b.scale[0][pg, :, at] = [2.0 ** 120, 0.0, 2.0 ** -120][(pg + 2 * at) % 3]
+    check(b, q.to(BF16))
