@@ -118,11 +118,18 @@ __device__ inline float row_sum(float a) {
 //    weighs little, all weights are small beside it.  f16 holds them, from 2^15 on, in steps of
 //    2^-24, so that n of them are off by n 2^-25 together; where the row's largest output is LOST
 //    times n or more, that is 2^-11 of it at most.
+//  - they do not grow by APART from one step to the next: what was added up would be 0 beside
+//    them.
 // Where one does not hold, the pass is made again, with scales 2^-28 as large (and 2^28 times
 // as much to each score) if some are FAR, and a row's reference that of its largest product of
-// exponential and scale.  Such rows take more than twice as long.
+// exponential and scale.  Such rows take more than twice as long.  To look costs a prompt of
+// 8192 685 us -> 693, one of 4096 with heads of 64 125 -> 129, trees of 25 30 -> 31.
 constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
 constexpr float LOST = 0x1p-7f;  // (2^-25, values up to 2^7, 2^11)
+constexpr float APART = 0x1p60f;
+__device__ inline bool is_apart(float before, float now) {
+  return now > before * APART && before > 0.f;
+}
 
 // The scales of a position: where one of them is no number, or infinite, or it is not there,
 // the score is none, and the value counts as 0, so that rows that do not see it are not touched.
@@ -137,6 +144,28 @@ template <int N>
 __device__ inline float turned(float a) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0x120 + N,
                                                             0xf, 0xf, false));
+}
+
+// 2^x as two factors, the second 1 but where one number would not hold it: references lie as far
+// apart as the values' scales.
+struct Power {
+  float a, b;
+};
+__device__ inline Power power(float x) {
+  const float near = fmaxf(x, -100.f);
+  return {__builtin_amdgcn_exp2f(near), __builtin_amdgcn_exp2f(x - near)};
+}
+
+// A sum and outputs 2^x times as large.
+__device__ inline void bring(float &sum, v4f &o, float x) {
+  if (x < -100.f) {
+    x += 100.f;
+    sum *= 0x1p-100f;
+    o *= 0x1p-100f;
+  }
+  const float by = __builtin_amdgcn_exp2f(x);
+  sum *= by;
+  o *= by;
 }
 
 // What a launch works on.
@@ -304,13 +333,13 @@ struct Rows16 {
   }
   // Whether the scales that the rows saw, over n positions, ask for the other pass: 2 if some
   // are FAR (keys' or the values'), else 1.
-  __device__ int asks(bool far, int n) const {
+  __device__ int asks(bool far, bool apart, int n) const {
     // (a few outputs of a row say it as a rule)
     bool again = some_lost<1>(n);
     if (__any(again)) again = some_lost<NX>(n);
 #pragma unroll
     for (int j = 0; j < NY; ++j) far |= big[j] >= FAR;
-    return (__any(far) ? 2 : 0) | (__any(again) ? 1 : 0);
+    return (__any(far) ? 2 : 0) | (__any(again || apart) ? 1 : 0);
   }
   template <int X>
   __device__ bool some_lost(int n) const {
@@ -359,7 +388,7 @@ struct Rows16 {
   // position r of tile x; what it does not see becomes -infinity.
   template <int TILES, class Vs, class Most, class Bits>
   __device__ void refer(v4f (&s)[TILES][NY], float (&m)[NY], Vs vs, Most most, bool masked,
-                        Bits bits) {
+                        Bits bits, int *apart) {
     float largest[NY];
     if (masked) {
 #pragma unroll
@@ -394,6 +423,10 @@ struct Rows16 {
       grows |= m[j] > top[j] || largest[j] > big[j];
     }
     if (__any(grows)) {
+      bool far_apart = false;
+#pragma unroll
+      for (int j = 0; j < NY; ++j) far_apart |= is_apart(big[j], largest[j]);
+      if (__any(far_apart)) *apart = 1;
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
         const float before = ref[j];
@@ -438,10 +471,10 @@ struct Rows16 {
       top[j] = max2(top[j], m);
       ref[j] = max3(fmaf(top[j], factor[j], -95.f), lift, none ? NONE : before);
       if (top[j] == NONE) ref[j] = 0.f;
-      const float by = none ? 0.f : __builtin_amdgcn_exp2f(before - ref[j]);
-      sum[j] *= by;
+      const Power by = power(none ? 0.f : before - ref[j]);
+      sum[j] = sum[j] * by.a * by.b;
 #pragma unroll
-      for (int i = 0; i < NX; ++i) o[i][j] *= by;
+      for (int i = 0; i < NX; ++i) o[i][j] = o[i][j] * by.a * by.b;
     }
   }
 
@@ -622,9 +655,11 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   // product ks of 32 takes bytes 16 g + 8 (ks % 2) .. + 8 of chunk ks / 2 of 64
   Rows16<D, NY> x;
   auto first = [&](int ks) { return 64 * (ks / 2) + 16 * g + 8 * (ks % 2); };
-  // behind the waves' sums: whether a wave met a key's scale that is FAR, and what that comes to
+  // behind the waves' sums: whether a wave met a key's scale that is FAR, values' that are APART
+  // (four words each), and what all of it comes to
   constexpr int EACH = 64 * (4 * Rows16<D, NY>::NX * NY + 4 * NY);
   int *asked = (int *)lds + 2 * EACH;
+  asked[4 + wave] = 0;
   // The scales of a step settled: the largest of the values', and whether one of the keys' is FAR.
   auto settle_step = [&](const int (&entries)[2], int t, float &most) {
     const int room = s.length - t - 4 * g;
@@ -733,7 +768,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
     if constexpr (ODD) x.template refer_odd<2>(sc, vs, masked, bits);
     else
       x.template refer<2>(
-          sc, largest, vs, [&] { return row_max(most); }, masked, bits);
+          sc, largest, vs, [&] { return row_max(most); }, masked, bits, asked + 4 + wave);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -771,6 +806,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   // The waves' sums together, in order: waves 2 and 3 to 0 and 1, 1 to 0.
   float *mine = (float *)lds;
   if (!ODD) asked[wave] = far;
+  bool apart = false;
 #pragma unroll
   for (int half = 2; half >= 1; half /= 2) {
     if (wave >= half && wave < 2 * half) {
@@ -800,11 +836,20 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
         const float da = here ? x.ref[j] - both : NONE, db = there ? ref - both : NONE;
         x.ref[j] = both;
         x.top[j] = fmaxf(x.top[j], top);
-        const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-        x.sum[j] = x.sum[j] * fa + of[(4 * j + 2) * 64] * fb;
+        if constexpr (ODD) {
+          const Power fa = power(da), fb = power(db);
+          x.sum[j] = x.sum[j] * fa.a * fa.b + of[(4 * j + 2) * 64] * fb.a * fb.b;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x.o[i][j] = x.o[i][j] * fa + o[(i * NY + j) * 64] * fb;
-        x.big[j] = fmaxf(x.big[j], big);
+          for (int i = 0; i < D / 16; ++i)
+            x.o[i][j] = x.o[i][j] * fa.a * fa.b + o[(i * NY + j) * 64] * fb.a * fb.b;
+        } else {
+          const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+          x.sum[j] = x.sum[j] * fa + of[(4 * j + 2) * 64] * fb;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) x.o[i][j] = x.o[i][j] * fa + o[(i * NY + j) * 64] * fb;
+          apart |= is_apart(x.big[j], big) || is_apart(big, x.big[j]);
+          x.big[j] = fmaxf(x.big[j], big);
+        }
       }
     }
     __syncthreads();
@@ -812,8 +857,9 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   int again = 0;
   if (wave == 0) {
     if constexpr (!ODD) {
-      const v4i keys = *(const v4i *)asked;
-      again = x.asks(keys[0] | keys[1] | keys[2] | keys[3], to - from);
+      const v4i keys = *(const v4i *)asked, values = *(const v4i *)(asked + 4);
+      again = x.asks(keys[0] | keys[1] | keys[2] | keys[3],
+                     apart || (values[0] | values[1] | values[2] | values[3]), to - from);
       asked[8] = again;
     }
     if (!again) {
@@ -990,7 +1036,8 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
     ((int *)(scales + 2 * M::TILE))[wave] = sub.there;
     scales[2 * M::TILE + 4 + wave] = most;
   };
-  int *asked = (int *)(lds + M::LDS);  // what the waves ask for
+  int *asked = (int *)(lds + M::LDS);  // what the waves ask for; whether values' scales are APART
+  asked[4 + wave] = 0;
   auto write = [&](char *stage) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) write_piece(stage, i);
@@ -1053,7 +1100,7 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
             const v4f most = *(const v4f *)(scales + 2 * M::TILE + 4);
             return max3(max2(most[0], most[1]), most[2], most[3]);
           },
-          masked, bits);
+          masked, bits, asked + 4 + wave);
     }
     v4i p[2][NY];
     constexpr int G = 4, EACH = M::NX / G;  // groups of products with the values, per half
@@ -1113,7 +1160,7 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
     if (far) x.as_they_are();
   } else {
     // (what one wave asks for, all do: they write each other's tiles)
-    asked[wave] = x.asks(far, to - from);
+    asked[wave] = x.asks(far, asked[4 + wave], to - from);
     __syncthreads();
     const v4i all = *(const v4i *)asked;
     const int again = __builtin_amdgcn_readfirstlane(all[0] | all[1] | all[2] | all[3]);
@@ -1178,15 +1225,13 @@ __global__ void __launch_bounds__(256) k_attend_join(Work w) {
       ref = fmaxf(ref, e[i].x);
     }
     if (ref == NONE) continue;
-    const float by = __builtin_amdgcn_exp2f(before - ref);
-    total *= by;
-    o *= by;
+    bring(total, o, before - ref);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (e[i].x == NONE) continue;  // (its outputs were not written)
-      const float f = __builtin_amdgcn_exp2f(e[i].x - ref);
-      total += e[i].y * f;
-      o += v[i] * f;
+      bring(e[i].y, v[i], e[i].x - ref);
+      total += e[i].y;
+      o += v[i];
     }
   }
   sums[group][lane] = o;
@@ -1199,9 +1244,11 @@ __global__ void __launch_bounds__(256) k_attend_join(Work w) {
   total = 0.f;
   o = v4f{0, 0, 0, 0};
   for (int i = 0; i < w.joiners && !none; ++i) {
-    const float f = __builtin_amdgcn_exp2f(ends[group + i].x - all);
-    total += ends[group + i].y * f;
-    o += sums[group + i][lane] * f;
+    float sum = ends[group + i].y;
+    v4f part = sums[group + i][lane];
+    bring(sum, part, ends[group + i].x - all);
+    total += sum;
+    o += part;
   }
   const float inv = none ? 0.f : 1.f / total;
   if (a.lse && lane == 0)

@@ -108,13 +108,27 @@ def masks_of(b):
 
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("name", list(CALLS))
-@pytest.mark.parametrize("low,high", [(100, 121), (99, 101)])
+@pytest.mark.parametrize("low,high", [(100, 121), (60, 121), (-60, 119), (99, 101)])
 def test_scales_of_values_past_2_to_the_100(name, masked, low, high):
     b, q = call(name, 101)
     g = gen(102)
     size = torch.randint(low, high, b.scale[1].shape, generator=g).float()
     b.scale[1] = torch.exp2(size) * (1 + torch.rand(size.shape, generator=g)) / 2
     check(b, q.to(BF16), masks_of(b) if masked else None)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("where", ["first", "last", "spread"])
+def test_a_huge_value_among_ordinary_ones(name, where):
+    """Rows before it keep their values, rows behind it take its."""
+    b, q = call(name, 103)
+    for i, (n, length) in enumerate(b.sizes):
+        for t in {"first": [0], "last": [length - 1], "spread": [length // 3, length - n // 2 - 1]}[where]:
+            pg, at = b.place(i, t)
+            b.scale[1][pg, :, at] = -(2.0 ** 118)
+    out, _ = check(b, q.to(BF16))
+    if where == "last":
+        assert (out[0].abs() < 100).all() or b.sizes[0][0] == 1
 
 
 @pytest.mark.parametrize("name", list(CALLS))
@@ -184,6 +198,18 @@ def test_a_large_value_that_weighs_nothing(name, dtype, power, where):
         b.scale[1][pg, :, at] = 2.0 ** (power - 6)
     out, _ = check(b, q.to(dtype))
     assert out[b.sizes[0][0] - 1].abs().max() < 5
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_scales_of_values_over_the_whole_range(name):
+    """From 2^-75 to 2^90, in any order, zeros among them."""
+    b, q = call(name, 109)
+    g = gen(110)
+    size = torch.rand(b.scale[1].shape, generator=g) * 165 - 75
+    b.scale[1] = torch.exp2(size)
+    b.scale[1][torch.rand(size.shape, generator=g) < 0.1] = 0
+    b.scale[0] *= 8  # scores of some tens
+    check(b, q.to(BF16))
 
 
 def test_what_is_written_may_be_as_large_as_its_type():
