@@ -739,7 +739,8 @@ size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, s
 
 /* The cache: k and v [pages][kv_heads][page][dim] and their scales
  * [pages][kv_heads][page], each with the strides given, in elements (so pages of
- * places of heads, or keys and values in one buffer, will do too).  A head's `dim`
+ * places of heads, or keys and values in one buffer, in turn by page, head, place or
+ * row, will do too).  A head's `dim`
  * values, and a page's scales of a head, are contiguous.  value = scale * q, as
  * for the clear side's 8-bit rows, a row being one head of one position.
  * dim: a multiple of 16 up to 256; page: a power of two from 16 on; table_len *

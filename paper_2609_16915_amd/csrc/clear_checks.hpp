@@ -40,27 +40,55 @@ inline rosetta_status done(hipError_t e, const char *what) {
 
 inline bool is_type(int t) { return t == ROSETTA_F32 || t == ROSETTA_BF16 || t == ROSETTA_F16; }
 
-// A named device array: rows of `len` elements of `elem` bytes, `stride` apart.
+// A named device array: rows of `len` elements of `elem` bytes, `stride` apart.  A row may be
+// runs with others' elements between them: inner[0].n runs of inner[0].len elements,
+// inner[0].stride apart, and each of those inner[1].n of inner[1].len (n = 0: all its own).
+struct Runs {
+  size_t n, len, stride;
+};
 struct Array {
   const char *name;
   const void *p;
   size_t rows, len, stride, elem;
   bool out;
+  Runs inner[2] = {};
   // (past 64 bits where a caller's sizes are: 2^31 rows 2^32 elements apart)
   unsigned __int128 bytes() const {
     return rows && len ? ((unsigned __int128)(rows - 1) * stride + len) * elem : 0;
   }
+  // Level `at`, from the rows on: its parts, their length and distance in elements.
+  static constexpr int LEVELS = 3;
+  Runs level(int at) const {
+    if (at == 0) return {rows, len, stride};
+    return at < LEVELS && inner[at - 1].n ? inner[at - 1] : Runs{0, 0, 0};
+  }
 };
 
-// Whether two arrays share memory: by the whole ranges, or, rows as far apart in both
-// (columns of one buffer), by where the second's rows lie between the first's.
+// Whether two arrays share memory, from level ia of a and ib of b on, which are ea and eb bytes
+// long, b's `by` bytes behind a's: by the whole ranges, or, parts as far apart in both (columns
+// of one buffer), by the parts themselves.  Parts lie within their distance, so that one of a
+// meets two of b at most: those that start before it and behind.
+inline bool overlap_from(const Array &a, int ia, __int128 ea, const Array &b, int ib, __int128 eb,
+                         __int128 by) {
+  if (by >= ea || -by >= eb) return false;
+  const Runs x = a.level(ia), y = b.level(ib);
+  const __int128 ex = (__int128)x.len * a.elem, ey = (__int128)y.len * b.elem;
+  if (x.n == 1) return overlap_from(a, ia + 1, ex, b, ib, eb, by);
+  if (y.n == 1) return overlap_from(a, ia, ea, b, ib + 1, ey, by);
+  const __int128 pitch = (__int128)x.stride * a.elem;
+  if (!x.n || !y.n || pitch != (__int128)y.stride * b.elem) return true;
+  // part i of a and i + k of b
+  __int128 k = -by / pitch;
+  if (by + k * pitch > 0) --k;
+  for (int two = 0; two < 2; ++two, ++k)
+    if (k > -(__int128)x.n && k < (__int128)y.n &&
+        overlap_from(a, ia + 1, ex, b, ib + 1, ey, by + k * pitch))
+      return true;
+  return false;
+}
 inline bool overlap(const Array &a, const Array &b) {
-  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  if (!(x < y + b.bytes() && y < x + a.bytes())) return false;
-  const size_t pitch = a.stride * a.elem;
-  if (a.rows < 2 || b.rows < 2 || pitch != b.stride * b.elem) return true;
-  const size_t at = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;
-  return at < a.len * a.elem || at + b.len * b.elem > pitch;
+  return overlap_from(a, 0, a.bytes(), b, 0, b.bytes(),
+                      (__int128)(uintptr_t)b.p - (__int128)(uintptr_t)a.p);
 }
 
 inline rosetta_status check_strides(std::initializer_list<Array> as) {

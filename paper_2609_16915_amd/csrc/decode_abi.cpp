@@ -32,7 +32,7 @@ bool as_rows(Array &r, const char *name, const void *p, size_t n0, size_t s0, si
   const size_t len = n1 ? (n1 - 1) * s1 + dim : 0;
   if (n0 <= 1) s0 = len;
   if (s0 < len || (n0 > 1 && s0 > MAX_STRIDE)) return false;
-  r = Array{name, p, n0, len, s0, elem, out};
+  r = Array{name, p, n0, len, s0, elem, out, {Runs{n1, dim, s1}}};
   return true;
 }
 
@@ -83,7 +83,8 @@ rosetta_status check_given(const rosetta_kv_cache *c, const rosetta_kv_rows *r, 
                c->scale_head_stride, c->page, 4, out))
     return fail(ROSETTA_ERR_PARAMS, "cache: scale strides of %zu and %zu", c->scale_page_stride,
                 c->scale_head_stride);
-  g.k = Array{"cache k", c->k, c->pages, extent, page_stride, 1, out};
+  g.k = Array{"cache k", c->k, c->pages, extent, page_stride, 1, out,
+              {Runs{inner.rows, inner.len, inner.stride}, inner.inner[0]}};
   g.v = g.k;
   g.v.name = "cache v";
   g.v.p = c->v;
