@@ -1152,9 +1152,12 @@ def kv_attention(q, cache, table, starts, lens, masks=None, scale: float = None,
     the rows' own entries among it: row i of a sequence sees the positions before its
     rows, and its rows up to i, or with `masks` (int64 [rows][words], as tree_masks
     makes them) those whose bit is set.  A row that sees nothing gives zeros and -inf.
-    scale: 1 / sqrt(dim) where not given.  max_rows: the most rows of any sequence (all
-    rows, where not given; fewer leave less to launch).  lse is float32 [rows][heads], or
-    None.  Rows of no sequence, or behind max_rows, are not written."""
+    scale: 1 / sqrt(dim) where not given.  max_rows: the most rows of any sequence (where
+    not given all rows, or with masks as many as they have bits for; a batch of single
+    tokens that names 1 leaves less to launch).  A table that is longer than the longest
+    sequence (a narrower view of it will do) is cut in more parts than there is to do.  lse
+    is float32 [rows][heads], or None.  Rows of no sequence, or behind max_rows, are not
+    written."""
     torch = _torch()
     c, on = _cache(cache)
     if not isinstance(q, _tensor_class()):
@@ -1165,16 +1168,18 @@ def kv_attention(q, cache, table, starts, lens, masks=None, scale: float = None,
     shape = (rows, heads, c.dim)
     qa = _heads(q, "q", dtype, shape, on)
     r = _rows(table, starts, lens, rows, on)
-    max_rows = rows if max_rows is None else min(max_rows, rows)
-    if max_rows < 0:
-        raise ValueError("max_rows must not be negative")
-    if scale is None:
-        scale = c.dim ** -0.5
     mp, words = None, 0
     if masks is not None:
         size, _ = _tensor(masks, "masks", torch.int64, 2, on)
         words = size[1]
         mp = _vec(masks, "masks", torch.int64, rows * words, on)
+    if max_rows is None:
+        max_rows = min(rows, 64 * max(words, 1)) if masks is not None else rows
+    max_rows = min(max_rows, rows)
+    if max_rows < 0:
+        raise ValueError("max_rows must not be negative")
+    if scale is None:
+        scale = c.dim ** -0.5
     L = lib()
     need = L.rosetta_kv_attention_workspace_bytes(heads, c.kv_heads, c.dim, r.batch, rows, max_rows,
                                                   r.table_len * c.page)
@@ -1194,9 +1199,9 @@ def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=
     """(tokens, path, count): drafted tokens verified against the target's probabilities.
     p, q [rows][vocab] (of one type): the target's after each row, and those that the
     row's children were drawn from (anything, where it has none); drafts int64 [rows] the
-    tokens, u float32 [rows] numbers of [0, 1).  A sequence's rows are the nodes of a tree whose node 0 is the
-    last certain token; parents int32 [rows] as for tree_masks (None: each follows the
-    one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
+    tokens, u float32 [rows] numbers of [0, 1).  A sequence's rows are the nodes of a tree
+    whose node 0 is the last certain token; parents int32 [rows] as for tree_masks (None:
+    each follows the one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
     how many new tokens there are; path int32 and tokens int64 [rows]: those, from each
     sequence's first row on, -1 behind."""
     torch = _torch()
