@@ -789,7 +789,7 @@ rosetta_status rosetta_kv_keep(const rosetta_kv_cache *cache, const rosetta_kv_r
  * masks [rows][words] says whether row i is row j or has it among its ancestors.
  * parents [rows]: the place, among its sequence's rows, of each row's parent,
  * which lies before it; anything else is no parent.  Rows j >= 64 words have no
- * bit; rows of no sequence get none. */
+ * bit; rows of no sequence get none (where batch is 0, nothing is written). */
 rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts, size_t batch,
                                   size_t rows, size_t words, uint64_t *masks, void *stream);
 
@@ -843,7 +843,7 @@ size_t rosetta_kv_attention_workspace_bytes(size_t heads, size_t kv_heads, size_
  *   count[b]: the nodes kept, node 0 among them, and as many new tokens (0 for a
  *   sequence without rows); path, tokens [rows]: those nodes, and those tokens, from
  *   the sequence's first row on, -1 behind (and before the first sequence and behind
- *   the last).
+ *   the last; where batch is 0, nothing is written).
  * workspace: rosetta_verify_drafts_workspace_bytes bytes, on 8 bytes. */
 rosetta_status rosetta_verify_drafts(const void *p, size_t p_stride, const void *q, size_t q_stride,
                                      int dtype, const int64_t *drafts, const int32_t *parents,

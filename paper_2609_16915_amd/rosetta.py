@@ -1139,6 +1139,8 @@ def tree_masks(parents, starts, max_rows: int, stream=None):
     sp = _vec(starts, "starts", torch.int32, batch + 1, on)
     words = -(-max_rows // 64)
     masks = parents.new_empty((rows, words), dtype=torch.int64)
+    if batch == 0:  # (the library then does nothing)
+        masks.zero_()
     _check(lib().rosetta_tree_masks(pp, sp, batch, rows, words, masks.data_ptr(),
                                     _stream_of(parents, stream)))
     return masks
@@ -1203,7 +1205,7 @@ def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=
     whose node 0 is the last certain token; parents int32 [rows] as for tree_masks (None:
     each follows the one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
     how many new tokens there are; path int32 and tokens int64 [rows]: those, from each
-    sequence's first row on, -1 behind."""
+    sequence's first row on, -1 behind, and in rows of no sequence."""
     torch = _torch()
     pp, ps, rows, vocab = _mat(p, "p")
     dtype, on = p.dtype, p.get_device()
@@ -1223,6 +1225,9 @@ def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=
     tokens = drafts.new_empty(rows)
     path = starts.new_empty(rows)
     count = starts.new_empty(batch)
+    if batch == 0:  # (the library then does nothing)
+        tokens.fill_(-1)
+        path.fill_(-1)
     _check(L.rosetta_verify_drafts(pp, ps, qp, qs, _type(dtype, "p"), dp, ap, up, sp, batch, rows,
                                    vocab, tokens.data_ptr(), path.data_ptr(), count.data_ptr(), wp,
                                    wb, _stream_of(p, stream)))

@@ -56,3 +56,14 @@ def test_without_masks_all_rows(given):
     q = on(torch.zeros((528, 1, 64), dtype=torch.bfloat16))
     R.kv_attention(q, cache(), on(torch.zeros((1, 2), dtype=torch.int32)), ints(0, 528), ints(600))
     assert given["rosetta_kv_attention"][MAX_ROWS] == 528
+
+
+def test_nothing_verified_and_no_masks_where_there_is_no_sequence(given, monkeypatch):
+    """Rows of no sequence hold -1, and no bits, where there is no sequence at all."""
+    monkeypatch.setattr(OnDevice, "new_empty", lambda self, shape, dtype=None: on(
+        torch.full(shape if isinstance(shape, tuple) else (shape,), 7, dtype=dtype or self.dtype)))
+    p = on(torch.zeros((3, 9)))
+    tokens, path, count = R.verify_drafts(p, p, on(torch.zeros(3).long()), on(torch.zeros(3)), ints(0))
+    assert tokens.tolist() == [-1] * 3 and path.tolist() == [-1] * 3 and count.numel() == 0
+    assert tokens.dtype is torch.int64 and path.dtype is torch.int32
+    assert R.tree_masks(ints(-1, 0, 1), ints(0), 70).tolist() == [[0, 0]] * 3

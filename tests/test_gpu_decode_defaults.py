@@ -30,3 +30,17 @@ def test_trees_with_more_rows_together_than_a_mask_has_bits():
     o, z, bo, bl = attend64(b, q, masks.cpu(), 0.125)
     within(out, o, bo)
     within(lse, z, bl)
+
+
+def test_no_sequence_at_all():
+    """A batch that is all padding: starts of one element, and starts without rows."""
+    p = torch.rand((9, 50), device="cuda")
+    drafts, u = torch.zeros(9, device="cuda").long(), torch.zeros(9, device="cuda")
+    parents = ints([-1] + list(range(8))).cuda()
+    for starts in ([0], [0, 0, 0]):
+        junk = [torch.full((9,), 7, dtype=t, device="cuda") for t in (torch.int64, torch.int32) * 4]
+        del junk  # (so that new tensors hold 7)
+        s = ints(starts).cuda()
+        tokens, path, count = R.verify_drafts(p, p, drafts, u, s, parents=parents)
+        assert (tokens == -1).all() and (path == -1).all() and count.tolist() == [0] * (len(starts) - 1)
+        assert not R.tree_masks(parents, s, 9).any()
