@@ -327,10 +327,10 @@ __global__ void __launch_bounds__(TEAM) k_verify_end(Job j) {
       }
       return v_last;
     };
-    if (excl <= aim && incl > aim) {
-      const int v = some(excl);
-      if (v >= 0) atomicMin(&found, v);
-    }
+    // (of each wave the first thread with any weight that gets past the aim: sums in another
+    // order may pass it at a word without weight, by their last bit)
+    const uint64_t past = __ballot(mine > 0 && incl > aim);
+    if (past && lane == __builtin_ctzll(past)) atomicMin(&found, some(excl));
     __syncthreads();
     if (found == 0x7fffffff) {  // (the same in every thread)
       const int v = mine > 0 ? some(-__builtin_inf()) : -1;

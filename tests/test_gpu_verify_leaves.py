@@ -74,3 +74,16 @@ def test_nothing_left_is_drawn_from_p_whatever_q_holds():
     u[1] = u[3] = 0.9999
     drafts[:] = 5
     assert verify(p, q, drafts, u, starts, None) == verify64(p, q, drafts, u, starts, None)
+
+
+@pytest.mark.parametrize("shift", [0, 64, 256])
+def test_a_draw_on_a_border_next_to_words_without_weight(shift):
+    """1, then words of 2^-53 among words of 0: partial sums differ by their order in the last
+    bit, and a draw that is exactly 1 lies between two of them, at a word of weight 0.  What
+    follows is the next word that has any, not the last of all."""
+    p = torch.zeros((1, 600))
+    for at, w in ((0, 1.0), (1, 2.0 ** -53), (3, 2.0 ** -53), (13, 1.0), (150, 1.0), (199, 1.0)):
+        p[0, shift + at] = w
+    u = torch.tensor([0.25])  # of 4
+    tokens, path, count = verify(p, p, torch.zeros(1).long(), u, [0, 1], None)
+    assert tokens[0] - shift in (1, 3, 13) and path == [0] and count == [1]
