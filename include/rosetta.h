@@ -719,7 +719,7 @@ size_t rosetta_cross_entropy_backward_workspace_bytes(size_t rows, size_t dim, s
  * What a decode in the clear needs around its layers: keys and values kept in 8
  * bits, attention that reads them, and several tokens drafted for one step and
  * verified against the model's probabilities.  (How many of a table's drafts the
- * exact model accepts is a measure of the table: 1 - total variation a token.)
+ * exact model accepts is a measure of the table: of one draft 1 - total variation.)
  *
  * CONVENTIONS, beside those of the clear side above:
  *  - A batch is packed: sequence b has rows starts[b] .. starts[b + 1] - 1 of the
@@ -813,7 +813,8 @@ rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts,
  * gives next to no weight to values with scales far above the others', take twice as
  * long and more.  workspace:
  * rosetta_kv_attention_workspace_bytes bytes (0 where parts of a sequence need no
- * joining), positions being table_len * page. */
+ * joining), positions being table_len * page: that, not lens, says how many parts each
+ * sequence is cut in. */
 rosetta_status rosetta_kv_attention(const void *q, size_t q_row_stride, size_t q_head_stride,
                                     int dtype, size_t heads, const rosetta_kv_cache *cache,
                                     const rosetta_kv_rows *rows, size_t max_rows,

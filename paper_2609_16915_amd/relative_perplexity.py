@@ -20,9 +20,10 @@ values
 
 and with --drafts the model with the table then drafts tokens, that many one after
 the other and a second choice for each, which the exact model verifies in one pass a
-step: the share that it accepts is another measure of the table (1 - total
-variation, a token).  Weights and inputs are synthetic and seeded; targets are drawn
-from the exact model's own distribution, so that its perplexity means something.
+step: how many it accepts is another measure of the table (of one draft a token it
+would be 1 - total variation; the second choices add to that).  Weights and inputs are
+synthetic and seeded; targets are drawn from the exact model's own distribution, so
+that its perplexity means something.
 """
 from __future__ import annotations
 
