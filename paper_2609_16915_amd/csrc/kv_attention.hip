@@ -122,8 +122,9 @@ __device__ inline float row_sum(float a) {
 //    them.
 // Where one does not hold, the pass is made again, with scales 2^-28 as large (and 2^28 times
 // as much to each score) if some are FAR, and a row's reference that of its largest product of
-// exponential and scale.  Such rows take more than twice as long.  To look costs a prompt of
-// 8192 685 us -> 693, one of 4096 with heads of 64 125 -> 129, trees of 25 30 -> 31.
+// exponential and scale, which takes twice as long together.  To look costs a prompt of 8192
+// 688 us -> 697, one of 4096 with heads of 64 125 -> 130, of 256 328 -> 343, trees of 25 30.5
+// -> 31.6, 64 tokens 134.2 -> 134.7.
 constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
 constexpr float LOST = 0x1p-7f;  // (2^-25, values up to 2^7, 2^11)
 constexpr float APART = 0x1p60f;
@@ -875,7 +876,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
 }
 
 // (A function of its own: beside the first pass its registers cost that 10 %, on heads of 64.
-// The scratch memory that the compiler reports is what it saves of the kernel's.)
+// The scratch memory that the compiler reports is where it saves the kernel's registers.)
 template <int D, int NY>
 __device__ __attribute__((noinline)) void
 attend_few_odd(const Work *w, __attribute__((address_space(3))) char *lds, bool far) {

@@ -1203,9 +1203,9 @@ def verify_drafts(p, q, drafts, u, starts, parents=None, workspace=None, stream=
     row's children were drawn from (anything, where it has none); drafts int64 [rows] the
     tokens, u float32 [rows] numbers of [0, 1).  A sequence's rows are the nodes of a tree
     whose node 0 is the last certain token; parents int32 [rows] as for tree_masks (None:
-    each follows the one before).  count int32 [batch]: how many nodes are kept, node 0 among them, and
-    how many new tokens there are; path int32 and tokens int64 [rows]: those, from each
-    sequence's first row on, -1 behind, and in rows of no sequence."""
+    each follows the one before).  count int32 [batch]: how many nodes are kept, node 0
+    among them, and how many new tokens there are; path int32 and tokens int64 [rows]:
+    those, from each sequence's first row on, -1 behind, and in rows of no sequence."""
     torch = _torch()
     pp, ps, rows, vocab = _mat(p, "p")
     dtype, on = p.dtype, p.get_device()
