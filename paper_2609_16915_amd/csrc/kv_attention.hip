@@ -807,7 +807,6 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   // The waves' sums together, in order: waves 2 and 3 to 0 and 1, 1 to 0.
   float *mine = (float *)lds;
   if (!ODD) asked[wave] = far;
-  bool apart = false;
 #pragma unroll
   for (int half = 2; half >= 1; half /= 2) {
     if (wave >= half && wave < 2 * half) {
@@ -829,6 +828,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
     if (wave < half) {
       const float *of = mine + wave * EACH + lane;
       const v4f *o = (const v4f *)(mine + wave * EACH + 4 * NY * 64) + lane;
+      bool apart = false;
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
         const float top = of[(4 * j) * 64], ref = of[(4 * j + 1) * 64], big = of[(4 * j + 3) * 64];
@@ -852,6 +852,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
           x.big[j] = fmaxf(x.big[j], big);
         }
       }
+      if (!ODD && __any(apart)) asked[4 + wave] = 1;
     }
     __syncthreads();
   }
@@ -860,7 +861,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
     if constexpr (!ODD) {
       const v4i keys = *(const v4i *)asked, values = *(const v4i *)(asked + 4);
       again = x.asks(keys[0] | keys[1] | keys[2] | keys[3],
-                     apart || (values[0] | values[1] | values[2] | values[3]), to - from);
+                     values[0] | values[1] | values[2] | values[3], to - from);
       asked[8] = again;
     }
     if (!again) {

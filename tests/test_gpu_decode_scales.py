@@ -248,3 +248,16 @@ def test_unseen_scales_of_every_size_beside_small_ones(name):
                 b.scale[1][pg, :, at] = [2.0 ** 120, 2.0 ** 60, 0.0, math.inf][(pg + at) % 4]
                 b.scale[0][pg, :, at] = [2.0 ** 120, 0.0, 2.0 ** -120][(pg + 2 * at) % 3]
     check(b, q.to(BF16))
+
+
+@pytest.mark.parametrize("small", range(4))
+@pytest.mark.parametrize("heads,dim", [(2, 64), (20, 64), (4, 128), (3, 256)])
+def test_thirty_two_positions_of_small_values_among_large_ones(heads, dim, small):
+    """What one wave of four goes through has scales 2^148 below the others', whichever it is:
+    its exponentials count in every row's sum."""
+    b = Batch([(1, 128)], 1, dim, 16, seed=117)
+    for t in range(128):
+        pg, at = b.place(0, t)
+        b.scale[1][pg, :, at] *= 2.0 ** -58 if t // 32 == small else 2.0 ** 90
+    q = torch.randn((1, heads, dim), generator=gen(118)).to(BF16)
+    check(b, q)
