@@ -807,11 +807,11 @@ rosetta_status rosetta_tree_masks(const int32_t *parents, const int32_t *starts,
  * max_rows: no sequence has more rows (those behind are left as they were; with
  * masks, max_rows <= 64 words).  Scores, statistics and sums are 32-bit; the weights
  * of the values are rounded to f16 with 2^15 for the largest possible (scales of
- * values from 2^-80 on keep their precision).  Scales may be of any size; where a
- * sequence has some of 2^100 and more, its rows of q must lie below 2^100, and values'
- * scales keep their precision from 2^-52 on.  Such sequences, and those in which a row
- * gives next to no weight to values with scales far above the others', take twice as
- * long and more.  workspace:
+ * values from 2^-80 on keep their precision).  Scales may be of any size: where a
+ * sequence has some of 2^100 and more, of keys, its rows of q must lie below 2^100, and of
+ * values, the others keep their precision from 2^-52 on.  Such sequences, and those in
+ * which a row gives next to no weight to values with scales far above the others', take
+ * twice as long.  workspace:
  * rosetta_kv_attention_workspace_bytes bytes (0 where parts of a sequence need no
  * joining), positions being table_len * page: that, not lens, says how many parts each
  * sequence is cut in. */

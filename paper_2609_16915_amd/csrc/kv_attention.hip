@@ -120,12 +120,13 @@ __device__ inline float row_sum(float a) {
 //    times n or more, that is 2^-11 of it at most.
 //  - they do not grow by APART from one step to the next: what was added up would be 0 beside
 //    them.
-// Where one does not hold, the pass is made again, with scales 2^-28 as large (and 2^28 times
-// as much to each score) if some are FAR, and a row's reference that of its largest product of
-// exponential and scale, which takes twice as long together.  To look costs a prompt of 8192
+// Where one does not hold, the pass is made again, with keys' scales 2^-28 as large (and 2^28
+// times as much to each score) if some are FAR, with values' so if some of them are, and a row's
+// reference that of its largest product of exponential and scale, which takes twice as long together.  To look costs a prompt of 8192
 // 688 us -> 697, one of 4096 with heads of 64 125 -> 130, of 256 328 -> 343, trees of 25 30.5
 // -> 31.6, 64 tokens 134.2 -> 134.7.
 constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
+constexpr int AGAIN = 1, FAR_KEYS = 2, FAR_VALUES = 4;  // what a pass asks for
 constexpr float LOST = 0x1p-7f;  // (2^-25, values up to 2^7, 2^11)
 constexpr float APART = 0x1p60f;
 __device__ inline bool is_apart(float before, float now) {
@@ -332,15 +333,15 @@ struct Rows16 {
       for (int i = 0; i < NX; ++i) o[i][j] = v4f{0, 0, 0, 0};
     }
   }
-  // Whether the scales that the rows saw, over n positions, ask for the other pass: 2 if some
-  // are FAR (keys' or the values'), else 1.
-  __device__ int asks(bool far, bool apart, int n) const {
+  // What the scales that the rows saw, over n positions, ask for.
+  __device__ int asks(bool far_keys, bool apart, int n) const {
     // (a few outputs of a row say it as a rule)
-    bool again = some_lost<1>(n);
+    bool again = some_lost<1>(n), far = false;
     if (__any(again)) again = some_lost<NX>(n);
 #pragma unroll
     for (int j = 0; j < NY; ++j) far |= big[j] >= FAR;
-    return (__any(far) ? 2 : 0) | (__any(again || apart) ? 1 : 0);
+    return (far_keys ? FAR_KEYS : 0) | (__any(far) ? FAR_VALUES : 0) |
+           (__any(again || apart) ? AGAIN : 0);
   }
   template <int X>
   __device__ bool some_lost(int n) const {
@@ -356,14 +357,14 @@ struct Rows16 {
     }
     return lost;
   }
-  // Before and after a pass with scales NEARER times as large: scores as they are; sums that
-  // are as much smaller as the outputs.
-  __device__ void nearer() {
+  // Scores as they are, of keys' scales NEARER times as large.
+  __device__ void nearer_keys() {
 #pragma unroll
     for (int j = 0; j < NY; ++j)
       factor[j] = factor[j] > LEAST ? factor[j] * (1 / NEARER) : factor[j];
   }
-  __device__ void as_they_are() {
+  // Sums that are as much smaller as the outputs of values' scales NEARER times as large.
+  __device__ void nearer_values() {
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
       ref[j] += 28;
@@ -588,10 +589,10 @@ __device__ inline void part_of(int length, int parts, int part, int unit, int &f
 // one's as soon as the scores are there, its values after the second product: no
 // register waits twice, and the other waves' work covers the rest of the way.
 //
-// ODD: the other pass, with scales that are `far` or not.  Returns whether the scales met ask for
-// it (2: some are FAR; the same in all threads); then nothing is stored.
+// ODD: the other pass, `given` what the first one asked for.  That returns what it asks for, the same in all
+// threads; if it does, nothing is stored.
 template <int D, int NY, bool ODD>
-__device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
+__device__ __forceinline__ int attend_few(const Work &w, char *lds, int given) {
   const AttendArgs &a = w.a;
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -661,6 +662,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
   constexpr int EACH = 64 * (4 * Rows16<D, NY>::NX * NY + 4 * NY);
   int *asked = (int *)lds + 2 * EACH;
   asked[4 + wave] = 0;
+  bool far_keys = false;  // (this wave's, the same in all lanes)
   // The scales of a step settled: the largest of the values', and whether one of the keys' is FAR.
   auto settle_step = [&](const int (&entries)[2], int t, float &most) {
     const int room = s.length - t - 4 * g;
@@ -698,7 +700,7 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
 
   if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
   else x.template load<f16>(a, s.first, row, first);
-  if (ODD && far) x.nearer();
+  if (given & FAR_KEYS) x.nearer_keys();
 
   for (; t < to; t += TURN) {
     const bool more = t + TURN < to;
@@ -744,11 +746,11 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
       if constexpr (ODD) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          fks[h] *= far ? NEARER : 1.f;
-          fvs[h] *= far ? NEARER : 1.f;
+          fks[h] *= given & FAR_KEYS ? NEARER : 1.f;
+          fvs[h] *= given & FAR_VALUES ? NEARER : 1.f;
         }
       } else {
-        far |= now_far;
+        far_keys |= now_far;
       }
     }
     v4i p[1][NY];
@@ -802,11 +804,11 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
       next[h] = later[h];
     }
   }
-  if (ODD && far) x.as_they_are();
+  if (given & FAR_VALUES) x.nearer_values();
 
   // The waves' sums together, in order: waves 2 and 3 to 0 and 1, 1 to 0.
   float *mine = (float *)lds;
-  if (!ODD) asked[wave] = far;
+  if (!ODD) asked[wave] = far_keys;
 #pragma unroll
   for (int half = 2; half >= 1; half /= 2) {
     if (wave >= half && wave < 2 * half) {
@@ -880,8 +882,8 @@ __device__ __forceinline__ int attend_few(const Work &w, char *lds, bool far) {
 // The scratch memory that the compiler reports is where it saves the kernel's registers.)
 template <int D, int NY>
 __device__ __attribute__((noinline)) void
-attend_few_odd(const Work *w, __attribute__((address_space(3))) char *lds, bool far) {
-  attend_few<D, NY, true>(*alike(w), (char *)lds, far);
+attend_few_odd(const Work *w, __attribute__((address_space(3))) char *lds, int given) {
+  attend_few<D, NY, true>(*alike(w), (char *)lds, given);
 }
 
 // (waves to a SIMD as the first pass has them by itself: the function would take more registers)
@@ -889,10 +891,10 @@ template <int D, int NY>
 __global__ void __launch_bounds__(256, (D == 64 ? 3 : D == 128 ? 2 : 1) + (D <= 128 && NY == 1))
     k_attend_few(Work w) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int again = attend_few<D, NY, false>(w, lds, false);
+  const int again = attend_few<D, NY, false>(w, lds, 0);
   if (again)
     attend_few_odd<D, NY>((const Work *)(const void *)__builtin_amdgcn_kernarg_segment_ptr(),
-                          (__attribute__((address_space(3))) char *)lds, again >= 2);
+                          (__attribute__((address_space(3))) char *)lds, again);
 }
 
 // MACS matrix instructions with VALUS vector instructions spread between them.
@@ -923,7 +925,7 @@ struct Many {
 
 // (ODD and what it returns as for attend_few)
 template <int D, int NY, bool ODD>
-__device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales_far) {
+__device__ __forceinline__ int attend_many(const Work &w, char *lds, int given) {
   using M = Many<D, NY>;
   const AttendArgs &a = w.a;
   const int lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
@@ -949,8 +951,8 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
   auto first = [&](int ks) { return 32 * ks + 8 * g; };
   if (a.dtype == ROSETTA_BF16) x.template load<bf16>(a, s.first, row, first);
   else x.template load<f16>(a, s.first, row, first);
-  uint64_t far = scales_far;
-  if (ODD && far) x.nearer();
+  if (given & FAR_KEYS) x.nearer_keys();
+  uint64_t far_keys = 0;  // lanes that met some
 
   // what some row of the workgroup sees, of this wave sees, and all of this wave's see
   const int n1 = s.n - 1;
@@ -1021,10 +1023,10 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
     float *scales = (float *)(stage + M::KEYS + M::VALUES);
     settle(sub.ks, sub.vs, m < sub.room);
     if constexpr (ODD) {
-      sub.ks *= far ? NEARER : 1.f;
-      sub.vs *= far ? NEARER : 1.f;
+      sub.ks *= given & FAR_KEYS ? NEARER : 1.f;
+      sub.vs *= given & FAR_VALUES ? NEARER : 1.f;
     } else {
-      far |= __ballot(fabsf(sub.ks) >= FAR);
+      far_keys |= __ballot(fabsf(sub.ks) >= FAR);
     }
     // the largest v_scale of the sixteen
     float most = fabsf(sub.vs);
@@ -1159,10 +1161,10 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
     if (t + 2 * M::TILE < to) load(t + 2 * M::TILE);
   }
   if constexpr (ODD) {
-    if (far) x.as_they_are();
+    if (given & FAR_VALUES) x.nearer_values();
   } else {
     // (what one wave asks for, all do: they write each other's tiles)
-    asked[wave] = x.asks(far, asked[4 + wave], to - from);
+    asked[wave] = x.asks(far_keys, asked[4 + wave], to - from);
     __syncthreads();
     const v4i all = *(const v4i *)asked;
     const int again = __builtin_amdgcn_readfirstlane(all[0] | all[1] | all[2] | all[3]);
@@ -1175,17 +1177,17 @@ __device__ __forceinline__ int attend_many(const Work &w, char *lds, bool scales
 
 template <int D, int NY>
 __device__ __attribute__((noinline)) void
-attend_many_odd(const Work *w, __attribute__((address_space(3))) char *lds, bool far) {
-  attend_many<D, NY, true>(*alike(w), (char *)lds, far);
+attend_many_odd(const Work *w, __attribute__((address_space(3))) char *lds, int given) {
+  attend_many<D, NY, true>(*alike(w), (char *)lds, given);
 }
 
 template <int D, int NY>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) k_attend_many(Work w) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int again = attend_many<D, NY, false>(w, lds, false);
+  const int again = attend_many<D, NY, false>(w, lds, 0);
   if (again)
     attend_many_odd<D, NY>((const Work *)(const void *)__builtin_amdgcn_kernarg_segment_ptr(),
-                           (__attribute__((address_space(3))) char *)lds, again >= 2);
+                           (__attribute__((address_space(3))) char *)lds, again);
 }
 
 // ---- parts of a sequence joined ----

@@ -261,3 +261,12 @@ def test_thirty_two_positions_of_small_values_among_large_ones(heads, dim, small
         b.scale[1][pg, :, at] *= 2.0 ** -58 if t // 32 == small else 2.0 ** 90
     q = torch.randn((1, heads, dim), generator=gen(118)).to(BF16)
     check(b, q)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_huge_scales_of_keys_beside_tiny_ones_of_values(name):
+    """That keys' scales are past 2^100 takes nothing from values of 2^-78."""
+    b, q = call(name, 119)
+    b.scale[0] *= torch.where(torch.rand(b.scale[0].shape, generator=gen(120)) < 0.3, 2.0 ** 120, 1.0)
+    b.scale[1] *= 2.0 ** -72
+    check(b, (q * 2.0 ** -120).to(BF16))
