@@ -117,7 +117,8 @@ __device__ inline float row_sum(float a) {
 //    score and of its largest scale, which need not be one position's: where the largest scale
 //    weighs little, all weights are small beside it.  f16 holds them, from 2^15 on, in steps of
 //    2^-24, so that n of them are off by n 2^-25 together; where the row's largest output is LOST
-//    times n or more, that is 2^-11 of it at most.
+//    times n or more, that is 2^-11 of it at most.  It is PLENTY, too, or more, so that the largest
+//    weight is 2^-2 at least and those beside it have their bits.
 //  - they do not grow by APART from one step to the next: what was added up would be 0 beside
 //    them.
 // Where one does not hold, the pass is made again, with keys' scales 2^-28 as large (and 2^28
@@ -127,7 +128,7 @@ __device__ inline float row_sum(float a) {
 // -> 31.6, 64 tokens 134.2 -> 134.7.
 constexpr float FAR = 0x1p100f, NEARER = 0x1p-28f;
 constexpr int AGAIN = 1, FAR_KEYS = 2, FAR_VALUES = 4;  // what a pass asks for
-constexpr float LOST = 0x1p-7f;  // (2^-25, values up to 2^7, 2^11)
+constexpr float LOST = 0x1p-7f, PLENTY = 32;  // (2^-25, values up to 2^7, 2^11; 2^-2 2^7)
 constexpr float APART = 0x1p60f;
 __device__ inline bool is_apart(float before, float now) {
   return now > before * APART && before > 0.f;
@@ -345,6 +346,7 @@ struct Rows16 {
   }
   template <int X>
   __device__ bool some_lost(int n) const {
+    const float enough = fmaxf((float)n * LOST, PLENTY);
     bool lost = false;
 #pragma unroll
     for (int j = 0; j < NY; ++j) {
@@ -353,7 +355,7 @@ struct Rows16 {
       for (int i = 0; i < X; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) l = max2(l, fabsf(o[i][j][r]));
-      lost |= row_max(l) < (float)n * LOST && big[j] > 0.f && sum[j] > 0.f;
+      lost |= row_max(l) < enough && big[j] > 0.f && sum[j] > 0.f;
     }
     return lost;
   }

@@ -270,3 +270,20 @@ def test_huge_scales_of_keys_beside_tiny_ones_of_values(name):
     b.scale[0] *= torch.where(torch.rand(b.scale[0].shape, generator=gen(120)) < 0.3, 2.0 ** 120, 1.0)
     b.scale[1] *= 2.0 ** -72
     check(b, (q * 2.0 ** -120).to(BF16))
+
+
+@pytest.mark.parametrize("heads", [1, 40])
+def test_words_of_few_positions_keep_their_bits(heads):
+    """Thirty-two positions: one of a large scale and no weight, one that weighs almost all, and
+    ones of 2^-12 of its product, which alone make some of the outputs."""
+    b = Batch([(1, 32)], 1, 64, 16, seed=121)
+    q = torch.ones((1, heads, 64))
+    for t in range(32):
+        pg, at = b.place(0, t)
+        b.q8[0][pg, :, at] = 100 if t == 9 else -100 if t == 3 else 0
+        b.scale[0][pg, :, at] = 10 / 800  # scores of 10, 0 and -10
+        # (0.878 e^-10 2^-6 is 10.4 of f16's steps of 2^-24)
+        b.scale[1][pg, :, at] = 2.0 ** 14 if t == 3 else 2.0 ** -8 if t == 9 else 0.878 * 2.0 ** -6
+        b.q8[1][pg, :, at, :32] = 0 if t in (3, 9) else b.q8[1][pg, :, at, :32]
+    b.scale[0][b.place(0, 3)[0], :, b.place(0, 3)[1]] *= 3
+    check(b, q.to(BF16))
